@@ -325,6 +325,139 @@ slicemoe_status slicemoe_backward(const slicemoe_config *cfg, const void *h, con
                                   const void *d_out, void *d_h, const slicemoe_weight_grads *grads,
                                   void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
 
+/*
+ * ---- Operators around the layer in a transformer block -----------------------------------------------------------------
+ * The layer reads normalised rows and adds to a residual stream (both outside of it, as in the paper), often beside a
+ * feed-forward network that every token takes, and its gradients are bounded before an optimizer uses them.  The
+ * conventions above hold for these entry points too: caller-allocated device memory, 16-byte aligned unless it says otherwise,
+ * kernels on `stream` only (nothing here uses another stream), no allocation, no host synchronisation, bit-identical
+ * results for the same inputs, and calls may be captured into a HIP graph.  Calls that overlap in time need workspaces of
+ * their own.  Arrays are contiguous; an output may take an input's place only where that is said.
+ */
+typedef struct {
+    int32_t T;     /* rows (tokens), 0 <= T                                                  */
+    int32_t d;     /* row width, 1 <= d <= 16384                                             */
+    float eps;     /* >= 0, finite                                                           */
+    int32_t dtype; /* slicemoe_dtype                                                         */
+} slicemoe_norm_config;
+
+/*
+ * Root-mean-square norm with the residual's addition: s = x + residual, y = s / sqrt(mean(s^2) + eps) * weight, in fp32
+ * throughout; y is taken of the fp32 sum and rounded once.
+ *   x         [T, d] in
+ *   residual  [T, d] in, may be NULL: then s = x
+ *   weight    [d]    in
+ *   sum       [T, d] out, s in the storage dtype; may be NULL; may be x or residual
+ *   y         [T, d] out, storage dtype; may be NULL when y_quantized is given; may be x or residual if sum is not that one
+ *   y_quantized [T, d] out, may be NULL: the same rows as OCP e4m3 bytes, y / y_scale rounded to nearest even
+ *   y_scale   [T] out float, with y_quantized: max|y| of the row / 448, where a maximum below 1e-30 counts as 1e-30 (a row
+ *             of zeros); NaN for a row that holds a NaN or an infinity
+ */
+slicemoe_status slicemoe_add_rmsnorm(const slicemoe_norm_config *cfg, const void *x, const void *residual, const void *weight,
+                                     void *sum, void *y, void *y_quantized, float *y_scale, slicemoe_stream_t stream);
+
+/*
+ * Its backward pass, from the stored sum (the forward keeps nothing else):
+ *   sum   [T, d] in
+ *   d_y   [T, d] in, dL/dy
+ *   d_sum [T, d] in, the gradient that reaches s along the residual stream; may be NULL (zero)
+ *   d_x   [T, d] out, dL/ds, the gradient of x and of residual alike; one rounding; may be d_y or d_sum
+ *   d_weight [d] out float, overwritten (zeros for T = 0)
+ *   workspace >= slicemoe_add_rmsnorm_backward_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; its size never
+ *             falls as T grows
+ */
+size_t slicemoe_add_rmsnorm_backward_workspace_bytes(const slicemoe_norm_config *cfg);
+slicemoe_status slicemoe_add_rmsnorm_backward(const slicemoe_norm_config *cfg, const void *sum, const void *weight, const void *d_y,
+                                              const void *d_sum, void *d_x, float *d_weight, void *workspace,
+                                              size_t workspace_bytes, slicemoe_stream_t stream);
+
+typedef struct {
+    int32_t T;     /* rows (tokens), 0 <= T < 2^30                                           */
+    int32_t d;     /* row width, 1 <= d <= 2^20                                              */
+    int32_t H;     /* hidden width, 1 <= H <= 2^20; T * max(d, H) <= 2^40                    */
+    int32_t dtype; /* slicemoe_dtype                                                         */
+} slicemoe_gated_config;
+typedef struct {
+    const void *Wg; /* [d, H] gate projection */
+    const void *Wu; /* [d, H] up projection   */
+    const void *Wd; /* [H, d] down projection */
+} slicemoe_gated_weights;
+typedef struct {
+    void *Wg, *Wu, *Wd;
+} slicemoe_gated_weight_grads;
+
+/*
+ * Gated feed-forward network: y = addend + (silu(x Wg) * (x Wu)) Wd, silu(g) = g / (1 + exp(-g)).  With addend = h' of the
+ * layer it is the expert that every token takes beside the routed ones.
+ *   x [T, d] in;  addend [T, d] in, may be NULL (zero);  y [T, d] out, may be addend or x
+ *   workspace >= slicemoe_gated_ffn_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; its size never falls as T
+ *             grows
+ * All products run on the bf16 matrix cores with fp32 accumulation.  bf16 storage: the hidden row silu(g) u is rounded to bf16
+ * once between the products.  fp32 storage: every operand enters as three bf16 terms that keep its 24 bits, results of fp32 grade;
+ * an infinity in an operand may come out as NaN.  Widths that are not multiples of 8 (and fp32) are laid out again in the workspace first.
+ * A row's result does not depend on the other rows, but the order of its sums depends on T.
+ */
+size_t slicemoe_gated_ffn_workspace_bytes(const slicemoe_gated_config *cfg);
+slicemoe_status slicemoe_gated_ffn(const slicemoe_gated_config *cfg, const void *x, const slicemoe_gated_weights *w,
+                                   const void *addend, void *y, void *workspace, size_t workspace_bytes,
+                                   slicemoe_stream_t stream);
+
+/*
+ * Its backward pass.  The forward keeps nothing: both projections are computed again.
+ *   x, w     as given to the forward;  d_y [T, d] in, dL/dy
+ *   addend   [T, d] in, added to dL/dx (the gradient that reaches x elsewhere, such as d_h of the layer); may be NULL
+ *   d_x      [T, d] out, storage dtype, one rounding; may be d_y or addend
+ *   grads    out, one array per matrix in its layout, overwritten.  In the STORAGE dtype, unlike the layer's: their products take
+ *            the hidden gradients as bf16 with bf16 storage, so an fp32 array would hold eight significant bits.
+ *   workspace >= slicemoe_gated_ffn_backward_workspace_bytes(cfg), as above
+ */
+size_t slicemoe_gated_ffn_backward_workspace_bytes(const slicemoe_gated_config *cfg);
+slicemoe_status slicemoe_gated_ffn_backward(const slicemoe_gated_config *cfg, const void *x, const slicemoe_gated_weights *w,
+                                            const void *d_y, const void *addend, void *d_x,
+                                            const slicemoe_gated_weight_grads *grads, void *workspace, size_t workspace_bytes,
+                                            slicemoe_stream_t stream);
+
+/*
+ * The network for serving with 8-bit operands in its first two products, the larger part of its work: x as
+ * slicemoe_add_rmsnorm leaves it (e4m3 rows and their scales), Wg and Wu as slicemoe_gated_ffn_quantize_weights leaves them (row h
+ * holds column h of the matrix, with a scale).  g = (x_quantized . Wg[h]) x_scale Wg_scale[h]; hidden rows, Wd, addend and y are bf16.
+ * dtype must be SLICEMOE_BF16 and d a multiple of 16 (UNSUPPORTED otherwise).
+ */
+typedef struct {
+    const void *Wg, *Wu;                    /* [H, d] e4m3 bytes */
+    const float *Wg_scale, *Wu_scale;       /* [H]               */
+    const void *Wd;                         /* [H, d] bf16       */
+} slicemoe_gated_weights_quantized;
+size_t slicemoe_gated_ffn_quantized_workspace_bytes(const slicemoe_gated_config *cfg);
+slicemoe_status slicemoe_gated_ffn_quantized(const slicemoe_gated_config *cfg, const void *x_quantized, const float *x_scale,
+                                             const slicemoe_gated_weights_quantized *w, const void *addend, void *y,
+                                             void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
+/* One-time conversion of Wg and Wu (cfg->T is not read): scale = max|column| / 448 as in slicemoe_add_rmsnorm. */
+slicemoe_status slicemoe_gated_ffn_quantize_weights(const slicemoe_gated_config *cfg, const slicemoe_gated_weights *w,
+                                                    void *Wg, float *Wg_scale, void *Wu, float *Wu_scale,
+                                                    slicemoe_stream_t stream);
+
+/*
+ * Norm of all gradients together, and its bounding: norm = sqrt(sum of g^2 over every tensor) (squares and sums in 64 bits),
+ * factor = min(1, max_norm / (norm + 1e-6)), out = g * factor, rounded once to the tensor's dtype.  A norm that is not finite
+ * carries into the factor as the formula says (NaN, or 0).
+ *   grads     HOST array of `count` tensors, read during the call; count may be 0
+ *   max_norm  >= 0; INFINITY only measures (factor 1)
+ *   norm      out float, 4-byte aligned
+ *   workspace >= slicemoe_clip_grads_workspace_bytes(grads, count) (0 on invalid arguments), 256-byte aligned
+ * out of a tensor may be its own grad (in place), or NULL (the tensor is measured, not written).  INVALID_ARG if any out overlaps
+ * another tensor or its own grad in part: the same tensor listed twice, for instance.
+ */
+typedef struct {
+    const void *grad; /* n elements, aligned to its element size; may be NULL if n is 0 */
+    void *out;
+    int64_t n;
+    int32_t dtype;    /* slicemoe_dtype */
+} slicemoe_grad;
+size_t slicemoe_clip_grads_workspace_bytes(const slicemoe_grad *grads, int32_t count);
+slicemoe_status slicemoe_clip_grads(const slicemoe_grad *grads, int32_t count, float max_norm, float *norm,
+                                    void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,6 +32,10 @@ EXPORTS = [
     "slicemoe_combine", "slicemoe_load_stats", "slicemoe_forward",
     "slicemoe_route_train", "slicemoe_forward_train", "slicemoe_backward_workspace_bytes", "slicemoe_backward",
     "slicemoe_backward_uses_mfma", "slicemoe_dispatch_noalloc",
+    "slicemoe_add_rmsnorm", "slicemoe_add_rmsnorm_backward_workspace_bytes", "slicemoe_add_rmsnorm_backward",
+    "slicemoe_gated_ffn_workspace_bytes", "slicemoe_gated_ffn", "slicemoe_gated_ffn_backward_workspace_bytes",
+    "slicemoe_gated_ffn_backward", "slicemoe_gated_ffn_quantized_workspace_bytes", "slicemoe_gated_ffn_quantized",
+    "slicemoe_gated_ffn_quantize_weights", "slicemoe_clip_grads_workspace_bytes", "slicemoe_clip_grads",
 ]
 
 
@@ -63,6 +67,30 @@ class slicemoe_weight_grads(ctypes.Structure):
 class slicemoe_workspace_layout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in ("topk_idx", "topk_p", "counts_raw", "counts", "offsets", "perm",
                                                "inv", "y", "stats", "scratch", "packed", "total")]
+
+
+class slicemoe_norm_config(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class slicemoe_gated_config(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("H", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class slicemoe_gated_weights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("Wg", "Wu", "Wd")]
+
+
+class slicemoe_gated_weight_grads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("Wg", "Wu", "Wd")]
+
+
+class slicemoe_gated_weights_quantized(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("Wg", "Wu", "Wg_scale", "Wu_scale", "Wd")]
+
+
+class slicemoe_grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -115,6 +143,20 @@ def lib() -> ctypes.CDLL:
         L.slicemoe_backward.restype = ctypes.c_int
         L.slicemoe_backward.argtypes = [cfgp, vp, wp, tpp, vp, vp, vp, st, vp, vp, ctypes.POINTER(slicemoe_weight_grads),
                                         vp, st, vp]
+        ncp, gcp = ctypes.POINTER(slicemoe_norm_config), ctypes.POINTER(slicemoe_gated_config)
+        gwp, grp = ctypes.POINTER(slicemoe_gated_weights), ctypes.POINTER(slicemoe_grad)
+        for f, a in ((L.slicemoe_add_rmsnorm_backward_workspace_bytes, [ncp]), (L.slicemoe_gated_ffn_workspace_bytes, [gcp]),
+                     (L.slicemoe_gated_ffn_backward_workspace_bytes, [gcp]), (L.slicemoe_gated_ffn_quantized_workspace_bytes, [gcp]),
+                     (L.slicemoe_clip_grads_workspace_bytes, [grp, ctypes.c_int32])):
+            f.restype, f.argtypes = st, a
+        for f, a in ((L.slicemoe_add_rmsnorm, [ncp, vp, vp, vp, vp, vp, vp, vp, vp]),
+                     (L.slicemoe_add_rmsnorm_backward, [ncp, vp, vp, vp, vp, vp, vp, vp, st, vp]),
+                     (L.slicemoe_gated_ffn, [gcp, vp, gwp, vp, vp, vp, st, vp]),
+                     (L.slicemoe_gated_ffn_backward, [gcp, vp, gwp, vp, vp, vp, ctypes.POINTER(slicemoe_gated_weight_grads), vp, st, vp]),
+                     (L.slicemoe_gated_ffn_quantized, [gcp, vp, vp, ctypes.POINTER(slicemoe_gated_weights_quantized), vp, vp, vp, st, vp]),
+                     (L.slicemoe_gated_ffn_quantize_weights, [gcp, gwp, vp, vp, vp, vp, vp]),
+                     (L.slicemoe_clip_grads, [grp, ctypes.c_int32, ctypes.c_float, vp, vp, st, vp])):
+            f.restype, f.argtypes = ctypes.c_int, a
         _lib = L
     return _lib
 
@@ -362,6 +404,138 @@ def slicemoe_backward(cfg, h, w, forward_workspace, d_out, d_h, grads: dict, wor
                                    npt, upt, fwp, fwb, _ptr(d_out, _tdtype(cfg), cfg.T * cfg.d, "d_out"),
                                    _ptr(d_h, _tdtype(cfg), cfg.T * cfg.d, "d_h"), ctypes.byref(g), wsp, wsb,
                                    _stream(stream)), "slicemoe_backward")
+
+
+# ------------------------------------------------------------------ operators around the layer
+def _dtype_code(dtype):
+    return SLICEMOE_BF16 if dtype in ("bf16", SLICEMOE_BF16) else SLICEMOE_F32
+
+
+def make_norm_config(T, d, eps=1e-5, dtype="bf16") -> slicemoe_norm_config:
+    return slicemoe_norm_config(T, d, float(eps), _dtype_code(dtype))
+
+
+def make_gated_config(T, d, H, dtype="bf16") -> slicemoe_gated_config:
+    return slicemoe_gated_config(T, d, H, _dtype_code(dtype))
+
+
+def _bytes_ptr(t, numel, name):
+    """Address of e4m3 values: a float8_e4m3fn tensor, or its bytes."""
+    if t is not None and isinstance(t, torch.Tensor) and t.dtype == torch.uint8:
+        return _ptr(t, torch.uint8, numel, name)
+    return _ptr(t, torch.float8_e4m3fn, numel, name)
+
+
+def slicemoe_add_rmsnorm(cfg, x, residual, weight, sum_out, y, y_quantized=None, y_scale=None, stream=None):
+    """residual, sum_out and, with y_quantized, y may be None."""
+    dt, n = _tdtype(cfg), cfg.T * cfg.d
+    _check(lib().slicemoe_add_rmsnorm(ctypes.byref(cfg), _ptr(x, dt, n, "x"), _ptr(residual, dt, n, "residual"),
+                                      _ptr(weight, dt, cfg.d, "weight"), _ptr(sum_out, dt, n, "sum_out"), _ptr(y, dt, n, "y"),
+                                      _bytes_ptr(y_quantized, n, "y_quantized"), _ptr(y_scale, torch.float32, cfg.T, "y_scale"),
+                                      _stream(stream)), "slicemoe_add_rmsnorm")
+
+
+def slicemoe_add_rmsnorm_backward_workspace_bytes(cfg) -> int:
+    return lib().slicemoe_add_rmsnorm_backward_workspace_bytes(ctypes.byref(cfg))
+
+
+def slicemoe_add_rmsnorm_backward(cfg, sum_in, weight, d_y, d_x, d_weight, workspace, d_sum=None, stream=None):
+    dt, n = _tdtype(cfg), cfg.T * cfg.d
+    wsp, wsb = _ws(workspace)
+    _check(lib().slicemoe_add_rmsnorm_backward(ctypes.byref(cfg), _ptr(sum_in, dt, n, "sum_in"), _ptr(weight, dt, cfg.d, "weight"),
+                                               _ptr(d_y, dt, n, "d_y"), _ptr(d_sum, dt, n, "d_sum"), _ptr(d_x, dt, n, "d_x"),
+                                               _ptr(d_weight, torch.float32, cfg.d, "d_weight"), wsp, wsb, _stream(stream)),
+           "slicemoe_add_rmsnorm_backward")
+
+
+def slicemoe_gated_ffn_workspace_bytes(cfg) -> int:
+    return lib().slicemoe_gated_ffn_workspace_bytes(ctypes.byref(cfg))
+
+
+def slicemoe_gated_ffn_backward_workspace_bytes(cfg) -> int:
+    return lib().slicemoe_gated_ffn_backward_workspace_bytes(ctypes.byref(cfg))
+
+
+def slicemoe_gated_ffn_quantized_workspace_bytes(cfg) -> int:
+    return lib().slicemoe_gated_ffn_quantized_workspace_bytes(ctypes.byref(cfg))
+
+
+def _gated_weights(cfg, w, kind=slicemoe_gated_weights, what="", down=True):
+    dt, n = _tdtype(cfg), cfg.d * cfg.H
+    return kind(_ptr(w["Wg"], dt, n, what + "Wg"), _ptr(w["Wu"], dt, n, what + "Wu"), _ptr(w["Wd"], dt, n, what + "Wd") if down else None)
+
+
+def slicemoe_gated_ffn(cfg, x, w, y, workspace, addend=None, stream=None):
+    """w: dict of Wg, Wu [d, H] and Wd [H, d]."""
+    dt, n = _tdtype(cfg), cfg.T * cfg.d
+    wsp, wsb = _ws(workspace)
+    ws = _gated_weights(cfg, w)
+    _check(lib().slicemoe_gated_ffn(ctypes.byref(cfg), _ptr(x, dt, n, "x"), ctypes.byref(ws), _ptr(addend, dt, n, "addend"),
+                                    _ptr(y, dt, n, "y"), wsp, wsb, _stream(stream)), "slicemoe_gated_ffn")
+
+
+def slicemoe_gated_ffn_backward(cfg, x, w, d_y, d_x, grads, workspace, addend=None, stream=None):
+    """grads: dict of Wg, Wu, Wd in the storage dtype, overwritten."""
+    dt, n = _tdtype(cfg), cfg.T * cfg.d
+    wsp, wsb = _ws(workspace)
+    ws, g = _gated_weights(cfg, w), _gated_weights(cfg, grads, slicemoe_gated_weight_grads, "grads.")
+    _check(lib().slicemoe_gated_ffn_backward(ctypes.byref(cfg), _ptr(x, dt, n, "x"), ctypes.byref(ws), _ptr(d_y, dt, n, "d_y"),
+                                             _ptr(addend, dt, n, "addend"), _ptr(d_x, dt, n, "d_x"), ctypes.byref(g), wsp, wsb,
+                                             _stream(stream)), "slicemoe_gated_ffn_backward")
+
+
+def slicemoe_gated_ffn_quantized(cfg, x_quantized, x_scale, w, y, workspace, addend=None, stream=None):
+    """w: dict of Wg, Wu [H, d] e4m3 with Wg_scale, Wu_scale [H], and Wd [H, d] bf16 (see quantize_gated_weights)."""
+    n, nw, f32 = cfg.T * cfg.d, cfg.d * cfg.H, torch.float32
+    wsp, wsb = _ws(workspace)
+    ws = slicemoe_gated_weights_quantized(_bytes_ptr(w["Wg"], nw, "Wg"), _bytes_ptr(w["Wu"], nw, "Wu"), _ptr(w["Wg_scale"], f32, cfg.H, "Wg_scale"),
+                                          _ptr(w["Wu_scale"], f32, cfg.H, "Wu_scale"), _ptr(w["Wd"], torch.bfloat16, nw, "Wd"))
+    _check(lib().slicemoe_gated_ffn_quantized(ctypes.byref(cfg), _bytes_ptr(x_quantized, n, "x_quantized"), _ptr(x_scale, f32, cfg.T, "x_scale"),
+                                              ctypes.byref(ws), _ptr(addend, torch.bfloat16, n, "addend"),
+                                              _ptr(y, torch.bfloat16, n, "y"), wsp, wsb, _stream(stream)), "slicemoe_gated_ffn_quantized")
+
+
+def slicemoe_gated_ffn_quantize_weights(cfg, w, Wg, Wg_scale, Wu, Wu_scale, stream=None):
+    nw, f32 = cfg.d * cfg.H, torch.float32
+    ws = _gated_weights(cfg, w, down=False)
+    _check(lib().slicemoe_gated_ffn_quantize_weights(ctypes.byref(cfg), ctypes.byref(ws), _bytes_ptr(Wg, nw, "Wg"),
+                                                     _ptr(Wg_scale, f32, cfg.H, "Wg_scale"), _bytes_ptr(Wu, nw, "Wu"),
+                                                     _ptr(Wu_scale, f32, cfg.H, "Wu_scale"), _stream(stream)),
+           "slicemoe_gated_ffn_quantize_weights")
+
+
+def quantize_gated_weights(cfg, w: dict, device="cuda:0") -> dict:
+    """The weight dict that slicemoe_gated_ffn_quantized takes, from the bf16 one (Wd is shared)."""
+    q = {n: torch.empty((cfg.H, cfg.d), dtype=torch.float8_e4m3fn, device=device) for n in ("Wg", "Wu")}
+    q.update({n: torch.empty(cfg.H, dtype=torch.float32, device=device) for n in ("Wg_scale", "Wu_scale")})
+    slicemoe_gated_ffn_quantize_weights(cfg, w, q["Wg"], q["Wg_scale"], q["Wu"], q["Wu_scale"])
+    return {**q, "Wd": w["Wd"]}
+
+
+def _grad_list(grads, out):
+    """C array of a list of gradient tensors; out: the list written, the same list for in place, or None to measure only."""
+    if out is not None and len(out) != len(grads):
+        raise ValueError("out must have as many tensors as grads")
+    arr = (slicemoe_grad * max(1, len(grads)))()
+    for i, g in enumerate(grads):
+        p = _ptr(g, None, None, f"grads[{i}]")
+        if p is None or g.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"grads[{i}] must be a float32 or bfloat16 tensor")
+        a = arr[i]
+        a.grad, a.n, a.dtype = p, g.numel(), SLICEMOE_BF16 if g.dtype == torch.bfloat16 else SLICEMOE_F32
+        a.out = None if out is None else _ptr(out[i], g.dtype, g.numel(), f"out[{i}]")
+    return arr
+
+
+def slicemoe_clip_grads_workspace_bytes(grads) -> int:
+    return lib().slicemoe_clip_grads_workspace_bytes(_grad_list(grads, None), len(grads))
+
+
+def slicemoe_clip_grads(grads, max_norm, norm, workspace, out=None, stream=None):
+    """out: the tensors written (grads itself for in place); None leaves all of them as they are and only measures."""
+    wsp, wsb = _ws(workspace)
+    _check(lib().slicemoe_clip_grads(_grad_list(grads, out), len(grads), max_norm, _ptr(norm, torch.float32, 1, "norm"), wsp, wsb,
+                                     _stream(stream)), "slicemoe_clip_grads")
 
 
 # ------------------------------------------------------------------ plumbing helpers (device memory only)

@@ -1,0 +1,16 @@
+// Global gradient norm and clipping (clip.hip).
+#pragma once
+#include "common.h"
+
+namespace slicemoe {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipChunks = 2048;
+struct ClipPlan {
+    int chunk;          // elements per chunk
+    long long chunks;   // of all tensors: one 64-bit partial sum each
+};
+ClipPlan clip_plan(const slicemoe_grad *g, int count);
+hipError_t launch_clip_grads(const slicemoe_grad *g, int count, const ClipPlan &plan, float max_norm, float *norm, double *part, hipStream_t s);
+
+}  // namespace slicemoe

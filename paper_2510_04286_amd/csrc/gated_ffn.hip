@@ -1,0 +1,771 @@
+// Gated feed-forward network that every token takes, forward and backward:
+//
+//   g = x Wg,  u = x Wu,  a = silu(g) u,  y = addend + a Wd                      (silu(g) = g sg,  sg = 1 / (1 + exp(-g)))
+//   da = dy Wd^T,  dg = da u (sg + g sg (1 - sg)),  du = da g sg
+//   dx = addend + dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  dWd = a^T dy
+#include <algorithm>
+
+#include "gated_ffn.h"
+#include "gemm_tile.h"
+#include "norm.h"
+
+namespace slicemoe {
+
+// ---- fp32 values as bf16 terms -------------------------------------------------------------------------------------------
+// fp32 storage: an operand is the sum of three bf16 values, cut off rather than rounded, so that the first two remainders are exact
+// and all 24 bits are kept.  A product is the six products of terms whose orders add up to at most two, largest first (the matrix
+// instruction cuts its accumulator when the products outweigh it); what is left out is below 2^-24 of the product.
+// Six bf16 products run at 2.6 times the rate of the fp32 matrix instruction.
+constexpr int kPairs = 6;
+constexpr int kPairR[kPairs] = {0, 0, 1, 1, 0, 2}, kPairF[kPairs] = {0, 1, 0, 1, 2, 0};
+
+__device__ __forceinline__ void split_terms(float v, bf16_t (&t)[3])
+{
+    const uint32_t b = __float_as_uint(v);
+    t[0] = (bf16_t)(b >> 16);
+    const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+    if ((b & 0x7fffffffu) > 0x7f800000u) t[0] |= 0x40;   // a NaN whose payload is in the lower half stays one
+    const float r1 = finite ? v - __uint_as_float(b & 0xffff0000u) : 0.f;
+    const uint32_t b1 = __float_as_uint(r1);
+    t[1] = (bf16_t)(b1 >> 16);
+    t[2] = f32_to_bf16(r1 - __uint_as_float(b1 & 0xffff0000u));
+}
+
+// Eight values of a row as bf16 terms, zeros past the row's end (up to a whole 16-byte piece).
+template <int TERMS> __device__ __forceinline__ void store_terms(bf16_t *p, size_t term, int col, int cols, const float *v)
+{
+    union {
+        bf16_t h[8];
+        uint4 q;
+    } o[TERMS];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = col + i < cols ? v[i] : 0.f;
+        if constexpr (TERMS == 3) {
+            bf16_t t[3];
+            split_terms(x, t);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) o[k].h[i] = t[k];
+        } else
+            o[0].h[i] = f32_to_bf16(x);
+    }
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) *(uint4 *)(p + k * term + col) = o[k].q;
+}
+
+struct CopyJob {
+    const void *src;
+    bf16_t *dst;
+    int rows, cols, ld;
+};
+struct CopyJobs {
+    CopyJob j[5];
+    int f32;
+};
+// One 16-byte piece of the copy per thread.
+__global__ __launch_bounds__(256) void gated_copy_kernel(CopyJobs jobs)
+{
+    const CopyJob j = jobs.j[blockIdx.y];
+    const int per_row = j.ld / 8;
+    const long long n = (long long)j.rows * per_row;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const long long row = i / per_row;
+        const int col = (int)(i - row * per_row) * 8;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const size_t at = (size_t)row * j.cols + col + k;
+            v[k] = col + k < j.cols ? (jobs.f32 ? ((const float *)j.src)[at] : bf16_to_f32(((const bf16_t *)j.src)[at])) : 0.f;
+        }
+        bf16_t *d = j.dst + (size_t)row * j.ld;
+        if (jobs.f32) store_terms<3>(d, (size_t)j.rows * j.ld, col, j.cols, v);
+        else store_terms<1>(d, 0, col, j.cols, v);
+    }
+}
+
+// ---- epilogues -----------------------------------------------------------------------------------------------------------
+// 32 rows of a wavefront's accumulators (of NT feature tiles) leave through its own part of the LDS, so that eight consecutive
+// features of a row come to one lane: put(row of the 32, feature of the tiles, eight values).
+template <int NT, typename GET, typename PUT> __device__ __forceinline__ void store_rows(char *lds, const GET &get, const PUT &put)
+{
+    constexpr int W = 32 * NT, STRIDE = W + 4, PIECES = W / 8;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & 31, g = lane >> 5;
+    float *st = (float *)lds + wave * 32 * STRIDE;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const f32x16 v = get(t);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *(f32x4 *)(st + j * STRIDE + 32 * t + 8 * q + 4 * g) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    }
+    wave_lds_sync();
+#pragma unroll
+    for (int i = 0; i < PIECES / 2; ++i) {
+        const int k = i * 64 + lane, r = k / PIECES, c = k % PIECES;
+        const f32x4 lo = *(const f32x4 *)(st + r * STRIDE + 8 * c), hi = *(const f32x4 *)(st + r * STRIDE + 8 * c + 4);
+        const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        put(r, 8 * c, v);
+    }
+    wave_lds_sync();
+    __builtin_amdgcn_sched_barrier(0);   // (the next rows' accumulators stay where they are until then)
+}
+constexpr int stage_bytes(int nt) { return 4 * 32 * (32 * nt + 4) * 4; }
+
+struct Out {
+    void *p;              // [rows][cols], bf16 or fp32
+    const void *addend;   // the same layout, or none
+    int rows, cols;
+    int f32;
+};
+// out = addend + v for eight columns of a row; rows are whole 16-byte pieces or not.
+__device__ __forceinline__ void put_out(const Out &o, int row, int col, const float *v)
+{
+    if (row >= o.rows || col >= o.cols) return;
+    const size_t at = (size_t)row * o.cols + col;
+    if ((o.cols & 7) == 0) {
+        if (o.f32) {
+            f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+            if (o.addend) {
+                a += *(const f32x4 *)((const float *)o.addend + at);
+                b += *(const f32x4 *)((const float *)o.addend + at + 4);
+            }
+            *(f32x4 *)((float *)o.p + at) = a;
+            *(f32x4 *)((float *)o.p + at + 4) = b;
+        } else {
+            u32x4 d = {0, 0, 0, 0}, r;
+            if (o.addend) d = *(const u32x4 *)((const bf16_t *)o.addend + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                r[i] = (uint32_t)f32_to_bf16(v[2 * i] + __uint_as_float(d[i] << 16)) |
+                       (uint32_t)f32_to_bf16(v[2 * i + 1] + __uint_as_float(d[i] & 0xffff0000u)) << 16;
+            *(u32x4 *)((bf16_t *)o.p + at) = r;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (col + i >= o.cols) break;
+        if (o.f32) ((float *)o.p)[at + i] = v[i] + (o.addend ? ((const float *)o.addend)[at + i] : 0.f);
+        else ((bf16_t *)o.p)[at + i] = f32_to_bf16(v[i] + (o.addend ? bf16_to_f32(((const bf16_t *)o.addend)[at + i]) : 0.f));
+    }
+}
+
+template <bool PRECISE> __device__ __forceinline__ float sigmoid(float g)
+{
+    if constexpr (PRECISE) return 1.f / (1.f + expf(-g));
+    return __builtin_amdgcn_rcpf(1.f + __expf(-g));
+}
+
+struct Hidden {
+    bf16_t *p[3];         // a, dg, du: [terms][rows][ld]
+    int rows, cols, ld;
+};
+template <int TERMS> __device__ __forceinline__ void put_hidden(const Hidden &h, int which, int row, int col, const float *v)
+{
+    if (row >= h.rows || col >= h.cols) return;
+    store_terms<TERMS>(h.p[which] + (size_t)row * h.ld, (size_t)h.rows * h.ld, col, h.cols, v);
+}
+
+struct Scales {
+    const float *x, *g, *u;   // per row of x, per hidden unit of Wg and Wu (e4m3 operands)
+};
+
+// ---- kernels -------------------------------------------------------------------------------------------------------------
+template <typename S> __device__ __forceinline__ void clear(f32x16 (&acc)[S::TF][S::TR])
+{
+#pragma unroll
+    for (int t = 0; t < S::TF; ++t)
+#pragma unroll
+        for (int u = 0; u < S::TR; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[t][u][i] = 0.f;
+}
+
+__device__ __forceinline__ void share_of(const GemmProblem &p, int split, int &s0, int &s1)
+{
+    const int steps = p.segments * ((p.K + 127) >> 7), each = (steps + p.splits - 1) / p.splits;
+    s0 = split * each;
+    s1 = s0 + each < steps ? s0 + each : steps;
+}
+
+// Both projections and the gate.  part: the raw sums of a share instead, [split][2][rows][ld] fp32.
+template <typename S, int TERMS>
+__global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, Scales sc, float *__restrict__ part)
+{
+    extern __shared__ __align__(1024) char lds[];
+    const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, p.splits);
+    const int row0 = at.r * S::BR, f0 = at.f * S::BF, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    f32x16 acc[S::TF][S::TR];
+    clear<S>(acc);
+    int s0, s1;
+    share_of(p, at.split, s0, s1);
+    mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
+    const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
+    if (part) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const Out o = {part + (size_t)(2 * at.split + m) * h.rows * h.ld, nullptr, h.rows, h.ld, 1};
+#pragma unroll
+            for (int u = 0; u < S::TR; ++u)
+                store_rows<S::FT>(lds, [&](int t) { return acc[m * S::FT + t][u]; },
+                                  [&](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); });
+        }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < S::TR; ++u) {
+        float sx = 1.f;
+        if constexpr (S::E4M3) {
+            const int r = row + 32 * u + (lane & 31);
+            sx = sc.x[r < h.rows ? r : h.rows - 1];
+        }
+        const auto gated = [&](int t) {
+            f32x16 a;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float g = acc[t][u][i], v = acc[S::FT + t][u][i];
+                if constexpr (S::E4M3) {
+                    int c = col + 32 * t + acc_feature(i, lane >> 5);
+                    c = c < h.cols ? c : h.cols - 1;
+                    g *= sx * sc.g[c];
+                    v *= sx * sc.u[c];
+                }
+                a[i] = g * sigmoid<TERMS == 3>(g) * v;
+            }
+            return a;
+        };
+        store_rows<S::FT>(lds, gated, [&](int r, int c, const float *v) { put_hidden<TERMS>(h, 0, row + 32 * u + r, col + c, v); });
+    }
+}
+
+// a from the shares' sums of both projections.
+template <int TERMS, bool E4M3>
+__global__ __launch_bounds__(256) void gated_up_sum_kernel(const float *__restrict__ part, Hidden h, Scales sc, int splits)
+{
+    const int per_row = (h.cols + 7) / 8;
+    const long long n = (long long)h.rows * per_row;
+    const size_t one = (size_t)h.rows * h.ld;
+    for (long long k = (long long)blockIdx.x * 256 + threadIdx.x; k < n; k += (long long)gridDim.x * 256) {
+        const int row = (int)(k / per_row), col = (int)(k - (long long)row * per_row) * 8;
+        float g[8], u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = u[i] = 0.f;
+        const float *q = part + (size_t)row * h.ld + col;
+        for (int s = 0; s < splits; ++s, q += 2 * one) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const f32x4 a = *(const f32x4 *)(q + 4 * i), b = *(const f32x4 *)(q + one + 4 * i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    g[4 * i + e] += a[e];
+                    u[4 * i + e] += b[e];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (E4M3) {
+                const int c = col + i < h.cols ? col + i : h.cols - 1;
+                g[i] *= sc.x[row] * sc.g[c];
+                u[i] *= sc.x[row] * sc.u[c];
+            }
+            g[i] = g[i] * sigmoid<TERMS == 3>(g[i]) * u[i];
+        }
+        put_hidden<TERMS>(h, 0, row, col, g);
+    }
+}
+
+// Up to three products in one launch, into their outputs or, with a split contraction, into fp32 shares.
+struct Products {
+    GemmProblem p[3];
+    Out out[3];
+    float *part[3];      // [split][rows][ld], ld = cols rounded up to 8; none without a split
+    int first[4];        // first block of each
+};
+template <typename S> __global__ __launch_bounds__(256) void gated_product_kernel(Products ps)
+{
+    extern __shared__ __align__(1024) char lds[];
+    int k = 0;
+    while (k < 2 && (int)blockIdx.x >= ps.first[k + 1]) ++k;
+    const GemmProblem &p = ps.p[k];
+    const TilePlace at = tile_of(blockIdx.x - ps.first[k], p.tiles_r, p.tiles_f, p.splits);
+    const int row0 = at.r * S::BR, f0 = at.f * S::BF, wave = threadIdx.x >> 6;
+    f32x16 acc[S::TF][S::TR];
+    clear<S>(acc);
+    int s0, s1;
+    share_of(p, at.split, s0, s1);
+    mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
+    Out o = ps.out[k];
+    if (ps.part[k]) {
+        const int ld = (o.cols + 7) & ~7;
+        o = {ps.part[k] + (size_t)at.split * o.rows * ld, nullptr, o.rows, ld, 1};
+    }
+    const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::TF;
+#pragma unroll
+    for (int u = 0; u < S::TR; ++u)
+        store_rows<S::TF>(lds, [&](int t) { return acc[t][u]; }, [&](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); });
+}
+
+__global__ __launch_bounds__(256) void gated_sum_kernel(Products ps)
+{
+    const int k = blockIdx.y;
+    if (!ps.part[k]) return;
+    const Out o = ps.out[k];
+    const int per_row = (o.cols + 7) / 8, ld = per_row * 8, splits = ps.p[k].splits;
+    const long long n = (long long)o.rows * per_row;
+    const size_t one = (size_t)o.rows * ld;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const int row = (int)(i / per_row), col = (int)(i - (long long)row * per_row) * 8;
+        const float *q = ps.part[k] + (size_t)row * ld + col;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        for (int s = 0; s < splits; ++s, q += one) {
+            a += *(const f32x4 *)q;
+            b += *(const f32x4 *)(q + 4);
+        }
+        const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        put_out(o, row, col, v);
+    }
+}
+
+// Backward of the gate: both projections again, da beside them, and a, dg, du.  S: as gated_up_kernel; D: the same rows and features
+// of dy Wd^T.
+template <typename S, typename D, int TERMS>
+__global__ __launch_bounds__(256) void gated_up_backward_kernel(GemmProblem p, GemmProblem q, Hidden h)
+{
+    static_assert(S::BR == D::BR && S::BF == D::BF && S::FT == D::TF && S::WF == D::WF, "one tile");
+    extern __shared__ __align__(1024) char lds[];
+    const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, 1);
+    const int row0 = at.r * S::BR, f0 = at.f * S::BF, wave = threadIdx.x >> 6;
+    f32x16 acc[S::TF][S::TR], da[D::TF][D::TR];
+    clear<S>(acc);
+    clear<D>(da);
+    mma_steps<S>(acc, p, row0, f0, 0, p.segments * ((p.K + 127) >> 7), lds);
+    mma_steps<D>(da, q, row0, f0, 0, q.segments * ((q.K + 127) >> 7), lds);
+    const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
+#pragma unroll
+    for (int u = 0; u < S::TR; ++u) {
+        const auto put = [&](int which) { return [&, which](int r, int c, const float *v) { put_hidden<TERMS>(h, which, row + 32 * u + r, col + c, v); }; };
+        const auto first = [&](int t) {   // a; acc and da become dg and du
+            f32x16 a;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float g = acc[t][u][i], v = acc[S::FT + t][u][i], d = da[t][u][i], sg = sigmoid<TERMS == 3>(g), s = g * sg;
+                a[i] = s * v;
+                acc[t][u][i] = d * v * (sg + s * (1.f - sg));
+                da[t][u][i] = d * s;
+            }
+            return a;
+        };
+        store_rows<S::FT>(lds, first, put(0));
+        store_rows<S::FT>(lds, [&](int t) { return acc[t][u]; }, put(1));
+        store_rows<S::FT>(lds, [&](int t) { return da[t][u]; }, put(2));
+    }
+}
+
+// ---- weights in e4m3 -----------------------------------------------------------------------------------------------------
+// Column h of W [d][H] becomes row h of the copy, with the scale of its largest value.  A block takes 32 columns: once for the
+// largest values, once more (from the cache) for the values, which turn in the LDS.
+__global__ __launch_bounds__(256) void gated_quantize_kernel(const bf16_t *__restrict__ Wg, const bf16_t *__restrict__ Wu, uint8_t *__restrict__ Qg,
+                                                             uint8_t *__restrict__ Qu, float *__restrict__ sg, float *__restrict__ su, int d, int H)
+{
+    const bf16_t *W = blockIdx.y ? Wu : Wg;
+    uint8_t *Q = blockIdx.y ? Qu : Qg;
+    float *scales = blockIdx.y ? su : sg;
+    __shared__ uint32_t top[8][32];
+    __shared__ float tile[64][33];
+    const int c = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+    uint32_t most = 0;
+    if (col < H)
+        for (int k = y; k < d; k += 8) {
+            const uint32_t a = (uint32_t)(W[(size_t)k * H + col] & 0x7fff) << 16;
+            most = a > most ? a : most;
+        }
+    top[y][c] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = top[i][c] > most ? top[i][c] : most;
+    const float t = __uint_as_float(most);
+    float scale = (t < kE4m3Floor ? kE4m3Floor : t) / kE4m3Max;
+    if (most >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);
+    if (y == 0 && col < H) scales[col] = scale;
+    const float inv = 1.f / scale;
+    for (int k0 = 0; k0 < d; k0 += 64) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int k = k0 + y + 8 * i;
+            tile[y + 8 * i][c] = k < d && col < H ? bf16_to_f32(W[(size_t)k * H + col]) * inv : 0.f;
+        }
+        __syncthreads();
+        // 32 rows of 64 values: 16 threads of four values per row
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = i * 16 + (threadIdx.x >> 4), k = (threadIdx.x & 15) * 4, h = blockIdx.x * 32 + r;
+            if (h < H && k0 + k < d)   // (d is a multiple of 16)
+                *(uint32_t *)(Q + (size_t)h * d + k0 + k) = pack_e4m3(tile[k][r], tile[k + 1][r], tile[k + 2][r], tile[k + 3][r]);
+        }
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+// Tile shapes.  Big: 256 rows x 256 features (gate and up: 128 of each), one block per CU.  Middle: 128 x 128, two blocks per CU.
+// Small: 32 rows x 128 features for the few rows of a decoding step.
+template <int RL, int FL, bool DUAL, bool E4M3> struct Shapes {
+    typedef TileShape<4, 4, 2, 2, RL, FL, DUAL, E4M3, 2> Big;
+    typedef TileShape<2, 2, 2, 2, RL, FL, DUAL, E4M3, 2> Middle;
+    typedef TileShape<1, DUAL ? 2 : 1, 1, 4, RL, FL, DUAL, E4M3, 4> Small;
+};
+template <typename S> constexpr int lds_of(int staged_tiles) { return S::LDS > stage_bytes(staged_tiles) ? S::LDS : stage_bytes(staged_tiles); }
+
+static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+static int steps_of(const GemmProblem &p) { return p.segments * ((p.K + 127) >> 7); }
+
+enum TileSize { kBig, kMiddle, kSmall };
+// The size of the tiles of nr x nf outputs, and into how many shares a contraction of `steps` steps goes so that the chip is full.
+constexpr int kFewRows = 64;   // up to these many rows of x take the small tiles
+struct TileChoice {
+    TileSize size;
+    int splits;
+};
+// The most that goes into one share: fewer steps than these do not pay for the ring's first round trip and the sums' way through memory.
+constexpr int kSmallShare = 2, kMiddleShare = 4;
+static int shares(long long tiles, long long slots, int steps, int least)
+{
+    const int n = (int)std::max<long long>(1, std::min<long long>(slots / std::max(1ll, tiles), steps / least));
+    return ceil_div(steps, ceil_div(steps, n));   // no empty ones
+}
+static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual, bool may_split)
+{
+    const int cus = num_compute_units();
+    const long long f = dual ? 2 : 1;
+    const long long big = (long long)ceil_div(nr, 256) * ceil_div(f * nf, 256), mid = (long long)ceil_div(nr, 128) * ceil_div(f * nf, 128);
+    if (nr <= kFewRows) return {kSmall, may_split ? shares((long long)ceil_div(nr, 32) * ceil_div(nf, 128), cus, steps, kSmallShare) : 1};
+    if (big * 4 >= 3 * cus) return {kBig, 1};
+    return {kMiddle, may_split ? shares(mid, 2 * cus, steps, kMiddleShare) : 1};
+}
+// The three weight gradients share a launch: one size, the same shares.
+static TileChoice choose_weight_tiles(long long d, long long H, int steps)
+{
+    const int cus = num_compute_units();
+    const long long big = 3ll * ceil_div(d, 256) * ceil_div(H, 256), mid = 3ll * ceil_div(d, 128) * ceil_div(H, 128);
+    if (big * 4 >= 3 * cus) return {kBig, 1};
+    return {kMiddle, steps == 0 ? 1 : shares(mid, 2 * cus, steps, kMiddleShare)};
+}
+// Bytes of the shares' sums, at most: shares fill the chip at most once (slots x a tile), and none is shorter than its least.  Neither
+// bound falls as T grows, so a workspace made for the largest batch takes every smaller one.
+static size_t share_bytes(long long slots, long long tile, int steps, int least, size_t rows, size_t ld)
+{
+    return (size_t)std::min<long long>(slots * tile * 4, (long long)(steps / least) * rows * ld * 4);
+}
+template <typename S> static void set_tiles(GemmProblem &p, int splits)
+{
+    p.tiles_r = ceil_div(p.nr, S::BR);
+    p.tiles_f = ceil_div(p.nf, S::BF);
+    p.splits = splits;
+}
+
+static size_t padded(int n) { return ((size_t)n + 63) / 64 * 64; }
+
+// Contractions of a call's products, in steps.
+struct CallSteps {
+    int up, down, dx, dwgu, dwd;
+};
+static CallSteps call_steps(const slicemoe_gated_config &c, int terms, bool e4m3)
+{
+    const int pairs = terms == 3 ? kPairs : 1;
+    const auto steps = [](long long bytes) { return (int)((bytes + 127) / 128); };
+    CallSteps s;
+    s.up = pairs * steps(e4m3 ? c.d : 2ll * c.d);
+    s.down = pairs * steps(2ll * c.H);
+    s.dx = 2 * s.down;
+    s.dwgu = s.dwd = pairs * steps(2ll * c.T);
+    return s;
+}
+
+GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantized)
+{
+    GatedPlan p = {};
+    const size_t T = c.T, d = c.d, H = c.H;
+    p.terms = c.dtype == SLICEMOE_BF16 ? 1 : 3;
+    p.copy_x = c.dtype != SLICEMOE_BF16 || c.d % 8 != 0;
+    p.copy_h = c.dtype != SLICEMOE_BF16 || c.H % 8 != 0;
+    p.ldd = (int)(p.copy_x ? padded(c.d) : d);
+    p.ldh = (int)padded(c.H);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t was = at;
+        at = align_up(at + bytes, 256);
+        return was;
+    };
+    const size_t t2 = 2 * (size_t)p.terms;
+    p.x = take(p.copy_x && !quantized ? t2 * T * p.ldd : 0);
+    p.dy = take(p.copy_x && backward ? t2 * T * p.ldd : 0);
+    p.Wg = take(p.copy_h && !quantized ? t2 * d * p.ldh : 0);
+    p.Wu = take(p.copy_h && !quantized ? t2 * d * p.ldh : 0);
+    p.Wd = take(p.copy_x ? t2 * H * p.ldd : 0);
+    p.a = take(t2 * T * p.ldh);
+    p.dg = take(backward ? t2 * T * p.ldh : 0);
+    p.du = take(backward ? t2 * T * p.ldh : 0);
+    const CallSteps st = call_steps(c, p.terms, quantized);
+    const size_t d8 = (d + 7) / 8 * 8, h8 = (H + 7) / 8 * 8, few = std::min<size_t>(T, kFewRows);
+    const long long cus = num_compute_units();
+    // (tiles reach past the outputs' edges; what is stored ends there, so the outputs bound the bytes of the first kind too)
+    const auto rows_shares = [&](int steps) {
+        return std::max(share_bytes(cus, 32 * 128, steps, kSmallShare, few, d8),
+                        T > few ? share_bytes(2 * cus, 128 * 128, steps, kMiddleShare, T, d8) : 0);
+    };
+    size_t part = 0;
+    if (!backward) part = std::max(share_bytes(cus, 2 * 32 * 128, st.up, kSmallShare, few, 2 * (size_t)p.ldh), rows_shares(st.down));
+    else
+        part = std::max(rows_shares(st.dx), 3 * 256 + 2 * share_bytes(2 * cus, 128 * 128, st.dwgu, kMiddleShare, d, h8) +
+                                                share_bytes(2 * cus, 128 * 128, st.dwd, kMiddleShare, H, d8));
+    p.part_bytes = part;
+    p.part = take(part);
+    p.total = std::max<size_t>(at, 256);
+    return p;
+}
+
+// The arrays that the tiles read: the caller's, or the copies.
+struct Operands {
+    const char *x, *dy, *Wg, *Wu, *Wd;
+    size_t tx, tw, twd, th;       // bytes from one term to the next: rows of x and dy, of Wg and Wu, of Wd, of the hidden arrays
+    long long ldx, ldw, ldwd, ldh;   // bytes per row
+};
+static hipError_t make_operands(const slicemoe_gated_config &c, const GatedPlan &p, const void *x, const void *dy, const slicemoe_gated_weights &w,
+                                char *ws, Operands *o, hipStream_t s)
+{
+    o->ldx = o->ldwd = 2ll * (p.copy_x ? p.ldd : c.d);
+    o->ldw = 2ll * (p.copy_h ? p.ldh : c.H);
+    o->ldh = 2ll * p.ldh;
+    o->tx = (size_t)c.T * o->ldx;
+    o->tw = (size_t)c.d * o->ldw;
+    o->twd = (size_t)c.H * o->ldwd;
+    o->th = (size_t)c.T * o->ldh;
+    CopyJobs jobs = {};
+    jobs.f32 = c.dtype != SLICEMOE_BF16;
+    int n = 0;
+    const auto operand = [&](const void *src, bool copy, size_t at, int rows, int cols, int ld) -> const char * {
+        if (!src || !copy) return (const char *)src;
+        jobs.j[n++] = {src, (bf16_t *)(ws + at), rows, cols, ld};
+        return ws + at;
+    };
+    o->x = operand(x, p.copy_x, p.x, c.T, c.d, p.ldd);
+    o->dy = operand(dy, p.copy_x, p.dy, c.T, c.d, p.ldd);
+    o->Wg = operand(w.Wg, p.copy_h, p.Wg, c.d, c.H, p.ldh);
+    o->Wu = operand(w.Wu, p.copy_h, p.Wu, c.d, c.H, p.ldh);
+    o->Wd = operand(w.Wd, p.copy_x, p.Wd, c.H, c.d, p.ldd);
+    if (n == 0) return hipSuccess;
+    long long most = 0;
+    for (int i = 0; i < n; ++i) most = std::max(most, (long long)jobs.j[i].rows * (jobs.j[i].ld / 8));
+    const int blocks = (int)std::min<long long>((most + 255) / 256, 8ll * num_compute_units());
+    gated_copy_kernel<<<dim3(blocks, n), 256, 0, s>>>(jobs);
+    return hipGetLastError();
+}
+
+// Fills the segments of r f^T: every pair of terms that counts.
+static void add_segments(GemmProblem &p, int terms, const char *r, size_t tr, const char *f, size_t tf, const char *f2 = nullptr)
+{
+    const int pairs = terms == 3 ? kPairs : 1;
+    for (int i = 0; i < pairs; ++i) {
+        const int k = p.segments++;
+        p.r[k] = r + kPairR[i] * tr;
+        p.f[k] = f + kPairF[i] * tf;
+        p.f2[k] = f2 ? f2 + kPairF[i] * tf : nullptr;
+    }
+}
+static GemmProblem problem(int nr, int nf, long long K, long long ldr, long long ldf)
+{
+    GemmProblem p = {};
+    p.nr = nr;
+    p.nf = nf;
+    p.K = (int)K;
+    p.ldr = ldr;
+    p.ldf = ldf;
+    return p;
+}
+
+template <typename K> static hipError_t ready(K kernel, int lds) { return grant_dynamic_lds((const void *)kernel, lds); }
+
+template <typename S, int TERMS> static hipError_t run_up(GemmProblem p, const Hidden &h, const Scales &sc, int splits, float *part, hipStream_t s)
+{
+    set_tiles<S>(p, splits);
+    constexpr int lds = lds_of<S>(S::FT);
+    const auto kernel = gated_up_kernel<S, TERMS>;
+    hipError_t e = ready(kernel, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<p.tiles_r * p.tiles_f * splits, 256, lds, s>>>(p, h, sc, splits > 1 ? part : nullptr);
+    if ((e = hipGetLastError()) != hipSuccess || splits == 1) return e;
+    const long long n = (long long)h.rows * ((h.cols + 7) / 8);
+    gated_up_sum_kernel<TERMS, S::E4M3><<<(int)std::min<long long>((n + 255) / 256, 8ll * num_compute_units()), 256, 0, s>>>(part, h, sc, splits);
+    return hipGetLastError();
+}
+template <int FL, bool E4M3, int TERMS>
+static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales &sc, float *part, hipStream_t s)
+{
+    typedef Shapes<kKContiguous, FL, true, E4M3> Sh;
+    const TileChoice t = choose_tiles(p.nr, p.nf, steps_of(p), true, p.nr <= kFewRows);
+    switch (t.size) {
+        case kBig: return run_up<typename Sh::Big, TERMS>(p, h, sc, t.splits, part, s);
+        case kMiddle: return run_up<typename Sh::Middle, TERMS>(p, h, sc, t.splits, part, s);
+        default: return run_up<typename Sh::Small, TERMS>(p, h, sc, t.splits, part, s);
+    }
+}
+
+template <typename S> static hipError_t run_products(Products &ps, int n, hipStream_t s)
+{
+    ps.first[0] = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (i < n) set_tiles<S>(ps.p[i], ps.p[i].splits);
+        ps.first[i + 1] = ps.first[i] + (i < n ? ps.p[i].tiles_r * ps.p[i].tiles_f * ps.p[i].splits : 0);
+    }
+    for (int i = n; i < 3; ++i) ps.first[i] = ps.first[n];
+    constexpr int lds = lds_of<S>(S::TF);
+    const auto kernel = gated_product_kernel<S>;
+    const hipError_t e = ready(kernel, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<ps.first[n], 256, lds, s>>>(ps);
+    return hipGetLastError();
+}
+// n products of one tile size; part: room for the shares.
+template <int RL, int FL> static hipError_t launch_products(Products &ps, int n, TileChoice t, char *part, hipStream_t s)
+{
+    typedef Shapes<RL, FL, false, false> Sh;
+    bool split = false;
+    long long most = 0;
+    size_t at = 0;
+    for (int i = 0; i < n; ++i) {
+        ps.p[i].splits = t.splits;
+        ps.part[i] = nullptr;
+        if (t.splits == 1) continue;
+        split = true;
+        const long long pieces = (long long)ps.out[i].rows * ((ps.out[i].cols + 7) / 8);
+        ps.part[i] = (float *)(part + at);
+        at = align_up(at + (size_t)t.splits * pieces * 32, 256);
+        most = std::max(most, pieces);
+    }
+    for (int i = n; i < 3; ++i) ps.part[i] = nullptr;
+    hipError_t e;
+    switch (t.size) {
+        case kBig: e = run_products<typename Sh::Big>(ps, n, s); break;
+        case kMiddle: e = run_products<typename Sh::Middle>(ps, n, s); break;
+        default: e = run_products<typename Sh::Small>(ps, n, s); break;
+    }
+    if (e != hipSuccess || !split) return e;
+    gated_sum_kernel<<<dim3((int)std::min<long long>((most + 255) / 256, 8ll * num_compute_units()), n), 256, 0, s>>>(ps);
+    return hipGetLastError();
+}
+
+static hipError_t launch_down(const slicemoe_gated_config &c, const GatedPlan &plan, const char *Wd, size_t twd, long long ldwd, const void *addend,
+                              void *y, char *ws, hipStream_t s)
+{
+    Products ps = {};
+    ps.p[0] = problem(c.T, c.d, 2ll * c.H, 2ll * plan.ldh, ldwd);
+    add_segments(ps.p[0], plan.terms, ws + plan.a, (size_t)c.T * 2 * plan.ldh, Wd, twd);
+    ps.out[0] = {y, addend, c.T, c.d, c.dtype != SLICEMOE_BF16};
+    return launch_products<kKContiguous, kKMajor>(ps, 1, choose_tiles(c.T, c.d, steps_of(ps.p[0]), false, true), ws + plan.part, s);
+}
+
+static Hidden hidden_of(const slicemoe_gated_config &c, const GatedPlan &p, char *ws)
+{
+    return {{(bf16_t *)(ws + p.a), (bf16_t *)(ws + p.dg), (bf16_t *)(ws + p.du)}, c.T, c.H, p.ldh};
+}
+
+hipError_t launch_gated_ffn(const slicemoe_gated_config &c, const GatedPlan &plan, const void *x, const slicemoe_gated_weights &w,
+                            const void *addend, void *y, char *ws, hipStream_t s)
+{
+    if (c.T == 0) return hipSuccess;
+    Operands o;
+    hipError_t e = make_operands(c, plan, x, nullptr, w, ws, &o, s);
+    if (e != hipSuccess) return e;
+    GemmProblem p = problem(c.T, c.H, 2ll * c.d, o.ldx, o.ldw);
+    add_segments(p, plan.terms, o.x, o.tx, o.Wg, o.tw, o.Wu);
+    const Hidden h = hidden_of(c, plan, ws);
+    float *part = (float *)(ws + plan.part);
+    e = plan.terms == 1 ? launch_up<kKMajor, false, 1>(p, h, Scales(), part, s) : launch_up<kKMajor, false, 3>(p, h, Scales(), part, s);
+    if (e != hipSuccess) return e;
+    return launch_down(c, plan, o.Wd, o.twd, o.ldwd, addend, y, ws, s);
+}
+
+hipError_t launch_gated_ffn_quantized(const slicemoe_gated_config &c, const GatedPlan &plan, const uint8_t *x, const float *x_scale,
+                                      const slicemoe_gated_weights_quantized &w, const void *addend, void *y, char *ws, hipStream_t s)
+{
+    if (c.T == 0) return hipSuccess;
+    const slicemoe_gated_weights logical = {nullptr, nullptr, w.Wd};
+    Operands o;
+    hipError_t e = make_operands(c, plan, nullptr, nullptr, logical, ws, &o, s);
+    if (e != hipSuccess) return e;
+    GemmProblem p = problem(c.T, c.H, c.d, c.d, c.d);
+    add_segments(p, 1, (const char *)x, 0, (const char *)w.Wg, 0, (const char *)w.Wu);
+    e = launch_up<kKContiguous, true, 1>(p, hidden_of(c, plan, ws), Scales{x_scale, w.Wg_scale, w.Wu_scale}, (float *)(ws + plan.part), s);
+    if (e != hipSuccess) return e;
+    return launch_down(c, plan, o.Wd, o.twd, o.ldwd, addend, y, ws, s);
+}
+
+template <typename S, typename D, int TERMS> static hipError_t run_up_backward(GemmProblem p, GemmProblem q, const Hidden &h, hipStream_t s)
+{
+    set_tiles<S>(p, 1);
+    set_tiles<D>(q, 1);
+    constexpr int a = lds_of<S>(S::FT), b = lds_of<D>(S::FT), lds = a > b ? a : b;
+    const auto kernel = gated_up_backward_kernel<S, D, TERMS>;
+    const hipError_t e = ready(kernel, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<p.tiles_r * p.tiles_f, 256, lds, s>>>(p, q, h);
+    return hipGetLastError();
+}
+template <int TERMS> static hipError_t launch_up_backward(const GemmProblem &p, const GemmProblem &q, const Hidden &h, hipStream_t s)
+{
+    typedef Shapes<kKContiguous, kKMajor, true, false> Sh;
+    if (choose_tiles(p.nr, p.nf, steps_of(p), true, false).size == kBig)
+        return run_up_backward<typename Sh::Big, TileShape<4, 2, 2, 2, kKContiguous, kKContiguous, false, false, 2>, TERMS>(p, q, h, s);
+    return run_up_backward<typename Sh::Middle, TileShape<2, 1, 2, 2, kKContiguous, kKContiguous, false, false, 2>, TERMS>(p, q, h, s);
+}
+
+hipError_t launch_gated_ffn_backward(const slicemoe_gated_config &c, const GatedPlan &plan, const void *x, const slicemoe_gated_weights &w,
+                                     const void *dy, const void *addend, void *dx, const slicemoe_gated_weight_grads &g, char *ws,
+                                     hipStream_t s)
+{
+    Operands o;
+    hipError_t e = make_operands(c, plan, x, dy, w, ws, &o, s);
+    if (e != hipSuccess) return e;
+    const int terms = plan.terms, f32 = c.dtype != SLICEMOE_BF16;
+    const char *a = ws + plan.a, *dg = ws + plan.dg, *du = ws + plan.du;
+    char *part = ws + plan.part;
+    if (c.T > 0) {
+        GemmProblem p = problem(c.T, c.H, 2ll * c.d, o.ldx, o.ldw), q = problem(c.T, c.H, 2ll * c.d, o.ldx, o.ldwd);
+        add_segments(p, terms, o.x, o.tx, o.Wg, o.tw, o.Wu);
+        add_segments(q, terms, o.dy, o.tx, o.Wd, o.twd);
+        const Hidden h = hidden_of(c, plan, ws);
+        e = terms == 1 ? launch_up_backward<1>(p, q, h, s) : launch_up_backward<3>(p, q, h, s);
+        if (e != hipSuccess) return e;
+    }
+    // The weight gradients, before dx: dx may then take the place of dy.  (T = 0: contractions of no steps, zeros.)
+    {
+        Products ps = {};
+        ps.p[0] = problem(c.d, c.H, 2ll * c.T, o.ldx, o.ldh);
+        ps.p[1] = ps.p[0];
+        ps.p[2] = problem(c.H, c.d, 2ll * c.T, o.ldh, o.ldx);
+        add_segments(ps.p[0], terms, o.x, o.tx, dg, o.th);
+        add_segments(ps.p[1], terms, o.x, o.tx, du, o.th);
+        add_segments(ps.p[2], terms, a, o.th, o.dy, o.tx);
+        ps.out[0] = {g.Wg, nullptr, c.d, c.H, f32};
+        ps.out[1] = {g.Wu, nullptr, c.d, c.H, f32};
+        ps.out[2] = {g.Wd, nullptr, c.H, c.d, f32};
+        const TileChoice t = choose_weight_tiles(c.d, c.H, steps_of(ps.p[0]));
+        e = launch_products<kKMajor, kKMajor>(ps, 3, t, part, s);
+        if (e != hipSuccess || c.T == 0) return e;
+    }
+    Products ps = {};
+    ps.p[0] = problem(c.T, c.d, 2ll * c.H, o.ldh, o.ldw);
+    add_segments(ps.p[0], terms, dg, o.th, o.Wg, o.tw);
+    add_segments(ps.p[0], terms, du, o.th, o.Wu, o.tw);
+    ps.out[0] = {dx, addend, c.T, c.d, f32};
+    return launch_products<kKContiguous, kKContiguous>(ps, 1, choose_tiles(c.T, c.d, steps_of(ps.p[0]), false, true), part, s);
+}
+
+hipError_t launch_gated_quantize_weights(const slicemoe_gated_config &c, const slicemoe_gated_weights &w, uint8_t *Wg, float *Wg_scale,
+                                         uint8_t *Wu, float *Wu_scale, hipStream_t s)
+{
+    gated_quantize_kernel<<<dim3((c.H + 31) / 32, 2), 256, 0, s>>>((const bf16_t *)w.Wg, (const bf16_t *)w.Wu, Wg, Wu, Wg_scale, Wu_scale, c.d, c.H);
+    return hipGetLastError();
+}
+
+}  // namespace slicemoe

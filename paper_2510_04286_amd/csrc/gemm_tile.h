@@ -1,0 +1,274 @@
+// Matrix-product tiles for the gated feed-forward network (gated_ffn.hip): C[rows, features] = R F^T over a list of segments, with
+// fp32 accumulation, operands in memory in either order.
+//
+// One block of four wavefronts owns a tile.  As in the layer's kernels the product is computed transposed: the features' operand F is
+// the matrix instruction's first, the rows' operand R its second, so a lane's accumulators are features of one row.
+//
+// A step of the contraction is 128 bytes of a row: 64 bf16 values or 128 e4m3 ones.  Its images in the LDS come straight from memory
+// (global_load_lds, 16 bytes per lane): 1 KB per instruction, linear in the lane, so the arrangement that keeps the reads free of
+// bank conflicts is made by which 16 bytes a lane asks for.
+//   K-contiguous operands ([row][k] in memory): 128 bytes per row, piece c of row i at place c ^ (i & 7); a fragment is one
+//     ds_read_b128 (lane = row, eight consecutive k).
+//   K-major operands ([k][row] in memory): rows of k, blocks of 64 bytes (32 rows) XORed with k & 3; a fragment is two
+//     ds_read_b64_tr_b16, which hand every lane the four k of its row.
+//
+// The ring has STAGES images.  Inside a step the fragments of the next quarter are read while the matrix instructions of the present
+// one run; in front of the last quarter stands the step's one barrier: behind it the next step's image has landed for every
+// wavefront and the present one, whose last fragments are in registers, is free for the loads STAGES steps ahead.
+//
+// Edges: rows and columns past an operand's end are read at its last one (their products are never stored); a step that reaches past
+// the end of K takes those 16-byte pieces from a page of zeros, in both operands.
+#pragma once
+#include "lds_rows.h"
+#include "wavefront.h"
+
+namespace slicemoe {
+
+constexpr int kMaxSegments = 12;
+// One product of a launch.  Leading dimensions and K in bytes; K is what is read of a K-contiguous row, a whole number of 16-byte
+// pieces, and the number of k times 2 for K-major operands.
+struct GemmProblem {
+    const char *r[kMaxSegments], *f[kMaxSegments], *f2[kMaxSegments];   // f2: the second image of the features (gate and up)
+    long long ldr, ldf;
+    int nr, nf;          // rows, features (of one image)
+    int K;               // bytes
+    int segments;
+    int tiles_r, tiles_f;
+    int splits;          // shares of the contraction, each a range of steps
+};
+
+__device__ const uint4 g_zero_piece[1] = {};
+
+enum { kKContiguous = 0, kKMajor = 1 };
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// 1 KB from memory to the LDS: lane l's 16 bytes go to `at` + 16 l.  (Written out, because the compiler would wait for all of
+// them in front of every LDS read; the waits are in the pipeline below.)
+__device__ __forceinline__ void load_lds_1k(uint32_t at, const char *base, uint32_t offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_lds_1k(uint32_t at, const char *address)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(address) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The image of one operand: N rows of the tile (a multiple of 32).  Instruction i of wavefront w fills kilobyte 4 i + w: every
+// wavefront's lanes then sit on the same k & 3 in all of its instructions, and one offset per lane does for a K-major operand.
+template <int LAYOUT, int N> struct TileImage {
+    static constexpr int BYTES = N * 128, PER_WAVE = N / 32;
+    static constexpr int K_PER_PIECE = 512 / N;   // rows of k per instruction (K-major)
+    static constexpr int OFFSETS = LAYOUT == kKContiguous ? PER_WAVE : 1;
+    static __device__ __forceinline__ int block_swizzle(int k) { return N >= 128 ? k & 3 : N == 64 ? k >> 1 & 1 : 0; }
+    static __device__ __forceinline__ int piece_of(int lane) { return (lane & 7) ^ (lane >> 3); }   // K-contiguous: which 16 bytes of its row
+
+    // This lane's offsets from the tile's corner (the operand's row `first`, step 0 of K).
+    static __device__ __forceinline__ void offsets(uint32_t (&o)[OFFSETS], int wave, int lane, int first, int rows, uint32_t ld)
+    {
+        if constexpr (LAYOUT == kKContiguous) {
+            const int last = rows - 1 - first;
+#pragma unroll
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const int row = 8 * (4 * i + wave) + (lane >> 3);
+                o[i] = (uint32_t)(row < last ? row : last) * ld + 16u * piece_of(lane);
+            }
+        } else {
+            const int k = lane / (N / 8), last = (rows - 1 - first) >> 3;
+            const int c = (lane % (N / 8)) ^ block_swizzle(wave * K_PER_PIECE + k) << 2;
+            o[0] = (uint32_t)(wave * K_PER_PIECE + k) * ld + 16u * (c < last ? c : last);
+        }
+    }
+    static __device__ __forceinline__ const char *corner(const char *p, int first, long long ld)
+    {
+        return LAYOUT == kKContiguous ? p + first * ld : p + 2ll * first;
+    }
+    static __device__ __forceinline__ long long step_bytes(long long ld) { return LAYOUT == kKContiguous ? 128 : 64 * ld; }
+
+    // Requests the image of one step.  left: bytes of K from this step on (below 128 in a step that reaches past the end).
+    static __device__ __forceinline__ void request(uint32_t lds, const char *base, const uint32_t (&o)[OFFSETS], int wave, int lane, int left, long long ld)
+    {
+        if (left >= 128) {
+#pragma unroll
+            for (int i = 0; i < PER_WAVE; ++i)
+                load_lds_1k(lds + 1024 * (4 * i + wave), LAYOUT == kKContiguous ? base : base + i * (4 * K_PER_PIECE * ld), o[LAYOUT == kKContiguous ? i : 0]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER_WAVE; ++i) {
+                const bool there = LAYOUT == kKContiguous ? 16 * piece_of(lane) < left : 2 * ((4 * i + wave) * K_PER_PIECE + lane / (N / 8)) < left;
+                const char *a = base + (LAYOUT == kKContiguous ? 0 : i * (4 * K_PER_PIECE * ld)) + o[LAYOUT == kKContiguous ? i : 0];
+                load_lds_1k(lds + 1024 * (4 * i + wave), there ? a : (const char *)g_zero_piece);
+            }
+        }
+    }
+};
+
+// Reads fragments of 32 rows (tile `t` of a wavefront whose first row of 32 is block `wb` of the image).
+template <int LAYOUT, int N, bool E4M3> struct FragmentReader {
+    typedef typename std::conditional<E4M3, i32x8, bf16x8>::type frag;
+    uint32_t base[4];
+    __device__ __forceinline__ void init(int wb, int lane)
+    {
+        const int i = lane & 31, g = lane >> 5;
+        if constexpr (LAYOUT == kKContiguous) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {   // E4M3: 32 bytes of a row, pieces 4 ks + 2 g and the next; else pieces 2 ks + g
+                const int c = E4M3 ? 4 * (q >> 1) + 2 * g + (q & 1) : 2 * q + g;
+                base[q] = (wb * 32 + i) * 128 + ((c ^ (i & 7)) << 4);
+            }
+        } else {
+            const int q = lane >> 2 & 3;   // which of four k this lane fetches
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                base[t] = (8 * g + q) * (2 * N) + (((wb + t) ^ TileImage<LAYOUT, N>::block_swizzle(q)) & (N / 32 - 1)) * 64 + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
+        }
+    }
+    __device__ __forceinline__ frag read(const char *image, int t, int ks) const
+    {
+        if constexpr (LAYOUT == kKContiguous) {
+            if constexpr (E4M3) {
+                union {
+                    uint4 h[2];
+                    i32x8 v;
+                } r;
+                r.h[0] = *(const uint4 *)(image + base[2 * ks] + t * 4096);
+                r.h[1] = *(const uint4 *)(image + base[2 * ks + 1] + t * 4096);
+                return r.v;
+            } else
+                return *(const bf16x8 *)(image + base[ks] + t * 4096);
+        } else {
+            const char *p = image + base[t] + ks * 16 * (2 * N);
+            return read_transposed(as_lds(p), as_lds(p + 4 * (2 * N)));
+        }
+    }
+};
+
+// TR x TF fragments of 32 rows and features per wavefront, WR x WF = 4 wavefronts.  DUAL: the first half of a wavefront's feature
+// tiles comes from f, the second from f2 (the same features of two matrices).
+template <int TR_, int TF_, int WR_, int WF_, int RL_, int FL_, bool DUAL_, bool E4M3_, int STAGES_> struct TileShape {
+    static constexpr int TR = TR_, TF = TF_, WR = WR_, WF = WF_, RL = RL_, FL = FL_, STAGES = STAGES_;
+    static constexpr bool DUAL = DUAL_, E4M3 = E4M3_;
+    static_assert(WR * WF == 4 && TR <= 4 && TF <= 4, "four wavefronts, at most 128 x 128 each");
+    static constexpr int IMAGES = DUAL ? 2 : 1, FT = TF / IMAGES;   // feature tiles per image and wavefront
+    static constexpr int BR = 32 * TR * WR, BF = 32 * FT * WF;      // rows, features (of one image) per block
+    typedef TileImage<RL, BR> RI;
+    typedef TileImage<FL, BF> FI;
+    static constexpr int STAGE_BYTES = RI::BYTES + IMAGES * FI::BYTES;
+    static constexpr int LOADS = RI::PER_WAVE + IMAGES * FI::PER_WAVE;   // instructions per wavefront and step
+    static constexpr int LDS = STAGES * STAGE_BYTES;
+    static constexpr int KS = E4M3 ? 2 : 4;                              // matrix-instruction steps per step
+};
+
+// acc[feature tile][row tile] += the steps [s0, s1) of the problem's contraction (counted through its segments).
+template <typename S>
+__device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const GemmProblem &p, int row0, int f0, int s0, int s1, char *lds)
+{
+    typedef typename S::RI RI;
+    typedef typename S::FI FI;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave / S::WF, wf = wave % S::WF;
+    const int n = s1 - s0;
+    if (n <= 0) return;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)as_lds(lds);
+    uint32_t ro[RI::OFFSETS], fo[FI::OFFSETS];
+    RI::offsets(ro, wave, lane, row0, p.nr, (uint32_t)p.ldr);
+    FI::offsets(fo, wave, lane, f0, p.nf, (uint32_t)p.ldf);
+    FragmentReader<S::RL, S::BR, S::E4M3> rr;
+    FragmentReader<S::FL, S::BF, S::E4M3> fr;
+    rr.init(wr * S::TR, lane);
+    fr.init(wf * S::FT, lane);
+
+    // where the next request comes from
+    const int per_segment = (p.K + 127) >> 7;
+    int seg = s0 / per_segment, at = s0 - seg * per_segment, slot = 0;
+    const char *rp, *fp, *fp2 = nullptr;
+    const auto enter = [&]() {
+        rp = RI::corner(p.r[seg], row0, p.ldr) + at * RI::step_bytes(p.ldr);
+        fp = FI::corner(p.f[seg], f0, p.ldf) + at * FI::step_bytes(p.ldf);
+        if constexpr (S::DUAL) fp2 = FI::corner(p.f2[seg], f0, p.ldf) + at * FI::step_bytes(p.ldf);
+    };
+    enter();
+    const auto request = [&]() {
+        const uint32_t to = lds0 + slot * S::STAGE_BYTES;
+        const int left = p.K - 128 * at;
+        RI::request(to, rp, ro, wave, lane, left, p.ldr);
+        FI::request(to + RI::BYTES, fp, fo, wave, lane, left, p.ldf);
+        if constexpr (S::DUAL) FI::request(to + RI::BYTES + FI::BYTES, fp2, fo, wave, lane, left, p.ldf);
+        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+        if (++at == per_segment) {
+            at = 0;
+            if (++seg < p.segments) enter();
+        } else {
+            rp += RI::step_bytes(p.ldr);
+            fp += FI::step_bytes(p.ldf);
+            if constexpr (S::DUAL) fp2 += FI::step_bytes(p.ldf);
+        }
+    };
+    typedef typename FragmentReader<S::RL, S::BR, S::E4M3>::frag frag;
+    frag rf[2][S::TR], ff[2][S::TF];
+    const auto read = [&](int set, const char *image, int ks) {
+#pragma unroll
+        for (int t = 0; t < S::TR; ++t) rf[set][t] = rr.read(image, t, ks);
+#pragma unroll
+        for (int t = 0; t < S::TF; ++t) ff[set][t] = fr.read(image + RI::BYTES + (t / S::FT) * FI::BYTES, t % S::FT, ks);
+    };
+    const auto multiply = [&](int set) {
+#pragma unroll
+        for (int t = 0; t < S::TF; ++t)
+#pragma unroll
+            for (int u = 0; u < S::TR; ++u) {
+                if constexpr (S::E4M3)   // (scales of 2^0)
+                    acc[t][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ff[set][t], rf[set][u], acc[t][u], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                else
+                    acc[t][u] = mfma_bf16(ff[set][t], rf[set][u], acc[t][u]);
+            }
+    };
+
+#pragma unroll
+    for (int i = 0; i < S::STAGES; ++i)
+        if (i < n) request();
+    if (n >= S::STAGES) wait_loads_and_barrier<S::LOADS *(S::STAGES - 1)>();
+    else wait_loads_and_barrier<0>();
+    read(0, lds, 0);
+    int cur = 0;
+    for (int s = 0; s < n; ++s) {
+        const char *image = lds + cur * S::STAGE_BYTES;
+        cur = cur + 1 == S::STAGES ? 0 : cur + 1;
+#pragma unroll
+        for (int ks = 0; ks < S::KS; ++ks) {
+            if (ks + 1 < S::KS) read((ks + 1) & 1, image, ks + 1);
+            else {
+                // (every request so far but the newest STAGES - 2 steps'; near the end all of them)
+                if (s + S::STAGES - 1 < n) wait_loads_and_barrier<S::LOADS *(S::STAGES - 2)>();
+                else wait_loads_and_barrier<0>();
+                if (s + S::STAGES < n) request();
+                if (s + 1 < n) read(0, lds + cur * S::STAGE_BYTES, 0);
+            }
+            multiply(ks & 1);
+        }
+    }
+}
+
+// Which tile and share of the contraction a block has: blocks of one XCD (blockIdx % 8) take consecutive tiles, in groups of eight row
+// tiles, so that the operands they share stay in its L2.
+struct TilePlace {
+    int r, f, split;
+};
+__device__ __forceinline__ TilePlace tile_of(int block, int tiles_r, int tiles_f, int splits)
+{
+    const int total = tiles_r * tiles_f * splits, q = total >> 3, rem = total & 7, x = block & 7;
+    int i = x * q + (x < rem ? x : rem) + (block >> 3);
+    TilePlace t;
+    t.split = i / (tiles_r * tiles_f);
+    i -= t.split * tiles_r * tiles_f;
+    const int group = 8 * tiles_f, first = i / group * 8, rows = tiles_r - first < 8 ? tiles_r - first : 8, in = i % group;
+    t.f = in / rows;
+    t.r = first + in % rows;
+    return t;
+}
+
+}  // namespace slicemoe

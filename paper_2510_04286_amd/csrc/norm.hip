@@ -1,0 +1,363 @@
+// Root-mean-square norm of the residual stream in front of the layer, with the residual's addition, and its backward pass.
+//
+//   forward    s = x + residual,  r = 1 / sqrt(mean(s^2) + eps),  y = s r w
+//   backward   n = s r,  m = dy w:   d_s = d_sum + r (m - n mean(m n)),   d_w = sum over the rows of dy n
+//
+// Both are one pass over memory: a row stays in the registers of the wavefronts that own it (one, four or sixteen of them) between
+// its sums and its outputs, all of its pieces are requested before any is used, and the statistics are fp32.  The norm is taken of
+// the fp32 sum, not of the stored one: y then carries one rounding.  The backward pass starts from the stored sum and computes r
+// again, so the forward keeps nothing for it.  d_w: persistent blocks, a column sum per lane in registers over the block's rows, one
+// row of partial sums per block, added in block order by a second kernel (bit-reproducible).
+//
+// The e4m3 row: scale = max|y| / 448 (448: the largest e4m3 value), values y / scale rounded to nearest even.  A largest value below
+// 1e-30 counts as 1e-30, so a row of zeros has a scale and no division by zero; a row that holds a NaN or an infinity has a NaN scale.
+//
+// HBM-bound.  Rows that are not whole 16-byte pieces (d not a multiple of 8 for bf16, 4 for fp32) start at any element:
+// their pieces are 16-byte accesses at element alignment, the last piece element by element.
+#include "common.h"
+#include "norm.h"
+#include "wavefront.h"
+
+namespace slicemoe {
+
+template <typename T> struct RowPiece;   // 16 bytes of a row
+template <> struct RowPiece<bf16_t> {
+    static constexpr int V = 8;
+    static __device__ __forceinline__ float get(const u32x4 &p, int i) { return __uint_as_float(i & 1 ? p[i >> 1] & 0xffff0000u : p[i >> 1] << 16); }
+    static __device__ __forceinline__ u32x4 make(const float *v)
+    {
+        u32x4 p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = (uint32_t)f32_to_bf16(v[2 * i]) | (uint32_t)f32_to_bf16(v[2 * i + 1]) << 16;
+        return p;
+    }
+};
+template <> struct RowPiece<float> {
+    static constexpr int V = 4;
+    static __device__ __forceinline__ float get(const u32x4 &p, int i) { return __uint_as_float(p[i]); }
+    static __device__ __forceinline__ u32x4 make(const float *v)
+    {
+        return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+};
+
+typedef u32x4 __attribute__((aligned(2))) loose;   // a row may start at any element
+// Piece `at` (an element index, a multiple of V) of a row of d elements, zeros past its end.  ALIGNED: rows are whole aligned pieces.
+template <typename T, bool ALIGNED> __device__ __forceinline__ u32x4 load_piece(const T *row, int at, int d)
+{
+    constexpr int V = RowPiece<T>::V;
+    if constexpr (ALIGNED) {   // (no branch: the pieces of a row are requested together)
+        u32x4 p = *(const u32x4 *)(row + (at < d ? at : 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = at < d ? p[i] : 0;
+        return p;
+    }
+    if (at >= d) return u32x4{0, 0, 0, 0};
+    if (at + V <= d) return *(const loose *)(row + at);
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = at + i < d ? Storage<T>::load(row + at + i) : 0.f;
+    return RowPiece<T>::make(v);
+}
+template <typename T, bool ALIGNED> __device__ __forceinline__ void store_piece(T *row, int at, int d, const float *v)
+{
+    constexpr int V = RowPiece<T>::V;
+    if constexpr (ALIGNED) *(u32x4 *)(row + at) = RowPiece<T>::make(v);
+    else if (at + V <= d) *(loose *)(row + at) = RowPiece<T>::make(v);
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (at + i < d) Storage<T>::store(row + at + i, v[i]);
+}
+
+// Sum (largest, as unsigned: absolute values in their bit order, a NaN above all) over the W wavefronts that own a row.
+template <int W> __device__ __forceinline__ float row_sum(float v, float *lds)
+{
+    v = wavefront_sum_f32(v);
+    if constexpr (W == 1) return v;
+    __syncthreads();   // the values of the row's last sum have been read
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) s += lds[i];
+    return s;
+}
+template <int W> __device__ __forceinline__ uint32_t row_max(uint32_t v, float *lds)
+{
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)v, m);
+        v = o > v ? o : v;
+    }
+    if constexpr (W == 1) return v;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = __uint_as_float(v);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const uint32_t o = __float_as_uint(lds[i]);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+// W wavefronts per row (W = 1: four rows per block of 256 threads), NP pieces per lane.
+template <typename T, bool ALIGNED, int W, int NP, bool QUANT>
+__global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_kernel(const T *__restrict__ x, const T *__restrict__ residual,
+                                                                         const T *__restrict__ w, T *__restrict__ sum, T *__restrict__ y,
+                                                                         uint8_t *__restrict__ yq, float *__restrict__ yscale, int rows,
+                                                                         int d, float eps)
+{
+    constexpr int V = RowPiece<T>::V, LANES = 64 * W;
+    __shared__ float lds[W];
+    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const long long row = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (row >= rows) return;   // (a whole wavefront; with W > 1 every block has its row)
+    const size_t at0 = (size_t)row * d;
+    u32x4 px[NP], pr[NP], pw[NP];
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+        const int at = (lane + c * LANES) * V;
+        px[c] = load_piece<T, ALIGNED>(x + at0, at, d);
+        pw[c] = load_piece<T, ALIGNED>(w, at, d);
+    }
+    if (residual)
+#pragma unroll
+        for (int c = 0; c < NP; ++c) pr[c] = load_piece<T, ALIGNED>(residual + at0, (lane + c * LANES) * V, d);
+    float s[NP][V], ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < NP; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s[c][i] = RowPiece<T>::get(px[c], i);
+            if (residual) s[c][i] += RowPiece<T>::get(pr[c], i);   // (without one, -0 stays -0)
+            ss += s[c][i] * s[c][i];
+        }
+    ss = row_sum<W>(ss, lds);
+    const float r = 1.f / sqrtf(ss / d + eps);
+    uint32_t most = 0;
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+        const int at = (lane + c * LANES) * V;
+        if (at < d && sum) store_piece<T, ALIGNED>(sum + at0, at, d, s[c]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s[c][i] = s[c][i] * r * RowPiece<T>::get(pw[c], i);
+            const uint32_t a = __float_as_uint(s[c][i]) & 0x7fffffffu;
+            if (QUANT && at + i < d) most = a > most ? a : most;
+        }
+        if (at < d && y) store_piece<T, ALIGNED>(y + at0, at, d, s[c]);
+    }
+    if constexpr (QUANT) {
+        most = row_max<W>(most, lds);
+        const float top = __uint_as_float(most);
+        float scale = (top < kE4m3Floor ? kE4m3Floor : top) / kE4m3Max;
+        if (most >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // an infinity or a NaN in the row
+        const float inv = 1.f / scale;
+        if (lane == 0) yscale[row] = scale;
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            const int at = (lane + c * LANES) * V;
+            if (at >= d) continue;
+            uint32_t q[V / 4];
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) q[i] = pack_e4m3(s[c][4 * i] * inv, s[c][4 * i + 1] * inv, s[c][4 * i + 2] * inv, s[c][4 * i + 3] * inv);
+            uint8_t *o = yq + at0 + at;
+            if (ALIGNED) {
+                if constexpr (V == 8) *(uint2 *)o = make_uint2(q[0], q[1]);
+                else *(uint32_t *)o = q[0];
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (at + i < d) o[i] = (uint8_t)(q[i >> 2] >> 8 * (i & 3));
+            }
+        }
+    }
+}
+
+// Block b takes the rows b, b + gridDim.x, .. (W = 1: its four wavefronts the row groups), so that a block's share differs by
+// at most one row (group).  part[b][d]: its column sums of dy n.
+template <typename T, bool ALIGNED, int W, int NP>
+__global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_backward_kernel(
+    const T *__restrict__ sum, const T *__restrict__ w, const T *__restrict__ dy, const T *__restrict__ dsum, T *__restrict__ dx,
+    float *__restrict__ part, int rows, int d, float eps)
+{
+    constexpr int V = RowPiece<T>::V, LANES = 64 * W, ROWS = W == 1 ? 4 : 1;
+    __shared__ float lds[2 * W];
+    __shared__ float cols[W == 1 ? 3 : 1][W == 1 ? 64 * V : 1];
+    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, wave = threadIdx.x >> 6;
+    u32x4 pw[NP];
+    float acc[NP][V];
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+        const int at = (lane + c * LANES) * V;
+        pw[c] = load_piece<T, ALIGNED>(w, at, d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[c][i] = 0.f;
+    }
+    const float inv_d = 1.f / d;
+    for (long long row = (long long)blockIdx.x * ROWS + (W == 1 ? wave : 0); row < rows; row += (long long)gridDim.x * ROWS) {
+        const size_t at0 = (size_t)row * d;
+        u32x4 ps[NP], pg[NP], pd[NP];
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            const int at = (lane + c * LANES) * V;
+            ps[c] = load_piece<T, ALIGNED>(sum + at0, at, d);
+            pg[c] = load_piece<T, ALIGNED>(dy + at0, at, d);
+            pd[c] = u32x4{0, 0, 0, 0};
+        }
+        if (dsum)
+#pragma unroll
+            for (int c = 0; c < NP; ++c) pd[c] = load_piece<T, ALIGNED>(dsum + at0, (lane + c * LANES) * V, d);
+        float ss = 0.f, along = 0.f;
+#pragma unroll
+        for (int c = 0; c < NP; ++c)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float s = RowPiece<T>::get(ps[c], i);
+                ss += s * s;
+                along += RowPiece<T>::get(pg[c], i) * RowPiece<T>::get(pw[c], i) * s;
+            }
+        ss = row_sum<W>(ss, lds);
+        along = row_sum<W>(along, lds + W);
+        const float r = 1.f / sqrtf(ss * inv_d + eps);
+        const float k = along * r * inv_d;   // mean(m n)
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            const int at = (lane + c * LANES) * V;
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float n = RowPiece<T>::get(ps[c], i) * r, g = RowPiece<T>::get(pg[c], i);
+                acc[c][i] += g * n;
+                v[i] = RowPiece<T>::get(pd[c], i) + r * (g * RowPiece<T>::get(pw[c], i) - n * k);
+            }
+            if (at < d) store_piece<T, ALIGNED>(dx + at0, at, d, v);
+        }
+    }
+    // the block's column sums; with a row per wavefront the four wavefronts' are added in their order
+    float *out = part + (size_t)blockIdx.x * d;
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+        const int at = (lane + c * LANES) * V;
+        if constexpr (W == 1) {
+            __syncthreads();
+            if (wave > 0)
+#pragma unroll
+                for (int i = 0; i < V; ++i) cols[wave - 1][i * 64 + lane] = acc[c][i];
+            __syncthreads();
+            if (wave == 0)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[c][i] = ((acc[c][i] + cols[0][i * 64 + lane]) + cols[1][i * 64 + lane]) + cols[2][i * 64 + lane];
+        }
+        if (W > 1 || wave == 0)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (at + i < d) out[at + i] = acc[c][i];
+    }
+}
+
+// d_w[c] = sum over the blocks, in their order: 64 columns per block, its 16 wavefronts take the partial rows b, b + 16, ..
+__global__ __launch_bounds__(1024) void norm_weight_sum_kernel(const float *__restrict__ part, float *__restrict__ dw, int blocks, int d)
+{
+    __shared__ float t[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    float a[4] = {0.f, 0.f, 0.f, 0.f};
+    if (col < d) {
+        int b = wave;
+        for (; b + 48 < blocks; b += 64) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] += part[(size_t)(b + 16 * i) * d + col];
+        }
+        for (; b < blocks; b += 16) a[0] += part[(size_t)b * d + col];
+    }
+    t[wave][lane] = (a[0] + a[1]) + (a[2] + a[3]);
+    __syncthreads();
+    if (wave == 0 && col < d) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += t[i][lane];
+        dw[col] = s;
+    }
+}
+
+// Calls f.run<T, ALIGNED, W, NP>() for a row of d elements: one wavefront takes up to eight pieces per lane (4096 bf16 or 2048 fp32
+// values), then four, then sixteen of them.
+template <typename T, typename F> static hipError_t pick_row(int d, const F &f)
+{
+    constexpr int V = RowPiece<T>::V;
+    const int pieces = (d + V - 1) / V;
+    const auto go = [&](auto al) {
+        constexpr bool A = decltype(al)::value;
+        if (pieces <= 64) return f.template run<T, A, 1, 1>();
+        if (pieces <= 128) return f.template run<T, A, 1, 2>();
+        if (pieces <= 256) return f.template run<T, A, 1, 4>();
+        if (pieces <= 512) return f.template run<T, A, 1, 8>();
+        if (pieces <= 1024) return f.template run<T, A, 4, 4>();
+        if constexpr (V == 4)   // (bf16 rows end at 2048 pieces)
+            if (pieces > 2048) return f.template run<T, A, 16, 4>();
+        return f.template run<T, A, 4, 8>();
+    };
+    return d % V == 0 ? go(std::true_type()) : go(std::false_type());
+}
+
+struct ForwardCall {
+    const void *x, *residual, *w;
+    void *sum, *y;
+    uint8_t *yq;
+    float *yscale;
+    int rows, d;
+    float eps;
+    hipStream_t s;
+    template <typename T, bool A, int W, int NP> hipError_t run() const
+    {
+        const unsigned blocks = W == 1 ? (unsigned)((rows + 3ll) / 4) : (unsigned)rows;
+        const int threads = W == 16 ? 1024 : 256;
+        if (yq)
+            add_rmsnorm_kernel<T, A, W, NP, true><<<blocks, threads, 0, s>>>((const T *)x, (const T *)residual, (const T *)w, (T *)sum, (T *)y,
+                                                                           yq, yscale, rows, d, eps);
+        else
+            add_rmsnorm_kernel<T, A, W, NP, false><<<blocks, threads, 0, s>>>((const T *)x, (const T *)residual, (const T *)w, (T *)sum, (T *)y,
+                                                                            nullptr, nullptr, rows, d, eps);
+        return hipGetLastError();
+    }
+};
+
+struct BackwardCall {
+    const void *sum, *w, *dy, *dsum;
+    void *dx;
+    float *part;
+    int rows, d, blocks;
+    float eps;
+    hipStream_t s;
+    template <typename T, bool A, int W, int NP> hipError_t run() const
+    {
+        add_rmsnorm_backward_kernel<T, A, W, NP><<<blocks, W == 16 ? 1024 : 256, 0, s>>>((const T *)sum, (const T *)w, (const T *)dy, (const T *)dsum,
+                                                                                       (T *)dx, part, rows, d, eps);
+        return hipGetLastError();
+    }
+};
+
+int norm_backward_blocks(int rows) { return rows < 1 ? 1 : rows < 4 * kNormBackwardBlocks ? (rows + 3) / 4 : kNormBackwardBlocks; }
+
+hipError_t launch_add_rmsnorm(const slicemoe_norm_config &c, const void *x, const void *residual, const void *weight, void *sum, void *y,
+                              uint8_t *yq, float *yscale, hipStream_t s)
+{
+    if (c.T == 0) return hipSuccess;
+    const ForwardCall f{x, residual, weight, sum, y, yq, yscale, c.T, c.d, c.eps, s};
+    return c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);
+}
+
+hipError_t launch_add_rmsnorm_backward(const slicemoe_norm_config &c, const void *sum, const void *weight, const void *dy,
+                                       const void *dsum, void *dx, float *dw, float *part, hipStream_t s)
+{
+    const int blocks = norm_backward_blocks(c.T);
+    const BackwardCall f{sum, weight, dy, dsum, dx, part, c.T, c.d, blocks, c.eps, s};
+    const hipError_t e = c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);   // T = 0 writes zeros to part
+    if (e != hipSuccess) return e;
+    norm_weight_sum_kernel<<<(c.d + 63) / 64, 1024, 0, s>>>(part, dw, blocks, c.d);
+    return hipGetLastError();
+}
+
+}  // namespace slicemoe

@@ -16,6 +16,17 @@ __device__ __forceinline__ int wavefront_sum(int v)
            __builtin_amdgcn_readlane(v, 48);
 }
 
+__device__ __forceinline__ float wavefront_sum_f32(float v)   // in the order of the pairs above, the same in every lane
+{
+    v += __int_as_float(lane_move<0xB1>(__float_as_int(v)));
+    v += __int_as_float(lane_move<0x4E>(__float_as_int(v)));
+    v += __int_as_float(lane_move<0x141>(__float_as_int(v)));
+    v += __int_as_float(lane_move<0x140>(__float_as_int(v)));
+    const int b = __float_as_int(v);
+    return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
+           (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+}
+
 __device__ __forceinline__ int wavefront_exclusive_scan(int v, int lane)
 {
     int s = v;

@@ -1,0 +1,78 @@
+"""Gated feed-forward network, both directions and with 8-bit operands, against 64 bits."""
+import pytest
+import torch
+
+import block_reference as R
+
+pytestmark = pytest.mark.gpu
+
+B16, F32 = torch.bfloat16, torch.float32
+NAME = {B16: "bf16", F32: "f32"}
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2510_04286_amd import binding
+    assert torch.cuda.is_available()
+    return binding
+
+
+def tensor(shape, seed, scale=1.0, dt=torch.float64):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, dtype=torch.float64, device="cuda") * scale).to(dt)
+
+
+def weights(d, H, dt, seed=0):
+    return {"Wg": tensor((d, H), seed + 1, d ** -0.5, dt), "Wu": tensor((d, H), seed + 2, d ** -0.5, dt),
+            "Wd": tensor((H, d), seed + 3, H ** -0.5, dt)}
+
+
+def space(n):
+    return torch.full((n,), 255, dtype=torch.uint8, device="cuda")   # (NaN wherever something is read that was not written)
+
+
+def run(B, T, d, H, dt, backward=True, seed=0, addend=True):
+    w = weights(d, H, dt, seed)
+    x, add, dy, dadd = (tensor((T, d), seed + 10 + i, s, dt) for i, s in enumerate((1.0, 1.0, 1e-3, 1e-3)))
+    if not addend:
+        add = dadd = None
+    cfg = B.make_gated_config(T, d, H, NAME[dt])
+    got = {"y": torch.full((T, d), 7.0, dtype=dt, device="cuda")}
+    B.slicemoe_gated_ffn(cfg, x, w, got["y"], space(B.slicemoe_gated_ffn_workspace_bytes(cfg)), addend=add)
+    ref = R.gated(x, w, add, dt, dy if backward else None, dadd)
+    if backward:
+        got["d_x"] = torch.full((T, d), 7.0, dtype=dt, device="cuda")
+        got.update({n: torch.full_like(t, 7.0) for n, t in w.items()})
+        B.slicemoe_gated_ffn_backward(cfg, x, w, dy, got["d_x"], got, space(B.slicemoe_gated_ffn_backward_workspace_bytes(cfg)), addend=dadd)
+    torch.cuda.synchronize()
+    for n, (v, e) in ref.items():
+        R.within(got[n], v, e, f"{n} at T={T} d={d} H={H} {dt}")
+        # and over all elements: every rounding of the path at its largest, independent of one another
+        off = float((got[n].double() - v).norm())
+        assert off <= 3 * R.HALF[dt] * float(v.norm()) * (1 if dt == B16 else 8), n
+    return got
+
+
+# (T, d, H): one token and one value; ragged everything; whole tiles; each tile size; splits of the contraction
+SMALL = [(1, 1, 1), (1, 8, 8), (1, 64, 64), (3, 5, 7), (31, 40, 33), (32, 64, 128), (33, 72, 200), (64, 128, 256), (64, 1000, 520),
+         (65, 65, 65), (100, 257, 683), (128, 64, 64), (129, 136, 72), (257, 264, 1032), (300, 512, 96), (1000, 256, 683)]
+
+
+@pytest.mark.parametrize("dt", [B16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,d,H", SMALL)
+def test_small(B, T, d, H, dt):
+    run(B, T, d, H, dt)
+
+
+@pytest.mark.parametrize("T,d,H", [(4096, 512, 4096), (4099, 520, 4104), (3001, 4096, 2049)])
+def test_large_tiles(B, T, d, H):
+    run(B, T, d, H, B16)
+
+
+def test_large_tiles_fp32(B):
+    run(B, 2051, 300, 6500, F32)
+
+
+def test_without_addends(B):
+    run(B, 77, 96, 200, B16, addend=False)
+    run(B, 300, 257, 200, F32, addend=False)
