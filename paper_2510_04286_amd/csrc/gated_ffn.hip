@@ -187,8 +187,8 @@ __device__ __forceinline__ void share_of(const GemmProblem &p, int split, int &s
     s1 = s0 + each < steps ? s0 + each : steps;
 }
 
-// Both projections and the gate.  part: the raw sums of a share instead, [split][2][rows][ld] fp32.
-template <typename S, int TERMS>
+// Both projections and the gate.  SHARE: the raw sums of a share of the contraction instead, part[split][2][rows][ld] in fp32.
+template <typename S, int TERMS, bool SHARE>
 __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, Scales sc, float *__restrict__ part)
 {
     extern __shared__ __align__(1024) char lds[];
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, 
     share_of(p, at.split, s0, s1);
     mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
     const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
-    if (part) {
+    if constexpr (SHARE) {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const Out o = {part + (size_t)(2 * at.split + m) * h.rows * h.ld, nullptr, h.rows, h.ld, 1};
@@ -585,17 +585,15 @@ static GemmProblem problem(int nr, int nf, long long K, long long ldr, long long
 
 template <typename K> static hipError_t ready(K kernel, int lds) { return grant_dynamic_lds((const void *)kernel, lds); }
 
-template <typename S, int TERMS> static hipError_t run_up(GemmProblem p, const Hidden &h, const Scales &sc, int splits, float *part, hipStream_t s)
+template <typename S, int TERMS, bool SHARE>
+static hipError_t run_up(GemmProblem p, const Hidden &h, const Scales &sc, int splits, float *part, hipStream_t s)
 {
     set_tiles<S>(p, splits);
     constexpr int lds = lds_of<S>(S::FT);
-    const auto kernel = gated_up_kernel<S, TERMS>;
-    hipError_t e = ready(kernel, lds);
+    const auto kernel = gated_up_kernel<S, TERMS, SHARE>;
+    const hipError_t e = ready(kernel, lds);
     if (e != hipSuccess) return e;
-    kernel<<<p.tiles_r * p.tiles_f * splits, 256, lds, s>>>(p, h, sc, splits > 1 ? part : nullptr);
-    if ((e = hipGetLastError()) != hipSuccess || splits == 1) return e;
-    const long long n = (long long)h.rows * ((h.cols + 7) / 8);
-    gated_up_sum_kernel<TERMS, S::E4M3><<<(int)std::min<long long>((n + 255) / 256, 8ll * num_compute_units()), 256, 0, s>>>(part, h, sc, splits);
+    kernel<<<p.tiles_r * p.tiles_f * splits, 256, lds, s>>>(p, h, sc, part);
     return hipGetLastError();
 }
 template <int FL, bool E4M3, int TERMS>
@@ -603,11 +601,14 @@ static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales 
 {
     typedef Shapes<kKContiguous, FL, true, E4M3> Sh;
     const TileChoice t = choose_tiles(p.nr, p.nf, steps_of(p), true, p.nr <= kFewRows);
-    switch (t.size) {
-        case kBig: return run_up<typename Sh::Big, TERMS>(p, h, sc, t.splits, part, s);
-        case kMiddle: return run_up<typename Sh::Middle, TERMS>(p, h, sc, t.splits, part, s);
-        default: return run_up<typename Sh::Small, TERMS>(p, h, sc, t.splits, part, s);
-    }
+    if (t.size == kBig) return run_up<typename Sh::Big, TERMS, false>(p, h, sc, 1, nullptr, s);
+    if (t.size == kMiddle) return run_up<typename Sh::Middle, TERMS, false>(p, h, sc, 1, nullptr, s);
+    if (t.splits == 1) return run_up<typename Sh::Small, TERMS, false>(p, h, sc, 1, nullptr, s);
+    const hipError_t e = run_up<typename Sh::Small, TERMS, true>(p, h, sc, t.splits, part, s);
+    if (e != hipSuccess) return e;
+    const long long n = (long long)h.rows * ((h.cols + 7) / 8);
+    gated_up_sum_kernel<TERMS, E4M3><<<(int)std::min<long long>((n + 255) / 256, 8ll * num_compute_units()), 256, 0, s>>>(part, h, sc, t.splits);
+    return hipGetLastError();
 }
 
 template <typename S> static hipError_t run_products(Products &ps, int n, hipStream_t s)

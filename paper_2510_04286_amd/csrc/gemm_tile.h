@@ -7,18 +7,20 @@
 // A step of the contraction is 128 bytes of a row: 64 bf16 values or 128 e4m3 ones.  Its images in the LDS come straight from memory
 // (global_load_lds, 16 bytes per lane): 1 KB per instruction, linear in the lane, so the arrangement that keeps the reads free of
 // bank conflicts is made by which 16 bytes a lane asks for.
-//   K-contiguous operands ([row][k] in memory): 128 bytes per row, piece c of row i at place c ^ (i & 7); a fragment is one
+//   K-contiguous operands ([row][k] in memory): 128 bytes per row, piece c of row i at place c ^ (i / 2 % 8); a fragment is one
 //     ds_read_b128 (lane = row, eight consecutive k).
 //   K-major operands ([k][row] in memory): rows of k, blocks of 64 bytes (32 rows) XORed with k & 3; a fragment is two
 //     ds_read_b64_tr_b16, which hand every lane the four k of its row.
 //
-// The ring has STAGES images.  Inside a step the fragments of the next quarter are read while the matrix instructions of the present
-// one run; in front of the last quarter stands the step's one barrier: behind it the next step's image has landed for every
-// wavefront and the present one, whose last fragments are in registers, is free for the loads STAGES steps ahead.
+// The ring has STAGES images.  Inside a step the fragments of the next quarter are read between the matrix instructions of the present
+// one; in front of the last quarter stands the step's one barrier: behind it the next step's image has landed for every
+// wavefront and the present one, whose last fragments are in registers, is free for the requests STAGES steps ahead.
 //
 // Edges: rows and columns past an operand's end are read at its last one (their products are never stored); a step that reaches past
 // the end of K takes those 16-byte pieces from a page of zeros, in both operands.
 #pragma once
+#include <type_traits>
+
 #include "lds_rows.h"
 #include "wavefront.h"
 
@@ -43,66 +45,76 @@ enum { kKContiguous = 0, kKMajor = 1 };
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// 1 KB from memory to the LDS: lane l's 16 bytes go to `at` + 16 l.  (Written out, because the compiler would wait for all of
-// them in front of every LDS read; the waits are in the pipeline below.)
-__device__ __forceinline__ void load_lds_1k(uint32_t at, const char *base, uint32_t offset)
+template <int I> using Int = std::integral_constant<int, I>;
+// f(Int<A>()), .. f(Int<B - 1>())
+template <int A, int B, typename F> __device__ __forceinline__ void for_range(const F &f)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory");
+    if constexpr (A < B) {
+        f(Int<A>());
+        for_range<A + 1, B>(f);
+    }
 }
-__device__ __forceinline__ void load_lds_1k(uint32_t at, const char *address)
+
+
+// 1 KB from memory to the LDS: lane l's 16 bytes go to M0 + AT + 16 l and come from base + offset + AT (the instruction's own offset
+// moves both).  Written out, because the compiler would wait for all of them in front of every LDS read; the waits are in the
+// pipeline below.  Nothing else in these kernels writes M0.
+__device__ __forceinline__ void set_lds_target(uint32_t at) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(at) : "memory"); }
+template <int AT> __device__ __forceinline__ void load_lds_1k(const char *base, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(address) : "memory");
+    asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(offset), "s"(base), "n"(AT) : "memory");
+}
+template <int AT> __device__ __forceinline__ void load_lds_1k(const char *address)
+{
+    asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(address), "n"(AT) : "memory");
 }
 template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
 {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// The image of one operand: N rows of the tile (a multiple of 32).  Instruction i of wavefront w fills kilobyte 4 i + w: every
-// wavefront's lanes then sit on the same k & 3 in all of its instructions, and one offset per lane does for a K-major operand.
+// The image of one operand: N rows of the tile (a multiple of 32).  Wavefront w fills the kilobytes PER_WAVE w + i, four of them (or
+// all) from one LDS target.
 template <int LAYOUT, int N> struct TileImage {
     static constexpr int BYTES = N * 128, PER_WAVE = N / 32;
-    static constexpr int K_PER_PIECE = 512 / N;   // rows of k per instruction (K-major)
-    static constexpr int OFFSETS = LAYOUT == kKContiguous ? PER_WAVE : 1;
+    static constexpr int K_PER_PIECE = 512 / N;   // rows of k per kilobyte (K-major)
+    static constexpr int BIAS = 3072;             // what the instruction's own offset adds at most is taken off the base, added to the offsets
     static __device__ __forceinline__ int block_swizzle(int k) { return N >= 128 ? k & 3 : N == 64 ? k >> 1 & 1 : 0; }
-    static __device__ __forceinline__ int piece_of(int lane) { return (lane & 7) ^ (lane >> 3); }   // K-contiguous: which 16 bytes of its row
+    // K-contiguous: which 16 bytes of its row a lane fetches (see FragmentReader: 16 rows at a time, two to the 64 banks)
+    static __device__ __forceinline__ int piece_of(int kb, int lane) { return (lane & 7) ^ ((kb & 1) << 2 | lane >> 4); }
 
     // This lane's offsets from the tile's corner (the operand's row `first`, step 0 of K).
-    static __device__ __forceinline__ void offsets(uint32_t (&o)[OFFSETS], int wave, int lane, int first, int rows, uint32_t ld)
+    static __device__ __forceinline__ void offsets(uint32_t (&o)[PER_WAVE], int wave, int lane, int first, int rows, uint32_t ld)
     {
-        if constexpr (LAYOUT == kKContiguous) {
-            const int last = rows - 1 - first;
 #pragma unroll
-            for (int i = 0; i < PER_WAVE; ++i) {
-                const int row = 8 * (4 * i + wave) + (lane >> 3);
-                o[i] = (uint32_t)(row < last ? row : last) * ld + 16u * piece_of(lane);
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int kb = wave * PER_WAVE + i;
+            if constexpr (LAYOUT == kKContiguous) {
+                const int row = 8 * kb + (lane >> 3), last = rows - 1 - first;
+                o[i] = (uint32_t)(row < last ? row : last) * ld + 16u * piece_of(kb, lane);
+            } else {
+                const int k = kb * K_PER_PIECE + lane / (N / 8), last = (rows - 1 - first) >> 3;
+                const int c = (lane % (N / 8)) ^ block_swizzle(k) << 2;
+                o[i] = (uint32_t)k * ld + 16u * (c < last ? c : last);
             }
-        } else {
-            const int k = lane / (N / 8), last = (rows - 1 - first) >> 3;
-            const int c = (lane % (N / 8)) ^ block_swizzle(wave * K_PER_PIECE + k) << 2;
-            o[0] = (uint32_t)(wave * K_PER_PIECE + k) * ld + 16u * (c < last ? c : last);
+            o[i] += BIAS - 1024 * (i & 3);
         }
     }
     static __device__ __forceinline__ const char *corner(const char *p, int first, long long ld)
     {
-        return LAYOUT == kKContiguous ? p + first * ld : p + 2ll * first;
+        return (LAYOUT == kKContiguous ? p + first * ld : p + 2ll * first) - BIAS;
     }
     static __device__ __forceinline__ long long step_bytes(long long ld) { return LAYOUT == kKContiguous ? 128 : 64 * ld; }
 
-    // Requests the image of one step.  left: bytes of K from this step on (below 128 in a step that reaches past the end).
-    static __device__ __forceinline__ void request(uint32_t lds, const char *base, const uint32_t (&o)[OFFSETS], int wave, int lane, int left, long long ld)
+    // Requests kilobyte i of this wavefront's share of the image of one step.  TAIL: the last step of K, of which `left` bytes are there.
+    template <bool TAIL, int I> static __device__ __forceinline__ void request(uint32_t lds, const char *base, const uint32_t (&o)[PER_WAVE], int wave, int lane, int left)
     {
-        if (left >= 128) {
-#pragma unroll
-            for (int i = 0; i < PER_WAVE; ++i)
-                load_lds_1k(lds + 1024 * (4 * i + wave), LAYOUT == kKContiguous ? base : base + i * (4 * K_PER_PIECE * ld), o[LAYOUT == kKContiguous ? i : 0]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < PER_WAVE; ++i) {
-                const bool there = LAYOUT == kKContiguous ? 16 * piece_of(lane) < left : 2 * ((4 * i + wave) * K_PER_PIECE + lane / (N / 8)) < left;
-                const char *a = base + (LAYOUT == kKContiguous ? 0 : i * (4 * K_PER_PIECE * ld)) + o[LAYOUT == kKContiguous ? i : 0];
-                load_lds_1k(lds + 1024 * (4 * i + wave), there ? a : (const char *)g_zero_piece);
-            }
+        if constexpr (I % 4 == 0) set_lds_target(lds + 1024 * (wave * PER_WAVE + I));
+        if constexpr (!TAIL) load_lds_1k<1024 * (I & 3)>(base, o[I]);
+        else {
+            const int kb = wave * PER_WAVE + I;
+            const bool there = LAYOUT == kKContiguous ? 16 * piece_of(kb, lane) < left : 2 * (kb * K_PER_PIECE + lane / (N / 8)) < left;
+            load_lds_1k<1024 * (I & 3)>(there ? base + o[I] : (const char *)g_zero_piece - 1024 * (I & 3));
         }
     }
 };
@@ -118,7 +130,7 @@ template <int LAYOUT, int N, bool E4M3> struct FragmentReader {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {   // E4M3: 32 bytes of a row, pieces 4 ks + 2 g and the next; else pieces 2 ks + g
                 const int c = E4M3 ? 4 * (q >> 1) + 2 * g + (q & 1) : 2 * q + g;
-                base[q] = (wb * 32 + i) * 128 + ((c ^ (i & 7)) << 4);
+                base[q] = (wb * 32 + i) * 128 + ((c ^ (i >> 1 & 7)) << 4);
             }
         } else {
             const int q = lane >> 2 & 3;   // which of four k this lane fetches
@@ -160,7 +172,8 @@ template <int TR_, int TF_, int WR_, int WF_, int RL_, int FL_, bool DUAL_, bool
     static constexpr int STAGE_BYTES = RI::BYTES + IMAGES * FI::BYTES;
     static constexpr int LOADS = RI::PER_WAVE + IMAGES * FI::PER_WAVE;   // instructions per wavefront and step
     static constexpr int LDS = STAGES * STAGE_BYTES;
-    static constexpr int KS = E4M3 ? 2 : 4;                              // matrix-instruction steps per step
+    static constexpr int KS = E4M3 ? 2 : 4;                              // matrix-instruction steps (quarters, halves) per step
+    static constexpr int SPREAD = E4M3 ? 1 : 2;
 };
 
 // acc[feature tile][row tile] += the steps [s0, s1) of the problem's contraction (counted through its segments).
@@ -174,7 +187,7 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
     const int n = s1 - s0;
     if (n <= 0) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)as_lds(lds);
-    uint32_t ro[RI::OFFSETS], fo[FI::OFFSETS];
+    uint32_t ro[RI::PER_WAVE], fo[FI::PER_WAVE];
     RI::offsets(ro, wave, lane, row0, p.nr, (uint32_t)p.ldr);
     FI::offsets(fo, wave, lane, f0, p.nf, (uint32_t)p.ldf);
     FragmentReader<S::RL, S::BR, S::E4M3> rr;
@@ -184,6 +197,8 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
 
     // where the next request comes from
     const int per_segment = (p.K + 127) >> 7;
+    uint64_t rstep = RI::step_bytes(p.ldr), fstep = FI::step_bytes(p.ldf);
+    asm volatile("" : "+s"(rstep), "+s"(fstep));   // (kept in registers: fetched again inside the loop they would make it wait for every LDS read)
     int seg = s0 / per_segment, at = s0 - seg * per_segment, slot = 0;
     const char *rp, *fp, *fp2 = nullptr;
     const auto enter = [&]() {
@@ -192,65 +207,117 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
         if constexpr (S::DUAL) fp2 = FI::corner(p.f2[seg], f0, p.ldf) + at * FI::step_bytes(p.ldf);
     };
     enter();
-    const auto request = [&]() {
+    // kilobyte I of the step that is requested next, and the move to the one after it
+    const auto piece = [&](auto tail, auto index, int left) {
+        constexpr bool TAIL = decltype(tail)::value;
+        constexpr int I = decltype(index)::value, F = I - RI::PER_WAVE;
         const uint32_t to = lds0 + slot * S::STAGE_BYTES;
-        const int left = p.K - 128 * at;
-        RI::request(to, rp, ro, wave, lane, left, p.ldr);
-        FI::request(to + RI::BYTES, fp, fo, wave, lane, left, p.ldf);
-        if constexpr (S::DUAL) FI::request(to + RI::BYTES + FI::BYTES, fp2, fo, wave, lane, left, p.ldf);
+        if constexpr (F < 0) RI::template request<TAIL, I>(to, rp, ro, wave, lane, left);
+        else if constexpr (F < FI::PER_WAVE) FI::template request<TAIL, F>(to + RI::BYTES, fp, fo, wave, lane, left);
+        else FI::template request<TAIL, F - FI::PER_WAVE>(to + RI::BYTES + FI::BYTES, fp2, fo, wave, lane, left);
+    };
+    const auto pieces = [&](auto tail, auto from, auto to, int left) {
+        for_range<decltype(from)::value, decltype(to)::value>([&](auto i) { piece(tail, i, left); });
+    };
+    const auto advance = [&]() {
         slot = slot + 1 == S::STAGES ? 0 : slot + 1;
         if (++at == per_segment) {
             at = 0;
             if (++seg < p.segments) enter();
         } else {
-            rp += RI::step_bytes(p.ldr);
-            fp += FI::step_bytes(p.ldf);
-            if constexpr (S::DUAL) fp2 += FI::step_bytes(p.ldf);
+            rp += rstep;
+            fp += fstep;
+            if constexpr (S::DUAL) fp2 += fstep;
         }
     };
     typedef typename FragmentReader<S::RL, S::BR, S::E4M3>::frag frag;
     frag rf[2][S::TR], ff[2][S::TF];
-    const auto read = [&](int set, const char *image, int ks) {
-#pragma unroll
-        for (int t = 0; t < S::TR; ++t) rf[set][t] = rr.read(image, t, ks);
-#pragma unroll
-        for (int t = 0; t < S::TF; ++t) ff[set][t] = fr.read(image + RI::BYTES + (t / S::FT) * FI::BYTES, t % S::FT, ks);
+    // fragment i of quarter ks, in the order of their first use: the first features', all rows', the other features'
+    const auto read = [&](int set, const char *image, int ks, int i) {
+        if (i >= 1 && i <= S::TR) rf[set][i - 1] = rr.read(image, i - 1, ks);
+        else {
+            const int t = i == 0 ? 0 : i - S::TR;
+            ff[set][t] = fr.read(image + RI::BYTES + (t / S::FT) * FI::BYTES, t % S::FT, ks);
+        }
     };
-    const auto multiply = [&](int set) {
-#pragma unroll
-        for (int t = 0; t < S::TF; ++t)
-#pragma unroll
-            for (int u = 0; u < S::TR; ++u) {
-                if constexpr (S::E4M3)   // (scales of 2^0)
-                    acc[t][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ff[set][t], rf[set][u], acc[t][u], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-                else
-                    acc[t][u] = mfma_bf16(ff[set][t], rf[set][u], acc[t][u]);
-            }
+    const auto multiply = [&](int set, int m) {
+        const int t = m / S::TR, u = m % S::TR;
+        if constexpr (S::E4M3)   // (scales of 2^0)
+            acc[t][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ff[set][t], rf[set][u], acc[t][u], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+        else
+            acc[t][u] = mfma_bf16(ff[set][t], rf[set][u], acc[t][u]);
     };
+    // One quarter: its matrix instructions, with the reads of the next quarter and the requests [from, to) of a later step between them.
+    // A wavefront issues in order, and one that asks for several kilobytes in a row stands still until the memory pipeline has taken
+    // them: each request has its own place.
+    constexpr int NM = S::TR * S::TF, NF = S::TR + S::TF;
+    const auto quarter = [&](int set, auto reads, const char *next, int next_ks, auto tail, auto from, auto to, int left) {
+        constexpr bool READS = decltype(reads)::value;
+        constexpr int FROM = decltype(from)::value, TO = decltype(to)::value;
+        for_range<0, NM>([&](auto mm) {
+            constexpr int M = decltype(mm)::value;
+            multiply(set, M);
+            if constexpr (READS)
+#pragma unroll
+                for (int i = M * NF / NM; i < (M + 1) * NF / NM; ++i) read(set ^ 1, next, next_ks, i);
+            pieces(tail, Int<FROM + M *(TO - FROM) / NM>(), Int<FROM + (M + 1) * (TO - FROM) / NM>(), left);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // The last quarter of one step and all but the last of the next one, whose image is `image`, with the requests of a later one:
+    // of how many kilobytes, and whether it is the last of its segment.
+    const auto step = [&](auto tail, auto loads, const char *image, int left) {
+        constexpr int LOADS = decltype(loads)::value;
+        for_range<0, S::KS>([&](auto qq) {
+            constexpr int Q = decltype(qq)::value, A = Q < S::SPREAD ? Q : S::SPREAD, Z = Q + 1 < S::SPREAD ? Q + 1 : S::SPREAD;
+            quarter((Q + S::KS - 1) & 1, std::true_type(), image, Q, tail, Int<A * LOADS / S::SPREAD>(), Int<Z * LOADS / S::SPREAD>(), left);
+        });
+    };
+    constexpr Int<0> none = {};
+    constexpr Int<S::LOADS> all = {};
 
-#pragma unroll
-    for (int i = 0; i < S::STAGES; ++i)
-        if (i < n) request();
+    for (int i = 0; i < S::STAGES && i < n; ++i) {
+        pieces(std::true_type(), none, all, p.K - 128 * at);
+        advance();
+    }
     if (n >= S::STAGES) wait_loads_and_barrier<S::LOADS *(S::STAGES - 1)>();
     else wait_loads_and_barrier<0>();
-    read(0, lds, 0);
-    int cur = 0;
-    for (int s = 0; s < n; ++s) {
-        const char *image = lds + cur * S::STAGE_BYTES;
-        cur = cur + 1 == S::STAGES ? 0 : cur + 1;
 #pragma unroll
-        for (int ks = 0; ks < S::KS; ++ks) {
-            if (ks + 1 < S::KS) read((ks + 1) & 1, image, ks + 1);
-            else {
-                // (every request so far but the newest STAGES - 2 steps'; near the end all of them)
-                if (s + S::STAGES - 1 < n) wait_loads_and_barrier<S::LOADS *(S::STAGES - 2)>();
-                else wait_loads_and_barrier<0>();
-                if (s + S::STAGES < n) request();
-                if (s + 1 < n) read(0, lds + cur * S::STAGE_BYTES, 0);
-            }
-            multiply(ks & 1);
+    for (int i = 0; i < NF; ++i) read(0, lds, 0, i);
+#pragma unroll
+    for (int q = 0; q + 1 < S::KS; ++q) quarter(q & 1, std::true_type(), lds, q + 1, std::false_type(), none, none, 0);
+    int cur = 0, todo = n - S::STAGES;   // steps to request
+    const auto next_image = [&]() {
+        cur = cur + 1 == S::STAGES ? 0 : cur + 1;
+        return lds + cur * S::STAGE_BYTES;
+    };
+    // (the newest STAGES - 2 steps' requests may be on their way still)
+    const auto whole_steps = [&](int count) {
+        at += count > 0 ? count : 0;
+        for (; count > 0; --count) {
+            wait_loads_and_barrier<S::LOADS *(S::STAGES - 2)>();
+            step(std::false_type(), all, next_image(), 0);
+            slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+            rp += rstep;
+            fp += fstep;
+            if constexpr (S::DUAL) fp2 += fstep;
         }
+    };
+    while (todo >= per_segment - at) {   // the rest of a segment: its whole steps, then its last
+        todo -= per_segment - at;
+        whole_steps(per_segment - at - 1);
+        wait_loads_and_barrier<S::LOADS *(S::STAGES - 2)>();
+        step(std::true_type(), all, next_image(), p.K - 128 * at);
+        advance();
     }
+    whole_steps(todo);
+    for (int s = (n < S::STAGES ? n : S::STAGES) - 1; s > 0; --s) {
+        wait_loads_and_barrier<0>();
+        step(std::false_type(), none, next_image(), 0);
+    }
+    quarter((S::KS - 1) & 1, std::false_type(), lds, 0, std::false_type(), none, none, 0);
+    // (the caller may use the LDS once every wavefront is past its last read: the barrier of the last step, or this one's)
+    if (n == 1) lds_barrier();
 }
 
 // Which tile and share of the contraction a block has: blocks of one XCD (blockIdx % 8) take consecutive tiles, in groups of eight row
