@@ -410,9 +410,9 @@ __global__ __launch_bounds__(256) void gated_quantize_kernel(const bf16_t *__res
 // Tile shapes.  Big: 256 rows x 256 features (gate and up: 128 of each), one block per CU.  Middle: 128 x 128, two blocks per CU.
 // Small: 32 rows x 128 features for the few rows of a decoding step.
 template <int RL, int FL, bool DUAL, bool E4M3> struct Shapes {
-    typedef TileShape<4, 4, 2, 2, RL, FL, DUAL, E4M3, 2> Big;
-    typedef TileShape<2, 2, 2, 2, RL, FL, DUAL, E4M3, 2> Middle;
-    typedef TileShape<1, DUAL ? 2 : 1, 1, 4, RL, FL, DUAL, E4M3, 4> Small;
+    typedef TileShape<4, 4, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Big;
+    typedef TileShape<2, 2, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Middle;
+    typedef TileShape<1, DUAL ? 2 : 1, 1, 4, RL, FL, DUAL, E4M3, 4, 4> Small;
 };
 template <typename S> constexpr int lds_of(int staged_tiles) { return S::LDS > stage_bytes(staged_tiles) ? S::LDS : stage_bytes(staged_tiles); }
 
@@ -716,8 +716,8 @@ template <int TERMS> static hipError_t launch_up_backward(const GemmProblem &p, 
 {
     typedef Shapes<kKContiguous, kKMajor, true, false> Sh;
     if (choose_tiles(p.nr, p.nf, steps_of(p), true, false).size == kBig)
-        return run_up_backward<typename Sh::Big, TileShape<4, 2, 2, 2, kKContiguous, kKContiguous, false, false, 2>, TERMS>(p, q, h, s);
-    return run_up_backward<typename Sh::Middle, TileShape<2, 1, 2, 2, kKContiguous, kKContiguous, false, false, 2>, TERMS>(p, q, h, s);
+        return run_up_backward<typename Sh::Big, TileShape<4, 2, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
+    return run_up_backward<typename Sh::Middle, TileShape<2, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
 }
 
 hipError_t launch_gated_ffn_backward(const slicemoe_gated_config &c, const GatedPlan &plan, const void *x, const slicemoe_gated_weights &w,

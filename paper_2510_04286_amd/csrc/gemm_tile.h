@@ -12,9 +12,10 @@
 //   K-major operands ([k][row] in memory): rows of k, blocks of 64 bytes (32 rows) XORed with k & 3; a fragment is two
 //     ds_read_b64_tr_b16, which hand every lane the four k of its row.
 //
-// The ring has STAGES images.  Inside a step the fragments of the next quarter are read between the matrix instructions of the present
-// one; in front of the last quarter stands the step's one barrier: behind it the next step's image has landed for every
-// wavefront and the present one, whose last fragments are in registers, is free for the requests STAGES steps ahead.
+// Each operand has a ring of images, the rows' one longer than the features' where the LDS has room for it (3 + 2 images of 32 KB).
+// Inside a step the fragments of the next quarter are read between the matrix instructions of the present one; in front of the last
+// quarter stands the step's one barrier: behind it the next step's images have landed for every wavefront and the present ones,
+// whose last fragments are in registers, are free for the requests two and three steps ahead.
 //
 // Edges: rows and columns past an operand's end are read at its last one (their products are never stored); a step that reaches past
 // the end of K takes those 16-byte pieces from a page of zeros, in both operands.
@@ -160,20 +161,20 @@ template <int LAYOUT, int N, bool E4M3> struct FragmentReader {
 };
 
 // TR x TF fragments of 32 rows and features per wavefront, WR x WF = 4 wavefronts.  DUAL: the first half of a wavefront's feature
-// tiles comes from f, the second from f2 (the same features of two matrices).
-template <int TR_, int TF_, int WR_, int WF_, int RL_, int FL_, bool DUAL_, bool E4M3_, int STAGES_> struct TileShape {
-    static constexpr int TR = TR_, TF = TF_, WR = WR_, WF = WF_, RL = RL_, FL = FL_, STAGES = STAGES_;
+// tiles comes from f, the second from f2 (the same features of two matrices).  SR, SF: images in the rings of the two operands.
+template <int TR_, int TF_, int WR_, int WF_, int RL_, int FL_, bool DUAL_, bool E4M3_, int SR_, int SF_> struct TileShape {
+    static constexpr int TR = TR_, TF = TF_, WR = WR_, WF = WF_, RL = RL_, FL = FL_, SR = SR_, SF = SF_;
     static constexpr bool DUAL = DUAL_, E4M3 = E4M3_;
     static_assert(WR * WF == 4 && TR <= 4 && TF <= 4, "four wavefronts, at most 128 x 128 each");
+    static_assert(SF >= 2 && (SR == SF || SR == SF + 1), "see the waits");
     static constexpr int IMAGES = DUAL ? 2 : 1, FT = TF / IMAGES;   // feature tiles per image and wavefront
     static constexpr int BR = 32 * TR * WR, BF = 32 * FT * WF;      // rows, features (of one image) per block
     typedef TileImage<RL, BR> RI;
     typedef TileImage<FL, BF> FI;
-    static constexpr int STAGE_BYTES = RI::BYTES + IMAGES * FI::BYTES;
-    static constexpr int LOADS = RI::PER_WAVE + IMAGES * FI::PER_WAVE;   // instructions per wavefront and step
-    static constexpr int LDS = STAGES * STAGE_BYTES;
+    static constexpr int R_BYTES = RI::BYTES, F_BYTES = IMAGES * FI::BYTES;
+    static constexpr int R_LOADS = RI::PER_WAVE, F_LOADS = IMAGES * FI::PER_WAVE;   // instructions per wavefront and step
+    static constexpr int LDS = SR * R_BYTES + SF * F_BYTES;
     static constexpr int KS = E4M3 ? 2 : 4;                              // matrix-instruction steps (quarters, halves) per step
-    static constexpr int SPREAD = E4M3 ? 1 : 2;
 };
 
 // acc[feature tile][row tile] += the steps [s0, s1) of the problem's contraction (counted through its segments).
@@ -195,49 +196,66 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
     rr.init(wr * S::TR, lane);
     fr.init(wf * S::FT, lane);
 
-    // where the next request comes from
+    // Where the next request of each operand comes from (segment, step of it, pointer) and goes to (image of its ring).
     const int per_segment = (p.K + 127) >> 7;
     uint64_t rstep = RI::step_bytes(p.ldr), fstep = FI::step_bytes(p.ldf);
     asm volatile("" : "+s"(rstep), "+s"(fstep));   // (kept in registers: fetched again inside the loop they would make it wait for every LDS read)
-    int seg = s0 / per_segment, at = s0 - seg * per_segment, slot = 0;
+    int rseg = s0 / per_segment, rat = s0 - rseg * per_segment, rslot = 0, fseg = rseg, fat = rat, fslot = 0;
     const char *rp, *fp, *fp2 = nullptr;
-    const auto enter = [&]() {
-        rp = RI::corner(p.r[seg], row0, p.ldr) + at * RI::step_bytes(p.ldr);
-        fp = FI::corner(p.f[seg], f0, p.ldf) + at * FI::step_bytes(p.ldf);
-        if constexpr (S::DUAL) fp2 = FI::corner(p.f2[seg], f0, p.ldf) + at * FI::step_bytes(p.ldf);
+    const auto enter_r = [&]() { rp = RI::corner(p.r[rseg], row0, p.ldr) + rat * rstep; };
+    const auto enter_f = [&]() {
+        fp = FI::corner(p.f[fseg], f0, p.ldf) + fat * fstep;
+        if constexpr (S::DUAL) fp2 = FI::corner(p.f2[fseg], f0, p.ldf) + fat * fstep;
     };
-    enter();
-    // kilobyte I of the step that is requested next, and the move to the one after it
-    const auto piece = [&](auto tail, auto index, int left) {
+    enter_r();
+    enter_f();
+    // kilobytes [from, to) of a step's requests: the features' first, then the rows'; TAIL: either may be in the last step of its segment
+    const auto pieces = [&](auto tail, auto from, auto to, int rleft, int fleft) {
         constexpr bool TAIL = decltype(tail)::value;
-        constexpr int I = decltype(index)::value, F = I - RI::PER_WAVE;
-        const uint32_t to = lds0 + slot * S::STAGE_BYTES;
-        if constexpr (F < 0) RI::template request<TAIL, I>(to, rp, ro, wave, lane, left);
-        else if constexpr (F < FI::PER_WAVE) FI::template request<TAIL, F>(to + RI::BYTES, fp, fo, wave, lane, left);
-        else FI::template request<TAIL, F - FI::PER_WAVE>(to + RI::BYTES + FI::BYTES, fp2, fo, wave, lane, left);
+        for_range<decltype(from)::value, decltype(to)::value>([&](auto index) {
+            constexpr int I = decltype(index)::value, G = I - FI::PER_WAVE, R = I - S::F_LOADS;
+            const uint32_t f_to = lds0 + S::SR * S::R_BYTES + fslot * S::F_BYTES;
+            if constexpr (R >= 0) RI::template request<TAIL, R>(lds0 + rslot * S::R_BYTES, rp, ro, wave, lane, rleft);
+            else if constexpr (G >= 0) FI::template request<TAIL, G>(f_to + FI::BYTES, fp2, fo, wave, lane, fleft);
+            else FI::template request<TAIL, I>(f_to, fp, fo, wave, lane, fleft);
+        });
     };
-    const auto pieces = [&](auto tail, auto from, auto to, int left) {
-        for_range<decltype(from)::value, decltype(to)::value>([&](auto i) { piece(tail, i, left); });
+    const auto next_r = [&]() {   // (within a segment)
+        rslot = rslot + 1 == S::SR ? 0 : rslot + 1;
+        ++rat;
+        rp += rstep;
     };
-    const auto advance = [&]() {
-        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
-        if (++at == per_segment) {
-            at = 0;
-            if (++seg < p.segments) enter();
-        } else {
-            rp += rstep;
-            fp += fstep;
-            if constexpr (S::DUAL) fp2 += fstep;
+    const auto next_f = [&]() {
+        fslot = fslot + 1 == S::SF ? 0 : fslot + 1;
+        ++fat;
+        fp += fstep;
+        if constexpr (S::DUAL) fp2 += fstep;
+    };
+    const auto advance_r = [&]() {
+        next_r();
+        if (rat == per_segment) {
+            rat = 0;
+            if (++rseg < p.segments) enter_r();
+        }
+    };
+    const auto advance_f = [&]() {
+        next_f();
+        if (fat == per_segment) {
+            fat = 0;
+            if (++fseg < p.segments) enter_f();
         }
     };
     typedef typename FragmentReader<S::RL, S::BR, S::E4M3>::frag frag;
     frag rf[2][S::TR], ff[2][S::TF];
-    // fragment i of quarter ks, in the order of their first use: the first features', all rows', the other features'
-    const auto read = [&](int set, const char *image, int ks, int i) {
-        if (i >= 1 && i <= S::TR) rf[set][i - 1] = rr.read(image, i - 1, ks);
+    // fragment i of quarter ks of the step in the rings' present images, in the order of their first use: the first features', all
+    // rows', the other features'
+    int rcur = 0, fcur = 0;
+    const auto read = [&](int set, int ks, int i) {
+        const char *rimage = lds + rcur * S::R_BYTES, *fimage = lds + S::SR * S::R_BYTES + fcur * S::F_BYTES;
+        if (i >= 1 && i <= S::TR) rf[set][i - 1] = rr.read(rimage, i - 1, ks);
         else {
             const int t = i == 0 ? 0 : i - S::TR;
-            ff[set][t] = fr.read(image + RI::BYTES + (t / S::FT) * FI::BYTES, t % S::FT, ks);
+            ff[set][t] = fr.read(fimage + (t / S::FT) * FI::BYTES, t % S::FT, ks);
         }
     };
     const auto multiply = [&](int set, int m) {
@@ -247,11 +265,11 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
         else
             acc[t][u] = mfma_bf16(ff[set][t], rf[set][u], acc[t][u]);
     };
-    // One quarter: its matrix instructions, with the reads of the next quarter and the requests [from, to) of a later step between them.
+    // One quarter: its matrix instructions, with the reads of the next quarter and the requests [FROM, TO) of a later step between them.
     // A wavefront issues in order, and one that asks for several kilobytes in a row stands still until the memory pipeline has taken
     // them: each request has its own place.
     constexpr int NM = S::TR * S::TF, NF = S::TR + S::TF;
-    const auto quarter = [&](int set, auto reads, const char *next, int next_ks, auto tail, auto from, auto to, int left) {
+    const auto quarter = [&](int set, auto reads, int next_ks, auto tail, auto from, auto to, int rleft, int fleft) {
         constexpr bool READS = decltype(reads)::value;
         constexpr int FROM = decltype(from)::value, TO = decltype(to)::value;
         for_range<0, NM>([&](auto mm) {
@@ -259,65 +277,73 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
             multiply(set, M);
             if constexpr (READS)
 #pragma unroll
-                for (int i = M * NF / NM; i < (M + 1) * NF / NM; ++i) read(set ^ 1, next, next_ks, i);
-            pieces(tail, Int<FROM + M *(TO - FROM) / NM>(), Int<FROM + (M + 1) * (TO - FROM) / NM>(), left);
+                for (int i = M * NF / NM; i < (M + 1) * NF / NM; ++i) read(set ^ 1, next_ks, i);
+            pieces(tail, Int<FROM + M *(TO - FROM) / NM>(), Int<FROM + (M + 1) * (TO - FROM) / NM>(), rleft, fleft);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    // The last quarter of one step and all but the last of the next one, whose image is `image`, with the requests of a later one:
-    // of how many kilobytes, and whether it is the last of its segment.
-    const auto step = [&](auto tail, auto loads, const char *image, int left) {
-        constexpr int LOADS = decltype(loads)::value;
+    // Behind a barrier: the last quarter of one step and all but the last of the next one, with the requests: the features' (needed first)
+    // in the first quarter, the rows' in the later ones.  LOADS: how many of them (0, the features', all).
+    const auto step = [&](auto tail, auto loads) {
+        rcur = rcur + 1 == S::SR ? 0 : rcur + 1;
+        fcur = fcur + 1 == S::SF ? 0 : fcur + 1;
+        const int rleft = p.K - 128 * rat, fleft = p.K - 128 * fat;
         for_range<0, S::KS>([&](auto qq) {
-            constexpr int Q = decltype(qq)::value, A = Q < S::SPREAD ? Q : S::SPREAD, Z = Q + 1 < S::SPREAD ? Q + 1 : S::SPREAD;
-            quarter((Q + S::KS - 1) & 1, std::true_type(), image, Q, tail, Int<A * LOADS / S::SPREAD>(), Int<Z * LOADS / S::SPREAD>(), left);
+            constexpr int Q = decltype(qq)::value, F = S::F_LOADS, R = decltype(loads)::value - F;
+            constexpr auto upto = [](int q) { return R + F == 0 || q == 0 ? 0 : F + R * (q - 1) / (S::KS - 1); };
+            quarter((Q + S::KS - 1) & 1, std::true_type(), Q, tail, Int<upto(Q)>(), Int<upto(Q + 1)>(), rleft, fleft);
         });
     };
     constexpr Int<0> none = {};
-    constexpr Int<S::LOADS> all = {};
+    constexpr Int<S::F_LOADS> features = {};
+    constexpr Int<S::F_LOADS + S::R_LOADS> all = {};
+    // What may be on its way at a step's barrier: all that was requested after the next step's images.
+    constexpr int IN_FLIGHT = (S::SF - 2) * (S::R_LOADS + S::F_LOADS) + (S::SR - S::SF) * S::R_LOADS;
 
-    for (int i = 0; i < S::STAGES && i < n; ++i) {
-        pieces(std::true_type(), none, all, p.K - 128 * at);
-        advance();
+    for (int i = 0; i < S::SF && i < n; ++i) {
+        pieces(std::true_type(), none, all, p.K - 128 * rat, p.K - 128 * fat);
+        advance_r();
+        advance_f();
     }
-    if (n >= S::STAGES) wait_loads_and_barrier<S::LOADS *(S::STAGES - 1)>();
+    if (S::SR > S::SF && n >= S::SR) {
+        pieces(std::true_type(), features, all, p.K - 128 * rat, 0);
+        advance_r();
+    }
+    if (n >= S::SR) wait_loads_and_barrier<IN_FLIGHT + S::R_LOADS + S::F_LOADS>();
     else wait_loads_and_barrier<0>();
 #pragma unroll
-    for (int i = 0; i < NF; ++i) read(0, lds, 0, i);
+    for (int i = 0; i < NF; ++i) read(0, 0, i);
 #pragma unroll
-    for (int q = 0; q + 1 < S::KS; ++q) quarter(q & 1, std::true_type(), lds, q + 1, std::false_type(), none, none, 0);
-    int cur = 0, todo = n - S::STAGES;   // steps to request
-    const auto next_image = [&]() {
-        cur = cur + 1 == S::STAGES ? 0 : cur + 1;
-        return lds + cur * S::STAGE_BYTES;
-    };
-    // (the newest STAGES - 2 steps' requests may be on their way still)
+    for (int q = 0; q + 1 < S::KS; ++q) quarter(q & 1, std::true_type(), q + 1, std::false_type(), none, none, 0, 0);
+    int todo = n - S::SR;   // steps that request both operands
     const auto whole_steps = [&](int count) {
-        at += count > 0 ? count : 0;
         for (; count > 0; --count) {
-            wait_loads_and_barrier<S::LOADS *(S::STAGES - 2)>();
-            step(std::false_type(), all, next_image(), 0);
-            slot = slot + 1 == S::STAGES ? 0 : slot + 1;
-            rp += rstep;
-            fp += fstep;
-            if constexpr (S::DUAL) fp2 += fstep;
+            wait_loads_and_barrier<IN_FLIGHT>();
+            step(std::false_type(), all);
+            next_r();
+            next_f();
         }
     };
-    while (todo >= per_segment - at) {   // the rest of a segment: its whole steps, then its last
-        todo -= per_segment - at;
-        whole_steps(per_segment - at - 1);
-        wait_loads_and_barrier<S::LOADS *(S::STAGES - 2)>();
-        step(std::true_type(), all, next_image(), p.K - 128 * at);
-        advance();
+    const auto until_last = [&]() { return per_segment - 1 - (rat > fat ? rat : fat); };   // of either operand's segment
+    for (int c; c = until_last(), c < todo;) {
+        whole_steps(c);
+        wait_loads_and_barrier<IN_FLIGHT>();
+        step(std::true_type(), all);
+        advance_r();
+        advance_f();
+        todo -= c + 1;
     }
     whole_steps(todo);
-    for (int s = (n < S::STAGES ? n : S::STAGES) - 1; s > 0; --s) {
-        wait_loads_and_barrier<0>();
-        step(std::false_type(), none, next_image(), 0);
+    if (S::SR > S::SF && n >= S::SR) {   // the features' last step
+        wait_loads_and_barrier<IN_FLIGHT>();
+        step(std::true_type(), features);
     }
-    quarter((S::KS - 1) & 1, std::false_type(), lds, 0, std::false_type(), none, none, 0);
-    // (the caller may use the LDS once every wavefront is past its last read: the barrier of the last step, or this one's)
-    if (n == 1) lds_barrier();
+    for (int s = n < S::SF ? n - 1 : S::SF - 1; s > 0; --s) {
+        wait_loads_and_barrier<0>();
+        step(std::false_type(), none);
+    }
+    lds_barrier();   // every wavefront is past its last read: the caller may use the LDS
+    quarter((S::KS - 1) & 1, std::false_type(), 0, std::false_type(), none, none, 0, 0);
 }
 
 // Which tile and share of the contraction a block has: blocks of one XCD (blockIdx % 8) take consecutive tiles, in groups of eight row
