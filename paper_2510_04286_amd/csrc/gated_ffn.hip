@@ -187,30 +187,17 @@ __device__ __forceinline__ void share_of(const GemmProblem &p, int split, int &s
     s1 = s0 + each < steps ? s0 + each : steps;
 }
 
-// Both projections and the gate.  SHARE: the raw sums of a share of the contraction instead, part[split][2][rows][ld] in fp32.
-template <typename S, int TERMS, bool SHARE>
-__global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, Scales sc, float *__restrict__ part)
+// Both projections and the gate.
+template <typename S, int TERMS>
+__global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, Scales sc)
 {
     extern __shared__ __align__(1024) char lds[];
     const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, p.splits);
     const int row0 = at.r * S::BR, f0 = at.f * S::BF, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     f32x16 acc[S::TF][S::TR];
     clear<S>(acc);
-    int s0, s1;
-    share_of(p, at.split, s0, s1);
-    mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
+    mma_steps<S>(acc, p, row0, f0, 0, p.segments * ((p.K + 127) >> 7), lds);
     const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
-    if constexpr (SHARE) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const Out o = {part + (size_t)(2 * at.split + m) * h.rows * h.ld, nullptr, h.rows, h.ld, 1};
-#pragma unroll
-            for (int u = 0; u < S::TR; ++u)
-                store_rows<S::FT>(lds, [&](int t) { return acc[m * S::FT + t][u]; },
-                                  [&](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); });
-        }
-        return;
-    }
 #pragma unroll
     for (int u = 0; u < S::TR; ++u) {
         float sx = 1.f;
@@ -237,41 +224,28 @@ __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, 
     }
 }
 
-// a from the shares' sums of both projections.
-template <int TERMS, bool E4M3>
-__global__ __launch_bounds__(256) void gated_up_sum_kernel(const float *__restrict__ part, Hidden h, Scales sc, int splits)
+// The same for few rows.
+template <typename S, int TERMS> __global__ __launch_bounds__(256) void gated_up_few_kernel(GemmProblem p, Hidden h, Scales sc)
 {
-    const int per_row = (h.cols + 7) / 8;
-    const long long n = (long long)h.rows * per_row;
-    const size_t one = (size_t)h.rows * h.ld;
-    for (long long k = (long long)blockIdx.x * 256 + threadIdx.x; k < n; k += (long long)gridDim.x * 256) {
-        const int row = (int)(k / per_row), col = (int)(k - (long long)row * per_row) * 8;
-        float g[8], u[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = u[i] = 0.f;
-        const float *q = part + (size_t)row * h.ld + col;
-        for (int s = 0; s < splits; ++s, q += 2 * one) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f32x4 a = *(const f32x4 *)(q + 4 * i), b = *(const f32x4 *)(q + one + 4 * i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    g[4 * i + e] += a[e];
-                    u[4 * i + e] += b[e];
-                }
-            }
-        }
+    extern __shared__ __align__(1024) char lds[];
+    const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, 1);
+    const int row0 = at.r * S::BR, f0 = at.f * S::BF;
+    few_rows<S>(p, row0, f0, 0, p.segments * ((p.K + 127) >> 7), lds, [&](int r, int c, const float (&v)[2][8]) {
+        const int row = row0 + r, col = f0 + c;
+        if (row >= h.rows) return;
+        float a[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (E4M3) {
-                const int c = col + i < h.cols ? col + i : h.cols - 1;
-                g[i] *= sc.x[row] * sc.g[c];
-                u[i] *= sc.x[row] * sc.u[c];
+            float g = v[0][i], u = v[1][i];
+            if constexpr (S::E4M3) {
+                const int k = col + i < h.cols ? col + i : h.cols - 1;
+                g *= sc.x[row] * sc.g[k];
+                u *= sc.x[row] * sc.u[k];
             }
-            g[i] = g[i] * sigmoid<TERMS == 3>(g[i]) * u[i];
+            a[i] = g * sigmoid<TERMS == 3>(g) * u;
         }
-        put_hidden<TERMS>(h, 0, row, col, g);
-    }
+        put_hidden<TERMS>(h, 0, row, col, a);
+    });
 }
 
 // Up to three products in one launch, into their outputs or, with a split contraction, into fp32 shares.
@@ -305,24 +279,58 @@ template <typename S> __global__ __launch_bounds__(256) void gated_product_kerne
         store_rows<S::TF>(lds, [&](int t) { return acc[t][u]; }, [&](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); });
 }
 
-__global__ __launch_bounds__(256) void gated_sum_kernel(Products ps)
+template <typename S> __global__ __launch_bounds__(256) void gated_product_few_kernel(Products ps)
 {
-    const int k = blockIdx.y;
+    extern __shared__ __align__(1024) char lds[];
+    const GemmProblem &p = ps.p[0];
+    const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, p.splits);
+    const int row0 = at.r * S::BR, f0 = at.f * S::BF;
+    int s0, s1;
+    share_of(p, at.split, s0, s1);
+    Out o = ps.out[0];
+    if (ps.part[0]) {
+        const int ld = (o.cols + 7) & ~7;
+        o = {ps.part[0] + (size_t)at.split * o.rows * ld, nullptr, o.rows, ld, 1};
+    }
+    few_rows<S>(p, row0, f0, s0, s1, lds, [&](int r, int c, const float (&v)[1][8]) { put_out(o, row0 + r, f0 + c, v[0]); });
+}
+
+// The shares' sums, in their order within each of GROUPS groups (neighbours in a block; more of them where there are many shares of few
+// outputs), then the groups'.
+template <int GROUPS> __global__ __launch_bounds__(256) void gated_sum_kernel(Products ps)
+{
+    constexpr int PIECES = 256 / GROUPS;
+    __shared__ float sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? PIECES : 1][8];
+    const int k = blockIdx.y, group = threadIdx.x / PIECES, lane = threadIdx.x % PIECES;
     if (!ps.part[k]) return;
     const Out o = ps.out[k];
     const int per_row = (o.cols + 7) / 8, ld = per_row * 8, splits = ps.p[k].splits;
     const long long n = (long long)o.rows * per_row;
     const size_t one = (size_t)o.rows * ld;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-        const int row = (int)(i / per_row), col = (int)(i - (long long)row * per_row) * 8;
-        const float *q = ps.part[k] + (size_t)row * ld + col;
+    for (long long base = (long long)blockIdx.x * PIECES; base < n; base += (long long)gridDim.x * PIECES) {
+        const long long i = base + lane;
+        const bool there = i < n;
+        const int row = there ? (int)(i / per_row) : 0, col = there ? (int)(i - (long long)row * per_row) * 8 : 0;
+        const float *q = ps.part[k] + (size_t)row * ld + col + group * one;
         f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-        for (int s = 0; s < splits; ++s, q += one) {
+        for (int s = group; s < splits; s += GROUPS, q += GROUPS * one) {
             a += *(const f32x4 *)q;
             b += *(const f32x4 *)(q + 4);
         }
+        if constexpr (GROUPS > 1) {
+            __syncthreads();   // the last round's sums have been read
+            *(f32x4 *)&sums[group][lane][0] = a;
+            *(f32x4 *)&sums[group][lane][4] = b;
+            __syncthreads();
+            if (group > 0) continue;
+#pragma unroll
+            for (int g = 1; g < GROUPS; ++g) {
+                a += *(const f32x4 *)&sums[g][lane][0];
+                b += *(const f32x4 *)&sums[g][lane][4];
+            }
+        }
         const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        put_out(o, row, col, v);
+        if (there) put_out(o, row, col, v);
     }
 }
 
@@ -408,26 +416,25 @@ __global__ __launch_bounds__(256) void gated_quantize_kernel(const bf16_t *__res
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
 // Tile shapes.  Big: 256 rows x 256 features (gate and up: 128 of each), one block per CU.  Middle: 128 x 128, two blocks per CU.
-// Small: 32 rows x 128 features for the few rows of a decoding step.
+// For the few rows of a decoding step: see FewShape.
 template <int RL, int FL, bool DUAL, bool E4M3> struct Shapes {
     typedef TileShape<4, 4, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Big;
     typedef TileShape<2, 2, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Middle;
-    typedef TileShape<1, DUAL ? 2 : 1, 1, 4, RL, FL, DUAL, E4M3, 4, 4> Small;
 };
 template <typename S> constexpr int lds_of(int staged_tiles) { return S::LDS > stage_bytes(staged_tiles) ? S::LDS : stage_bytes(staged_tiles); }
 
 static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 static int steps_of(const GemmProblem &p) { return p.segments * ((p.K + 127) >> 7); }
 
-enum TileSize { kBig, kMiddle, kSmall };
+enum TileSize { kBig, kMiddle, kFew };
 // The size of the tiles of nr x nf outputs, and into how many shares a contraction of `steps` steps goes so that the chip is full.
-constexpr int kFewRows = 64;   // up to these many rows of x take the small tiles
+constexpr int kFewRows = 64;   // up to these many rows of x take the kernels for few rows
 struct TileChoice {
     TileSize size;
     int splits;
 };
 // The most that goes into one share: fewer steps than these do not pay for the ring's first round trip and the sums' way through memory.
-constexpr int kSmallShare = 2, kMiddleShare = 4;
+constexpr int kFewShare = 4, kMiddleShare = 4;
 static int shares(long long tiles, long long slots, int steps, int least)
 {
     const int n = (int)std::max<long long>(1, std::min<long long>(slots / std::max(1ll, tiles), steps / least));
@@ -438,7 +445,7 @@ static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual,
     const int cus = num_compute_units();
     const long long f = dual ? 2 : 1;
     const long long big = (long long)ceil_div(nr, 256) * ceil_div(f * nf, 256), mid = (long long)ceil_div(nr, 128) * ceil_div(f * nf, 128);
-    if (nr <= kFewRows) return {kSmall, may_split ? shares((long long)ceil_div(nr, 32) * ceil_div(nf, 128), cus, steps, kSmallShare) : 1};
+    if (nr <= kFewRows) return {kFew, may_split ? shares(ceil_div(nf, 64), cus, steps, kFewShare) : 1};
     if (big * 4 >= 3 * cus) return {kBig, 1};
     return {kMiddle, may_split ? shares(mid, 2 * cus, steps, kMiddleShare) : 1};
 }
@@ -510,11 +517,11 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
     const long long cus = num_compute_units();
     // (tiles reach past the outputs' edges; what is stored ends there, so the outputs bound the bytes of the first kind too)
     const auto rows_shares = [&](int steps) {
-        return std::max(share_bytes(cus, 32 * 128, steps, kSmallShare, few, d8),
+        return std::max(share_bytes(cus, kFewRows * 64, steps, kFewShare, few, d8),
                         T > few ? share_bytes(2 * cus, 128 * 128, steps, kMiddleShare, T, d8) : 0);
     };
     size_t part = 0;
-    if (!backward) part = std::max(share_bytes(cus, 2 * 32 * 128, st.up, kSmallShare, few, 2 * (size_t)p.ldh), rows_shares(st.down));
+    if (!backward) part = rows_shares(st.down);
     else
         part = std::max(rows_shares(st.dx), 3 * 256 + 2 * share_bytes(2 * cus, 128 * 128, st.dwgu, kMiddleShare, d, h8) +
                                                 share_bytes(2 * cus, 128 * 128, st.dwd, kMiddleShare, H, d8));
@@ -585,59 +592,60 @@ static GemmProblem problem(int nr, int nf, long long K, long long ldr, long long
 
 template <typename K> static hipError_t ready(K kernel, int lds) { return grant_dynamic_lds((const void *)kernel, lds); }
 
-template <typename S, int TERMS, bool SHARE>
-static hipError_t run_up(GemmProblem p, const Hidden &h, const Scales &sc, int splits, float *part, hipStream_t s)
+template <typename S, typename KERNEL> static hipError_t run_up(KERNEL kernel, int lds, GemmProblem p, const Hidden &h, const Scales &sc, hipStream_t s)
 {
-    set_tiles<S>(p, splits);
-    constexpr int lds = lds_of<S>(S::FT);
-    const auto kernel = gated_up_kernel<S, TERMS, SHARE>;
+    set_tiles<S>(p, 1);
     const hipError_t e = ready(kernel, lds);
     if (e != hipSuccess) return e;
-    kernel<<<p.tiles_r * p.tiles_f * splits, 256, lds, s>>>(p, h, sc, part);
+    kernel<<<p.tiles_r * p.tiles_f, 256, lds, s>>>(p, h, sc);
     return hipGetLastError();
 }
-template <int FL, bool E4M3, int TERMS>
-static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales &sc, float *part, hipStream_t s)
+template <int FL, bool E4M3, int TERMS> static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales &sc, hipStream_t s)
 {
-    typedef Shapes<kKContiguous, FL, true, E4M3> Sh;
-    const TileChoice t = choose_tiles(p.nr, p.nf, steps_of(p), true, p.nr <= kFewRows);
-    if (t.size == kBig) return run_up<typename Sh::Big, TERMS, false>(p, h, sc, 1, nullptr, s);
-    if (t.size == kMiddle) return run_up<typename Sh::Middle, TERMS, false>(p, h, sc, 1, nullptr, s);
-    if (t.splits == 1) return run_up<typename Sh::Small, TERMS, false>(p, h, sc, 1, nullptr, s);
-    const hipError_t e = run_up<typename Sh::Small, TERMS, true>(p, h, sc, t.splits, part, s);
-    if (e != hipSuccess) return e;
-    const long long n = (long long)h.rows * ((h.cols + 7) / 8);
-    gated_up_sum_kernel<TERMS, E4M3><<<(int)std::min<long long>((n + 255) / 256, 8ll * num_compute_units()), 256, 0, s>>>(part, h, sc, t.splits);
-    return hipGetLastError();
+    typedef typename Shapes<kKContiguous, FL, true, E4M3>::Big Big;
+    typedef typename Shapes<kKContiguous, FL, true, E4M3>::Middle Middle;
+    switch (choose_tiles(p.nr, p.nf, steps_of(p), true, false).size) {
+        case kBig: return run_up<Big>(gated_up_kernel<Big, TERMS>, lds_of<Big>(Big::FT), p, h, sc, s);
+        case kMiddle: return run_up<Middle>(gated_up_kernel<Middle, TERMS>, lds_of<Middle>(Middle::FT), p, h, sc, s);
+        default: break;
+    }
+    const auto few = [&](auto shape) {
+        typedef decltype(shape) S;
+        return run_up<S>(gated_up_few_kernel<S, TERMS>, S::LDS, p, h, sc, s);
+    };
+    const bool many = ceil_div(p.nf, 32) > num_compute_units();
+    if constexpr (E4M3) {
+        if (p.nr <= 32) return many ? few(FewShape<1, 1, FL, true, true, 2>()) : few(FewShape<1, 1, FL, true, true, 1>());
+        return many ? few(FewShape<2, 1, FL, true, true, 2>()) : few(FewShape<2, 1, FL, true, true, 1>());
+    } else {
+        if (p.nr <= 32) return many ? few(FewShape<1, 2, FL, true, false, 1>()) : few(FewShape<1, 1, FL, true, false, 1>());
+        return many ? few(FewShape<2, 2, FL, true, false, 1>()) : few(FewShape<2, 1, FL, true, false, 1>());
+    }
 }
 
-template <typename S> static hipError_t run_products(Products &ps, int n, hipStream_t s)
+template <typename S, typename KERNEL> static hipError_t run_products(KERNEL kernel, int lds, Products &ps, int n, hipStream_t s)
 {
     ps.first[0] = 0;
     for (int i = 0; i < 3; ++i) {
         if (i < n) set_tiles<S>(ps.p[i], ps.p[i].splits);
         ps.first[i + 1] = ps.first[i] + (i < n ? ps.p[i].tiles_r * ps.p[i].tiles_f * ps.p[i].splits : 0);
     }
-    for (int i = n; i < 3; ++i) ps.first[i] = ps.first[n];
-    constexpr int lds = lds_of<S>(S::TF);
-    const auto kernel = gated_product_kernel<S>;
     const hipError_t e = ready(kernel, lds);
     if (e != hipSuccess) return e;
     kernel<<<ps.first[n], 256, lds, s>>>(ps);
     return hipGetLastError();
 }
-// n products of one tile size; part: room for the shares.
+// n products of one tile size (few rows: one product, R K-contiguous); part: room for the shares.
 template <int RL, int FL> static hipError_t launch_products(Products &ps, int n, TileChoice t, char *part, hipStream_t s)
 {
-    typedef Shapes<RL, FL, false, false> Sh;
-    bool split = false;
+    typedef typename Shapes<RL, FL, false, false>::Big Big;
+    typedef typename Shapes<RL, FL, false, false>::Middle Middle;
     long long most = 0;
     size_t at = 0;
     for (int i = 0; i < n; ++i) {
         ps.p[i].splits = t.splits;
         ps.part[i] = nullptr;
         if (t.splits == 1) continue;
-        split = true;
         const long long pieces = (long long)ps.out[i].rows * ((ps.out[i].cols + 7) / 8);
         ps.part[i] = (float *)(part + at);
         at = align_up(at + (size_t)t.splits * pieces * 32, 256);
@@ -645,13 +653,18 @@ template <int RL, int FL> static hipError_t launch_products(Products &ps, int n,
     }
     for (int i = n; i < 3; ++i) ps.part[i] = nullptr;
     hipError_t e;
-    switch (t.size) {
-        case kBig: e = run_products<typename Sh::Big>(ps, n, s); break;
-        case kMiddle: e = run_products<typename Sh::Middle>(ps, n, s); break;
-        default: e = run_products<typename Sh::Small>(ps, n, s); break;
-    }
-    if (e != hipSuccess || !split) return e;
-    gated_sum_kernel<<<dim3((int)std::min<long long>((most + 255) / 256, 8ll * num_compute_units()), n), 256, 0, s>>>(ps);
+    if (t.size == kBig) e = run_products<Big>(gated_product_kernel<Big>, lds_of<Big>(Big::TF), ps, n, s);
+    else if (t.size == kMiddle) e = run_products<Middle>(gated_product_kernel<Middle>, lds_of<Middle>(Middle::TF), ps, n, s);
+    else if constexpr (RL == kKContiguous) {
+        typedef FewShape<1, 2, FL, false, false, 1> One;
+        typedef FewShape<2, 2, FL, false, false, 1> Two;
+        e = ps.p[0].nr <= 32 ? run_products<One>(gated_product_few_kernel<One>, One::LDS, ps, n, s)
+                             : run_products<Two>(gated_product_few_kernel<Two>, Two::LDS, ps, n, s);
+    } else
+        e = hipErrorInvalidValue;
+    if (e != hipSuccess || t.splits == 1) return e;
+    if (t.splits >= 4) gated_sum_kernel<8><<<dim3((int)std::min<long long>((most + 31) / 32, 16ll * num_compute_units()), n), 256, 0, s>>>(ps);
+    else gated_sum_kernel<1><<<dim3((int)std::min<long long>((most + 255) / 256, 8ll * num_compute_units()), n), 256, 0, s>>>(ps);
     return hipGetLastError();
 }
 
@@ -680,8 +693,7 @@ hipError_t launch_gated_ffn(const slicemoe_gated_config &c, const GatedPlan &pla
     GemmProblem p = problem(c.T, c.H, 2ll * c.d, o.ldx, o.ldw);
     add_segments(p, plan.terms, o.x, o.tx, o.Wg, o.tw, o.Wu);
     const Hidden h = hidden_of(c, plan, ws);
-    float *part = (float *)(ws + plan.part);
-    e = plan.terms == 1 ? launch_up<kKMajor, false, 1>(p, h, Scales(), part, s) : launch_up<kKMajor, false, 3>(p, h, Scales(), part, s);
+    e = plan.terms == 1 ? launch_up<kKMajor, false, 1>(p, h, Scales(), s) : launch_up<kKMajor, false, 3>(p, h, Scales(), s);
     if (e != hipSuccess) return e;
     return launch_down(c, plan, o.Wd, o.twd, o.ldwd, addend, y, ws, s);
 }
@@ -696,7 +708,7 @@ hipError_t launch_gated_ffn_quantized(const slicemoe_gated_config &c, const Gate
     if (e != hipSuccess) return e;
     GemmProblem p = problem(c.T, c.H, c.d, c.d, c.d);
     add_segments(p, 1, (const char *)x, 0, (const char *)w.Wg, 0, (const char *)w.Wu);
-    e = launch_up<kKContiguous, true, 1>(p, hidden_of(c, plan, ws), Scales{x_scale, w.Wg_scale, w.Wu_scale}, (float *)(ws + plan.part), s);
+    e = launch_up<kKContiguous, true, 1>(p, hidden_of(c, plan, ws), Scales{x_scale, w.Wg_scale, w.Wu_scale}, s);
     if (e != hipSuccess) return e;
     return launch_down(c, plan, o.Wd, o.twd, o.ldwd, addend, y, ws, s);
 }

@@ -74,10 +74,10 @@ template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// The image of one operand: N rows of the tile (a multiple of 32).  Wavefront w fills the kilobytes PER_WAVE w + i, four of them (or
-// all) from one LDS target.
-template <int LAYOUT, int N> struct TileImage {
-    static constexpr int BYTES = N * 128, PER_WAVE = N / 32;
+// The image of one operand: N rows of the tile (a multiple of 32), filled by WAVES wavefronts.  Wavefront w has the kilobytes
+// PER_WAVE w + i, four of them (or all) from one LDS target.
+template <int LAYOUT, int N, int WAVES> struct TileImage {
+    static constexpr int BYTES = N * 128, PER_WAVE = N / 8 / WAVES;
     static constexpr int K_PER_PIECE = 512 / N;   // rows of k per kilobyte (K-major)
     static constexpr int BIAS = 3072;             // what the instruction's own offset adds at most is taken off the base, added to the offsets
     static __device__ __forceinline__ int block_swizzle(int k) { return N >= 128 ? k & 3 : N == 64 ? k >> 1 & 1 : 0; }
@@ -137,7 +137,7 @@ template <int LAYOUT, int N, bool E4M3> struct FragmentReader {
             const int q = lane >> 2 & 3;   // which of four k this lane fetches
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                base[t] = (8 * g + q) * (2 * N) + (((wb + t) ^ TileImage<LAYOUT, N>::block_swizzle(q)) & (N / 32 - 1)) * 64 + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
+                base[t] = (8 * g + q) * (2 * N) + (((wb + t) ^ TileImage<LAYOUT, N, 1>::block_swizzle(q)) & (N / 32 - 1)) * 64 + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
         }
     }
     __device__ __forceinline__ frag read(const char *image, int t, int ks) const
@@ -169,8 +169,8 @@ template <int TR_, int TF_, int WR_, int WF_, int RL_, int FL_, bool DUAL_, bool
     static_assert(SF >= 2 && (SR == SF || SR == SF + 1), "see the waits");
     static constexpr int IMAGES = DUAL ? 2 : 1, FT = TF / IMAGES;   // feature tiles per image and wavefront
     static constexpr int BR = 32 * TR * WR, BF = 32 * FT * WF;      // rows, features (of one image) per block
-    typedef TileImage<RL, BR> RI;
-    typedef TileImage<FL, BF> FI;
+    typedef TileImage<RL, BR, 4> RI;
+    typedef TileImage<FL, BF, 4> FI;
     static constexpr int R_BYTES = RI::BYTES, F_BYTES = IMAGES * FI::BYTES;
     static constexpr int R_LOADS = RI::PER_WAVE, F_LOADS = IMAGES * FI::PER_WAVE;   // instructions per wavefront and step
     static constexpr int LDS = SR * R_BYTES + SF * F_BYTES;
@@ -344,6 +344,138 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
     }
     lds_barrier();   // every wavefront is past its last read: the caller may use the LDS
     quarter((S::KS - 1) & 1, std::false_type(), 0, std::false_type(), none, none, 0, 0);
+}
+
+// Few rows: a tile of 32 TR rows and 32 FT features (of one or two images) per block, each wavefront with every fourth step of the
+// contraction, images and a ring of SLOTS of its own: no barrier, and as much of the weights in flight as the LDS holds.
+template <int TR_, int FT_, int FL_, bool DUAL_, bool E4M3_, int BLOCKS> struct FewShape {
+    static constexpr int TR = TR_, FT = FT_, FL = FL_, IMAGES = DUAL_ ? 2 : 1, KS = E4M3_ ? 2 : 4;
+    static constexpr bool DUAL = DUAL_, E4M3 = E4M3_;
+    static constexpr int BR = 32 * TR, BF = 32 * FT;
+    typedef TileImage<kKContiguous, BR, 1> RI;
+    typedef TileImage<FL, BF, 1> FI;
+    static constexpr int SLOT = RI::BYTES + IMAGES * FI::BYTES, LOADS = RI::PER_WAVE + IMAGES * FI::PER_WAVE;
+    static constexpr int FIT = 160 * 1024 / (4 * SLOT * BLOCKS), SLOTS = FIT < 4 ? FIT : 4;   // BLOCKS: per CU
+    static_assert(SLOTS >= 1 && LOADS * (SLOTS - 1) < 64, "the wait counts to 63");
+    static constexpr int STRIDE = BF + 4;                                    // floats of a row in the sums
+    static constexpr int SUMS = 4 * IMAGES * BR * STRIDE * 4;
+    static constexpr int LDS = 4 * SLOTS * SLOT > SUMS ? 4 * SLOTS * SLOT : SUMS;
+};
+
+// put(row of the tile, feature of the tile, eight values for each image) for the steps [s0, s1), the wavefronts' sums added in their order.
+template <typename S, typename PUT> __device__ __forceinline__ void few_rows(const GemmProblem &p, int row0, int f0, int s0, int s1, char *lds, const PUT &put)
+{
+    typedef typename S::RI RI;
+    typedef typename S::FI FI;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int NT = S::IMAGES * S::FT;   // feature tiles: those of the first image, then those of the second
+    f32x16 acc[NT][S::TR];
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int u = 0; u < S::TR; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][u][i] = 0.f;
+
+    const int n = (s1 - s0 - wave + 3) >> 2;   // this wavefront's steps (none: <= 0)
+    char *mine = lds + wave * S::SLOTS * S::SLOT;
+    const uint32_t mine0 = (uint32_t)(uintptr_t)as_lds(mine);
+    uint32_t ro[RI::PER_WAVE], fo[FI::PER_WAVE];
+    RI::offsets(ro, 0, lane, row0, p.nr, (uint32_t)p.ldr);
+    FI::offsets(fo, 0, lane, f0, p.nf, (uint32_t)p.ldf);
+    FragmentReader<kKContiguous, S::BR, S::E4M3> rr;
+    FragmentReader<S::FL, S::BF, S::E4M3> fr;
+    rr.init(0, lane);
+    fr.init(0, lane);
+    const int per_segment = (p.K + 127) >> 7;
+    int seg = (s0 + wave) / per_segment, at = s0 + wave - seg * per_segment, slot = 0;
+    const char *rp, *fp, *fp2 = nullptr;   // of the segment
+    const auto enter = [&]() {
+        rp = RI::corner(p.r[seg], row0, p.ldr);
+        fp = FI::corner(p.f[seg], f0, p.ldf);
+        if constexpr (S::DUAL) fp2 = FI::corner(p.f2[seg], f0, p.ldf);
+    };
+    if (n > 0) enter();
+    const uint64_t rstep = RI::step_bytes(p.ldr), fstep = FI::step_bytes(p.ldf);
+    const int segments = p.segments, K = p.K;
+    const auto request = [&]() {
+        const int left = K - 128 * at;
+        const uint32_t to = mine0 + slot * S::SLOT;
+        for_range<0, RI::PER_WAVE>([&](auto i) { RI::template request<true, decltype(i)::value>(to, rp + at * rstep, ro, 0, lane, left); });
+        for_range<0, FI::PER_WAVE>([&](auto i) { FI::template request<true, decltype(i)::value>(to + RI::BYTES, fp + at * fstep, fo, 0, lane, left); });
+        if constexpr (S::DUAL)
+            for_range<0, FI::PER_WAVE>([&](auto i) { FI::template request<true, decltype(i)::value>(to + RI::BYTES + FI::BYTES, fp2 + at * fstep, fo, 0, lane, left); });
+        slot = slot + 1 == S::SLOTS ? 0 : slot + 1;
+        at += 4;
+        if (at >= per_segment) {
+            do {
+                at -= per_segment;
+                ++seg;
+            } while (at >= per_segment);
+            if (seg < segments) enter();
+        }
+    };
+    for (int i = 0; i < S::SLOTS && i < n; ++i) request();
+    int cur = 0;
+    for (int j = 0; j < n; ++j) {
+        if (j + S::SLOTS <= n) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(S::LOADS *(S::SLOTS - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const char *image = mine + cur * S::SLOT;
+        cur = cur + 1 == S::SLOTS ? 0 : cur + 1;
+        typename FragmentReader<S::FL, S::BF, S::E4M3>::frag rf[S::KS][S::TR], ff[S::KS][NT];
+#pragma unroll
+        for (int k = 0; k < S::KS; ++k) {
+#pragma unroll
+            for (int u = 0; u < S::TR; ++u) rf[k][u] = rr.read(image, u, k);
+#pragma unroll
+            for (int m = 0; m < NT; ++m) ff[k][m] = fr.read(image + RI::BYTES + m / S::FT * FI::BYTES, m % S::FT, k);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the image is in registers: its place is free
+        if (j + S::SLOTS < n) request();
+#pragma unroll
+        for (int k = 0; k < S::KS; ++k)
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int u = 0; u < S::TR; ++u) {
+                    if constexpr (S::E4M3)
+                        acc[m][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ff[k][m], rf[k][u], acc[m][u], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+                    else
+                        acc[m][u] = mfma_bf16(ff[k][m], rf[k][u], acc[m][u]);
+                }
+    }
+    lds_barrier();   // every wavefront is done with its images
+    float *sums = (float *)lds;
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int u = 0; u < S::TR; ++u)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(f32x4 *)(sums + ((wave * S::IMAGES + m / S::FT) * S::BR + 32 * u + (lane & 31)) * S::STRIDE + 32 * (m % S::FT) + 8 * q + 4 * (lane >> 5)) =
+                    f32x4{acc[m][u][4 * q], acc[m][u][4 * q + 1], acc[m][u][4 * q + 2], acc[m][u][4 * q + 3]};
+    lds_barrier();
+    constexpr int PIECES = S::BF / 8;   // eight features of a row per thread
+    for (int i = tid; i < PIECES * S::BR; i += 256) {
+        const int row = i / PIECES, col = 8 * (i % PIECES);
+        float v[S::IMAGES][8];
+#pragma unroll
+        for (int m = 0; m < S::IMAGES; ++m) {
+            f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float *q = sums + ((w * S::IMAGES + m) * S::BR + row) * S::STRIDE + col;
+                a += *(const f32x4 *)q;
+                b += *(const f32x4 *)(q + 4);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[m][e] = a[e];
+                v[m][4 + e] = b[e];
+            }
+        }
+        put(row, col, v);
+    }
 }
 
 // Which tile and share of the contraction a block has: blocks of one XCD (blockIdx % 8) take consecutive tiles, in groups of eight row

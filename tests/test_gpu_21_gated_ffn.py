@@ -76,3 +76,27 @@ def test_large_tiles_fp32(B):
 def test_without_addends(B):
     run(B, 77, 96, 200, B16, addend=False)
     run(B, 300, 257, 200, F32, addend=False)
+
+
+@pytest.mark.parametrize("T,d,H", [(1, 16, 1), (1, 128, 64), (5, 48, 33), (16, 4096, 200), (32, 256, 768), (33, 272, 100), (64, 1024, 2816),
+                                   (65, 128, 130), (200, 400, 1000), (257, 2048, 96), (4100, 512, 2056)])
+def test_eight_bits(B, T, d, H):
+    cfg = B.make_gated_config(T, d, H, "bf16")
+    w = weights(d, H, B16)
+    w["Wg"][:, 0] = 0
+    q = B.quantize_gated_weights(cfg, w)
+    for n in ("Wg", "Wu"):   # one rounding to e4m3 of w / scale, scale = largest of the column / 448
+        top = w[n].double().abs().amax(0).clamp_min(1e-30)
+        R.within(q[n + "_scale"], top / 448, (top / 448) * (4 * R.U), n + "_scale")
+        step = torch.maximum(2.0 ** -4 * w[n].double().abs(), 2.0 ** -10 * (top / 448)) * (1 + 2.0 ** -10)
+        R.within((q[n].float().double() * q[n + "_scale"].double()[:, None]).t(), w[n].double(), step, n)
+    x, add = tensor((T, d), 5, 1.0, B16), tensor((T, d), 6, 1.0, B16)
+    ncfg = B.make_norm_config(T, d, 1e-5, "bf16")
+    xq, xs = torch.empty((T, d), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(T, device="cuda")
+    B.slicemoe_add_rmsnorm(ncfg, x, None, torch.ones(d, dtype=B16, device="cuda"), None, None, y_quantized=xq, y_scale=xs)
+    for addend in (add, None):
+        y = torch.full((T, d), 7.0, dtype=B16, device="cuda")
+        B.slicemoe_gated_ffn_quantized(cfg, xq, xs, q, y, space(B.slicemoe_gated_ffn_quantized_workspace_bytes(cfg)), addend=addend)
+        v, e = R.gated_quantized(xq, xs, q, addend)
+        R.within(y, v, e, "y")
+        assert float((y.double() - v).norm()) <= 3 * 2.0 ** -8 * float(v.norm())
