@@ -176,51 +176,81 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_kernel(const
     }
 }
 
+// Two sums over the W wavefronts that own a row, in one exchange.  flip: alternates from row to row, so that one barrier per row does.
+template <int W> __device__ __forceinline__ void row_sums(float &a, float &b, float (*lds)[2 * W], int flip)
+{
+    a = wavefront_sum_f32(a);
+    b = wavefront_sum_f32(b);
+    if constexpr (W == 1) return;
+    float *l = lds[flip];
+    if ((threadIdx.x & 63) == 0) {
+        l[threadIdx.x >> 6] = a;
+        l[W + (threadIdx.x >> 6)] = b;
+    }
+    lds_barrier();   // (the next row's loads stay on their way)
+    a = b = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        a += l[i];
+        b += l[W + i];
+    }
+}
+
 // Block b takes the rows b, b + gridDim.x, .. (W = 1: its four wavefronts the row groups), so that a block's share differs by
-// at most one row (group).  part[b][d]: its column sums of dy n.
+// at most one row (group).  A row's pieces are requested while the row before it is worked on.  part[b][d]: its column sums of dy n.
 template <typename T, bool ALIGNED, int W, int NP>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_backward_kernel(
-    const T *__restrict__ sum, const T *__restrict__ w, const T *__restrict__ dy, const T *__restrict__ dsum, T *__restrict__ dx,
-    float *__restrict__ part, int rows, int d, float eps)
+    const T *__restrict__ sum, const T *__restrict__ w, const T *dy, const T *dsum, T *dx, float *__restrict__ part, int rows, int d, float eps)
 {
     constexpr int V = RowPiece<T>::V, LANES = 64 * W, ROWS = W == 1 ? 4 : 1;
-    __shared__ float lds[2 * W];
+    __shared__ float lds[2][2 * W];
     __shared__ float cols[W == 1 ? 3 : 1][W == 1 ? 64 * V : 1];
     const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, wave = threadIdx.x >> 6;
-    u32x4 pw[NP];
+    u32x4 pw[NP], ps[NP], pg[NP], pd[NP];
     float acc[NP][V];
-#pragma unroll
-    for (int c = 0; c < NP; ++c) {
-        const int at = (lane + c * LANES) * V;
-        pw[c] = load_piece<T, ALIGNED>(w, at, d);
-#pragma unroll
-        for (int i = 0; i < V; ++i) acc[c][i] = 0.f;
-    }
-    const float inv_d = 1.f / d;
-    for (long long row = (long long)blockIdx.x * ROWS + (W == 1 ? wave : 0); row < rows; row += (long long)gridDim.x * ROWS) {
+    const auto request = [&](long long row) {
         const size_t at0 = (size_t)row * d;
-        u32x4 ps[NP], pg[NP], pd[NP];
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
             const int at = (lane + c * LANES) * V;
             ps[c] = load_piece<T, ALIGNED>(sum + at0, at, d);
             pg[c] = load_piece<T, ALIGNED>(dy + at0, at, d);
-            pd[c] = u32x4{0, 0, 0, 0};
         }
         if (dsum)
 #pragma unroll
             for (int c = 0; c < NP; ++c) pd[c] = load_piece<T, ALIGNED>(dsum + at0, (lane + c * LANES) * V, d);
+    };
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+        pw[c] = load_piece<T, ALIGNED>(w, (lane + c * LANES) * V, d);
+        pd[c] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[c][i] = 0.f;
+    }
+    const float inv_d = 1.f / d;
+    const long long stride = (long long)gridDim.x * ROWS;
+    long long row = (long long)blockIdx.x * ROWS + (W == 1 ? wave : 0);
+    constexpr bool AHEAD = W < 16 && NP < 8;   // (where the registers hold two rows)
+    if (AHEAD && row < rows) request(row);
+    int flip = 0;
+    for (; row < rows; row += stride, flip ^= 1) {
+        if (!AHEAD) request(row);
+        u32x4 cs[NP], cg[NP], cd[NP];
         float ss = 0.f, along = 0.f;
 #pragma unroll
-        for (int c = 0; c < NP; ++c)
+        for (int c = 0; c < NP; ++c) {
+            cs[c] = ps[c];
+            cg[c] = pg[c];
+            cd[c] = pd[c];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float s = RowPiece<T>::get(ps[c], i);
+                const float s = RowPiece<T>::get(cs[c], i);
                 ss += s * s;
-                along += RowPiece<T>::get(pg[c], i) * RowPiece<T>::get(pw[c], i) * s;
+                along += RowPiece<T>::get(cg[c], i) * RowPiece<T>::get(pw[c], i) * s;
             }
-        ss = row_sum<W>(ss, lds);
-        along = row_sum<W>(along, lds + W);
+        }
+        if (AHEAD && row + stride < rows) request(row + stride);
+        row_sums<W>(ss, along, lds, flip);
         const float r = 1.f / sqrtf(ss * inv_d + eps);
         const float k = along * r * inv_d;   // mean(m n)
 #pragma unroll
@@ -229,11 +259,11 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_backward_ker
             float v[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float n = RowPiece<T>::get(ps[c], i) * r, g = RowPiece<T>::get(pg[c], i);
+                const float n = RowPiece<T>::get(cs[c], i) * r, g = RowPiece<T>::get(cg[c], i);
                 acc[c][i] += g * n;
-                v[i] = RowPiece<T>::get(pd[c], i) + r * (g * RowPiece<T>::get(pw[c], i) - n * k);
+                v[i] = RowPiece<T>::get(cd[c], i) + r * (g * RowPiece<T>::get(pw[c], i) - n * k);
             }
-            if (at < d) store_piece<T, ALIGNED>(dx + at0, at, d, v);
+            if (at < d) store_piece<T, ALIGNED>(dx + (size_t)row * d, at, d, v);
         }
     }
     // the block's column sums; with a row per wavefront the four wavefronts' are added in their order
@@ -263,16 +293,19 @@ __global__ __launch_bounds__(1024) void norm_weight_sum_kernel(const float *__re
 {
     __shared__ float t[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
-    float a[4] = {0.f, 0.f, 0.f, 0.f};
+    float a = 0.f;
     if (col < d) {
         int b = wave;
-        for (; b + 48 < blocks; b += 64) {
+        for (; b + 15 * 16 < blocks; b += 256) {   // sixteen rows in flight
+            float v[16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] += part[(size_t)(b + 16 * i) * d + col];
+            for (int i = 0; i < 16; ++i) v[i] = part[(size_t)(b + 16 * i) * d + col];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) a += v[i];
         }
-        for (; b < blocks; b += 16) a[0] += part[(size_t)b * d + col];
+        for (; b < blocks; b += 16) a += part[(size_t)b * d + col];
     }
-    t[wave][lane] = (a[0] + a[1]) + (a[2] + a[3]);
+    t[wave][lane] = a;
     __syncthreads();
     if (wave == 0 && col < d) {
         float s = 0.f;
@@ -283,7 +316,8 @@ __global__ __launch_bounds__(1024) void norm_weight_sum_kernel(const float *__re
 }
 
 // Calls f.run<T, ALIGNED, W, NP>() for a row of d elements: one wavefront takes up to eight pieces per lane (4096 bf16 or 2048 fp32
-// values), then four, then sixteen of them.
+// values), then four, then sixteen of them.  kWide: four from three pieces per lane on (the backward pass holds four rows and a column
+// sum per element: at d = 4096 one wavefront per row has two wavefronts per SIMD to hide the memory behind, 556 us against 4 x 2).
 template <typename T, typename F> static hipError_t pick_row(int d, const F &f)
 {
     constexpr int V = RowPiece<T>::V;
@@ -292,8 +326,13 @@ template <typename T, typename F> static hipError_t pick_row(int d, const F &f)
         constexpr bool A = decltype(al)::value;
         if (pieces <= 64) return f.template run<T, A, 1, 1>();
         if (pieces <= 128) return f.template run<T, A, 1, 2>();
-        if (pieces <= 256) return f.template run<T, A, 1, 4>();
-        if (pieces <= 512) return f.template run<T, A, 1, 8>();
+        if constexpr (F::kWide) {
+            if (pieces <= 256) return f.template run<T, A, 4, 1>();
+            if (pieces <= 512) return f.template run<T, A, 4, 2>();
+        } else {
+            if (pieces <= 256) return f.template run<T, A, 1, 4>();
+            if (pieces <= 512) return f.template run<T, A, 1, 8>();
+        }
         if (pieces <= 1024) return f.template run<T, A, 4, 4>();
         if constexpr (V == 4)   // (bf16 rows end at 2048 pieces)
             if (pieces > 2048) return f.template run<T, A, 16, 4>();
@@ -303,6 +342,7 @@ template <typename T, typename F> static hipError_t pick_row(int d, const F &f)
 }
 
 struct ForwardCall {
+    static constexpr bool kWide = false;
     const void *x, *residual, *w;
     void *sum, *y;
     uint8_t *yq;
@@ -325,6 +365,7 @@ struct ForwardCall {
 };
 
 struct BackwardCall {
+    static constexpr bool kWide = true;
     const void *sum, *w, *dy, *dsum;
     void *dx;
     float *part;
