@@ -79,7 +79,7 @@ template <int N> __device__ __forceinline__ void wait_loads_and_barrier()
 template <int LAYOUT, int N, int WAVES> struct TileImage {
     static constexpr int BYTES = N * 128, PER_WAVE = N / 8 / WAVES;
     static constexpr int K_PER_PIECE = 512 / N;   // rows of k per kilobyte (K-major)
-    static constexpr int BIAS = 3072;             // what the instruction's own offset adds at most is taken off the base, added to the offsets
+    static constexpr int BIAS = 3 * 1024;            // what the instruction's own offset adds at most is taken off the base, added to the offsets
     static __device__ __forceinline__ int block_swizzle(int k) { return N >= 128 ? k & 3 : N == 64 ? k >> 1 & 1 : 0; }
     // K-contiguous: which 16 bytes of its row a lane fetches (see FragmentReader: 16 rows at a time, two to the 64 banks)
     static __device__ __forceinline__ int piece_of(int kb, int lane) { return (lane & 7) ^ ((kb & 1) << 2 | lane >> 4); }

@@ -41,8 +41,8 @@ def norm_backward(s, weight, dy, dsum, eps, dt):
     dx = g + r * (m - n * along)
     bx = HALF[dt] * dx.abs() + 128 * U * (g.abs() + r * (m.abs() + n.abs() * mag))
     dw = (dy * n).sum(0)
-    # rows one after the other in a wavefront (at least 4096 of them share the rows), 4 wavefronts, 16 + 16 partial sums
-    depth = s.shape[0] // 4096 + 48 + 96
+    # rows one after the other in a block (at most 768 of them share the rows), 4 wavefronts, 48 + 16 partial sums
+    depth = s.shape[0] // 768 + 68 + 96
     return dx, dw, bx, depth * U * (dy * n).abs().sum(0)
 
 
