@@ -137,25 +137,25 @@ template <bool BF16> __device__ __forceinline__ void scale_chunk(const ClipTable
     const char *base = (const char *)t.in[c.tensor] + c.begin * EL;
     char *out = (char *)t.out[c.tensor];
     const int n = (int)(c.end - c.begin), whole = out ? n / V : 0;
-    // the chunk's first pieces are on their way while the norm is added up
+    // from the chunk's end to its beginning; the first pieces are on their way while the norm is added up
     u32x4 p[AHEAD];
-    int i = threadIdx.x;
+    int i = whole - 1 - (int)threadIdx.x;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
-        if (i + k * kClipThreads < whole) p[k] = ((const loose *)base)[i + k * kClipThreads];
+        if (i - k * kClipThreads >= 0) p[k] = ((const loose *)base)[i - k * kClipThreads];
     const float norm = total_norm(part, parts, lds);
     const float q = max_norm / (norm + 1e-6f), f = q > 1.f ? 1.f : q;   // (a NaN stays one)
     if (norm_out && threadIdx.x == 0) *norm_out = norm;
     if (!out || (f == 1.f && t.out[c.tensor] == t.in[c.tensor])) return;
     out += c.begin * EL;
-    while (i < whole) {
+    while (i >= 0) {
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (i + k * kClipThreads < whole) ((loose *)out)[i + k * kClipThreads] = scaled<BF16>(p[k], f);
-        i += AHEAD * kClipThreads;
+            if (i - k * kClipThreads >= 0) __builtin_nontemporal_store(scaled<BF16>(p[k], f), (loose *)out + (i - k * kClipThreads));
+        i -= AHEAD * kClipThreads;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (i + k * kClipThreads < whole) p[k] = ((const loose *)base)[i + k * kClipThreads];
+            if (i - k * kClipThreads >= 0) p[k] = ((const loose *)base)[i - k * kClipThreads];
     }
     for (int j = whole * V + threadIdx.x; j < n; j += kClipThreads) {
         if constexpr (BF16) ((bf16_t *)out)[j] = f32_to_bf16(bf16_to_f32(((const bf16_t *)base)[j]) * f);
