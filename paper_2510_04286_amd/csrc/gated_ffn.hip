@@ -415,10 +415,11 @@ __global__ __launch_bounds__(256) void gated_quantize_kernel(const bf16_t *__res
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
-// Tile shapes.  Big: 256 rows x 256 features (gate and up: 128 of each), one block per CU.  Middle: 128 x 128, two blocks per CU.
-// For the few rows of a decoding step: see FewShape.
+// Tile shapes.  Big: 256 rows x 256 features (gate and up: 128 of each) and Wide: 256 x 128, one block per CU.  Middle: 128 x 128,
+// two blocks per CU.  For the few rows of a decoding step: see FewShape.
 template <int RL, int FL, bool DUAL, bool E4M3> struct Shapes {
     typedef TileShape<4, 4, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Big;
+    typedef TileShape<4, 2, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Wide;
     typedef TileShape<2, 2, 2, 2, RL, FL, DUAL, E4M3, 3, 2> Middle;
 };
 template <typename S> constexpr int lds_of(int staged_tiles) { return S::LDS > stage_bytes(staged_tiles) ? S::LDS : stage_bytes(staged_tiles); }
@@ -426,42 +427,56 @@ template <typename S> constexpr int lds_of(int staged_tiles) { return S::LDS > s
 static int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 static int steps_of(const GemmProblem &p) { return p.segments * ((p.K + 127) >> 7); }
 
-enum TileSize { kBig, kMiddle, kFew };
-// The size of the tiles of nr x nf outputs, and into how many shares a contraction of `steps` steps goes so that the chip is full.
+enum TileSize { kBig, kWide, kMiddle, kFew };
 constexpr int kFewRows = 64;   // up to these many rows of x take the kernels for few rows
 struct TileChoice {
     TileSize size;
-    int splits;
+    int splits;   // shares of the contraction, so that few tiles fill the chip
 };
-// The most that goes into one share: fewer steps than these do not pay for the ring's first round trip and the sums' way through memory.
-constexpr int kFewShare = 4, kMiddleShare = 4;
-static int shares(long long tiles, long long slots, int steps, int least)
+// The fewest steps of a share: the ring's first round trip and the sums' way through memory do not pay for less.
+constexpr int kLeastShare = 4;
+static int most_shares(long long tiles, long long slots, int steps)
 {
-    const int n = (int)std::max<long long>(1, std::min<long long>(slots / std::max(1ll, tiles), steps / least));
-    return ceil_div(steps, ceil_div(steps, n));   // no empty ones
+    return (int)std::max<long long>(1, std::min<long long>(slots / std::max(1ll, tiles), steps / kLeastShare));
 }
-static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual, bool may_split)
+static int whole_shares(int steps, int n) { return steps == 0 ? 1 : ceil_div(steps, ceil_div(steps, n)); }   // no empty ones
+
+// What the choice goes by, in us: a step and the rest (first round trip, epilogue, tail of the launch) of a round of tiles, the slots of
+// a CU, and for shares the launch of their addition and their way through memory.
+struct TileCost {
+    int rows, features, slots;
+    double step, rest;
+};
+constexpr TileCost kCosts[3] = {{256, 256, 1, 1.5, 8}, {256, 128, 1, 0.85, 6}, {128, 128, 2, 1.4, 5}};
+constexpr double kSumLaunch = 5, kSumPerMB = 0.4;
+// n products of nr x nf outputs (dual: two matrices' worth of features) and `steps` steps each.
+static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual, bool may_split, int n = 1)
 {
     const int cus = num_compute_units();
-    const long long f = dual ? 2 : 1;
-    const long long big = (long long)ceil_div(nr, 256) * ceil_div(f * nf, 256), mid = (long long)ceil_div(nr, 128) * ceil_div(f * nf, 128);
-    if (nr <= kFewRows) return {kFew, may_split ? shares(ceil_div(nf, 64), cus, steps, kFewShare) : 1};
-    if (big * 4 >= 3 * cus) return {kBig, 1};
-    return {kMiddle, may_split ? shares(mid, 2 * cus, steps, kMiddleShare) : 1};
-}
-// The three weight gradients share a launch: one size, the same shares.
-static TileChoice choose_weight_tiles(long long d, long long H, int steps)
-{
-    const int cus = num_compute_units();
-    const long long big = 3ll * ceil_div(d, 256) * ceil_div(H, 256), mid = 3ll * ceil_div(d, 128) * ceil_div(H, 128);
-    if (big * 4 >= 3 * cus) return {kBig, 1};
-    return {kMiddle, steps == 0 ? 1 : shares(mid, 2 * cus, steps, kMiddleShare)};
+    if (nr <= kFewRows && n == 1) return {kFew, may_split ? whole_shares(steps, most_shares(ceil_div(nf, 64), cus, steps)) : 1};
+    TileChoice best = {kBig, 1};
+    double least = 0;
+    for (int k = 0; k < 3; ++k) {
+        const TileCost &c = kCosts[k];
+        const long long slots = (long long)c.slots * cus, tiles = (long long)n * ceil_div(nr, c.rows) * ceil_div(dual ? 2 * nf : nf, c.features);
+        const int most = may_split ? most_shares(tiles, slots, steps) : 1;
+        for (int m = 1; m <= most; ++m) {
+            const int splits = whole_shares(steps, m);
+            double cost = ceil_div(tiles * splits, slots) * (ceil_div(steps, splits) * c.step + c.rest);
+            if (splits > 1) cost += kSumLaunch + kSumPerMB * 4e-6 * splits * n * nr * nf;
+            if (least == 0 || cost < least) {
+                least = cost;
+                best = {(TileSize)k, splits};
+            }
+        }
+    }
+    return best;
 }
 // Bytes of the shares' sums, at most: shares fill the chip at most once (slots x a tile), and none is shorter than its least.  Neither
 // bound falls as T grows, so a workspace made for the largest batch takes every smaller one.
-static size_t share_bytes(long long slots, long long tile, int steps, int least, size_t rows, size_t ld)
+static size_t share_bytes(long long slots, long long tile, int steps, size_t rows, size_t ld)
 {
-    return (size_t)std::min<long long>(slots * tile * 4, (long long)(steps / least) * rows * ld * 4);
+    return (size_t)std::min<long long>(slots * tile * 4, (long long)(steps / kLeastShare) * rows * ld * 4);
 }
 template <typename S> static void set_tiles(GemmProblem &p, int splits)
 {
@@ -472,19 +487,18 @@ template <typename S> static void set_tiles(GemmProblem &p, int splits)
 
 static size_t padded(int n) { return ((size_t)n + 63) / 64 * 64; }
 
-// Contractions of a call's products, in steps.
+// Contractions of a call's products that may be shared out, in steps.
 struct CallSteps {
-    int up, down, dx, dwgu, dwd;
+    int down, dx, dw;
 };
-static CallSteps call_steps(const slicemoe_gated_config &c, int terms, bool e4m3)
+static CallSteps call_steps(const slicemoe_gated_config &c, int terms)
 {
     const int pairs = terms == 3 ? kPairs : 1;
     const auto steps = [](long long bytes) { return (int)((bytes + 127) / 128); };
     CallSteps s;
-    s.up = pairs * steps(e4m3 ? c.d : 2ll * c.d);
     s.down = pairs * steps(2ll * c.H);
     s.dx = 2 * s.down;
-    s.dwgu = s.dwd = pairs * steps(2ll * c.T);
+    s.dw = pairs * steps(2ll * c.T);
     return s;
 }
 
@@ -512,19 +526,17 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
     p.a = take(t2 * T * p.ldh);
     p.dg = take(backward ? t2 * T * p.ldh : 0);
     p.du = take(backward ? t2 * T * p.ldh : 0);
-    const CallSteps st = call_steps(c, p.terms, quantized);
+    const CallSteps st = call_steps(c, p.terms);
     const size_t d8 = (d + 7) / 8 * 8, h8 = (H + 7) / 8 * 8, few = std::min<size_t>(T, kFewRows);
     const long long cus = num_compute_units();
     // (tiles reach past the outputs' edges; what is stored ends there, so the outputs bound the bytes of the first kind too)
     const auto rows_shares = [&](int steps) {
-        return std::max(share_bytes(cus, kFewRows * 64, steps, kFewShare, few, d8),
-                        T > few ? share_bytes(2 * cus, 128 * 128, steps, kMiddleShare, T, d8) : 0);
+        return std::max(share_bytes(cus, kFewRows * 64, steps, few, d8), T > few ? share_bytes(cus, 256 * 256, steps, T, d8) : 0);
     };
     size_t part = 0;
     if (!backward) part = rows_shares(st.down);
     else
-        part = std::max(rows_shares(st.dx), 3 * 256 + 2 * share_bytes(2 * cus, 128 * 128, st.dwgu, kMiddleShare, d, h8) +
-                                                share_bytes(2 * cus, 128 * 128, st.dwd, kMiddleShare, H, d8));
+        part = std::max(rows_shares(st.dx), 3 * 256 + 2 * share_bytes(cus, 256 * 256, st.dw, d, h8) + share_bytes(cus, 256 * 256, st.dw, H, d8));
     p.part_bytes = part;
     p.part = take(part);
     p.total = std::max<size_t>(at, 256);
@@ -603,8 +615,10 @@ template <typename S, typename KERNEL> static hipError_t run_up(KERNEL kernel, i
 template <int FL, bool E4M3, int TERMS> static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales &sc, hipStream_t s)
 {
     typedef typename Shapes<kKContiguous, FL, true, E4M3>::Big Big;
+    typedef typename Shapes<kKContiguous, FL, true, E4M3>::Wide Wide;
     typedef typename Shapes<kKContiguous, FL, true, E4M3>::Middle Middle;
     switch (choose_tiles(p.nr, p.nf, steps_of(p), true, false).size) {
+        case kWide: return run_up<Wide>(gated_up_kernel<Wide, TERMS>, lds_of<Wide>(Wide::FT), p, h, sc, s);
         case kBig: return run_up<Big>(gated_up_kernel<Big, TERMS>, lds_of<Big>(Big::FT), p, h, sc, s);
         case kMiddle: return run_up<Middle>(gated_up_kernel<Middle, TERMS>, lds_of<Middle>(Middle::FT), p, h, sc, s);
         default: break;
@@ -639,6 +653,7 @@ template <typename S, typename KERNEL> static hipError_t run_products(KERNEL ker
 template <int RL, int FL> static hipError_t launch_products(Products &ps, int n, TileChoice t, char *part, hipStream_t s)
 {
     typedef typename Shapes<RL, FL, false, false>::Big Big;
+    typedef typename Shapes<RL, FL, false, false>::Wide Wide;
     typedef typename Shapes<RL, FL, false, false>::Middle Middle;
     long long most = 0;
     size_t at = 0;
@@ -654,6 +669,7 @@ template <int RL, int FL> static hipError_t launch_products(Products &ps, int n,
     for (int i = n; i < 3; ++i) ps.part[i] = nullptr;
     hipError_t e;
     if (t.size == kBig) e = run_products<Big>(gated_product_kernel<Big>, lds_of<Big>(Big::TF), ps, n, s);
+    else if (t.size == kWide) e = run_products<Wide>(gated_product_kernel<Wide>, lds_of<Wide>(Wide::TF), ps, n, s);
     else if (t.size == kMiddle) e = run_products<Middle>(gated_product_kernel<Middle>, lds_of<Middle>(Middle::TF), ps, n, s);
     else if constexpr (RL == kKContiguous) {
         typedef FewShape<1, 2, FL, false, false, 1> One;
@@ -727,7 +743,11 @@ template <typename S, typename D, int TERMS> static hipError_t run_up_backward(G
 template <int TERMS> static hipError_t launch_up_backward(const GemmProblem &p, const GemmProblem &q, const Hidden &h, hipStream_t s)
 {
     typedef Shapes<kKContiguous, kKMajor, true, false> Sh;
-    if (choose_tiles(p.nr, p.nf, steps_of(p), true, false).size == kBig)
+    // (the products of a tile come one after the other: the sum of their steps; few rows: the middle tiles)
+    const TileSize size = choose_tiles(std::max(p.nr, kFewRows + 1), p.nf, 3 * steps_of(p) / 2, true, false).size;
+    if (size == kWide)
+        return run_up_backward<typename Sh::Wide, TileShape<4, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
+    if (size == kBig)
         return run_up_backward<typename Sh::Big, TileShape<4, 2, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
     return run_up_backward<typename Sh::Middle, TileShape<2, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
 }
@@ -762,7 +782,7 @@ hipError_t launch_gated_ffn_backward(const slicemoe_gated_config &c, const Gated
         ps.out[0] = {g.Wg, nullptr, c.d, c.H, f32};
         ps.out[1] = {g.Wu, nullptr, c.d, c.H, f32};
         ps.out[2] = {g.Wd, nullptr, c.H, c.d, f32};
-        const TileChoice t = choose_weight_tiles(c.d, c.H, steps_of(ps.p[0]));
+        const TileChoice t = choose_tiles(c.d, c.H, steps_of(ps.p[0]), false, true, 3);
         e = launch_products<kKMajor, kKMajor>(ps, 3, t, part, s);
         if (e != hipSuccess || c.T == 0) return e;
     }

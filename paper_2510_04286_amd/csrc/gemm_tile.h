@@ -13,9 +13,9 @@
 //     ds_read_b64_tr_b16, which hand every lane the four k of its row.
 //
 // Each operand has a ring of images, the rows' one longer than the features' where the LDS has room for it (3 + 2 images of 32 KB).
-// Inside a step the fragments of the next quarter are read between the matrix instructions of the present one; in front of the last
-// quarter stands the step's one barrier: behind it the next step's images have landed for every wavefront and the present ones,
-// whose last fragments are in registers, are free for the requests two and three steps ahead.
+// Fragments are read AHEAD quarters before their use, between the matrix instructions; that many quarters before a step's end stands
+// its one barrier: behind it the next step's images have landed for every wavefront and the present ones, whose last fragments are
+// in registers, are free for the requests two and three steps ahead.
 //
 // Edges: rows and columns past an operand's end are read at its last one (their products are never stored); a step that reaches past
 // the end of K takes those 16-byte pieces from a page of zeros, in both operands.
@@ -175,6 +175,7 @@ template <int TR_, int TF_, int WR_, int WF_, int RL_, int FL_, bool DUAL_, bool
     static constexpr int R_LOADS = RI::PER_WAVE, F_LOADS = IMAGES * FI::PER_WAVE;   // instructions per wavefront and step
     static constexpr int LDS = SR * R_BYTES + SF * F_BYTES;
     static constexpr int KS = E4M3 ? 2 : 4;                              // matrix-instruction steps (quarters, halves) per step
+    static constexpr int AHEAD = KS - 1;                                 // quarters between a fragment's read and its use
 };
 
 // acc[feature tile][row tile] += the steps [s0, s1) of the problem's contraction (counted through its segments).
@@ -246,7 +247,9 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
         }
     };
     typedef typename FragmentReader<S::RL, S::BR, S::E4M3>::frag frag;
-    frag rf[2][S::TR], ff[2][S::TF];
+    constexpr int SETS = S::AHEAD + 1;
+    static_assert(S::KS % SETS == 0, "quarter q has the set q % SETS in every step");
+    frag rf[SETS][S::TR], ff[SETS][S::TF];
     // fragment i of quarter ks of the step in the rings' present images, in the order of their first use: the first features', all
     // rows', the other features'
     int rcur = 0, fcur = 0;
@@ -265,25 +268,25 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
         else
             acc[t][u] = mfma_bf16(ff[set][t], rf[set][u], acc[t][u]);
     };
-    // One quarter: its matrix instructions, with the reads of the next quarter and the requests [FROM, TO) of a later step between them.
+    // One quarter: its matrix instructions, with the reads of quarter `ahead` and the requests [FROM, TO) of a later step between them.
     // A wavefront issues in order, and one that asks for several kilobytes in a row stands still until the memory pipeline has taken
     // them: each request has its own place.
     constexpr int NM = S::TR * S::TF, NF = S::TR + S::TF;
-    const auto quarter = [&](int set, auto reads, int next_ks, auto tail, auto from, auto to, int rleft, int fleft) {
+    const auto quarter = [&](int now, auto reads, int ahead, auto tail, auto from, auto to, int rleft, int fleft) {
         constexpr bool READS = decltype(reads)::value;
         constexpr int FROM = decltype(from)::value, TO = decltype(to)::value;
         for_range<0, NM>([&](auto mm) {
             constexpr int M = decltype(mm)::value;
-            multiply(set, M);
+            multiply(now % SETS, M);
             if constexpr (READS)
 #pragma unroll
-                for (int i = M * NF / NM; i < (M + 1) * NF / NM; ++i) read(set ^ 1, next_ks, i);
+                for (int i = M * NF / NM; i < (M + 1) * NF / NM; ++i) read(ahead % SETS, ahead, i);
             pieces(tail, Int<FROM + M *(TO - FROM) / NM>(), Int<FROM + (M + 1) * (TO - FROM) / NM>(), rleft, fleft);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    // Behind a barrier: the last quarter of one step and all but the last of the next one, with the requests: the features' (needed first)
-    // in the first quarter, the rows' in the later ones.  LOADS: how many of them (0, the features', all).
+    // Behind a barrier: the last AHEAD quarters of one step and the others of the next one, with the requests: the features' (needed
+    // first) in the first quarter, the rows' in the later ones.  LOADS: how many of them (0, the features', all).
     const auto step = [&](auto tail, auto loads) {
         rcur = rcur + 1 == S::SR ? 0 : rcur + 1;
         fcur = fcur + 1 == S::SF ? 0 : fcur + 1;
@@ -291,7 +294,7 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
         for_range<0, S::KS>([&](auto qq) {
             constexpr int Q = decltype(qq)::value, F = S::F_LOADS, R = decltype(loads)::value - F;
             constexpr auto upto = [](int q) { return R + F == 0 || q == 0 ? 0 : F + R * (q - 1) / (S::KS - 1); };
-            quarter((Q + S::KS - 1) & 1, std::true_type(), Q, tail, Int<upto(Q)>(), Int<upto(Q + 1)>(), rleft, fleft);
+            quarter((Q + S::KS - S::AHEAD) % S::KS, std::true_type(), Q, tail, Int<upto(Q)>(), Int<upto(Q + 1)>(), rleft, fleft);
         });
     };
     constexpr Int<0> none = {};
@@ -312,9 +315,11 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
     if (n >= S::SR) wait_loads_and_barrier<IN_FLIGHT + S::R_LOADS + S::F_LOADS>();
     else wait_loads_and_barrier<0>();
 #pragma unroll
-    for (int i = 0; i < NF; ++i) read(0, 0, i);
+    for (int q = 0; q < S::AHEAD; ++q)
 #pragma unroll
-    for (int q = 0; q + 1 < S::KS; ++q) quarter(q & 1, std::true_type(), q + 1, std::false_type(), none, none, 0, 0);
+        for (int i = 0; i < NF; ++i) read(q % SETS, q, i);
+#pragma unroll
+    for (int q = 0; q + S::AHEAD < S::KS; ++q) quarter(q, std::true_type(), q + S::AHEAD, std::false_type(), none, none, 0, 0);
     int todo = n - S::SR;   // steps that request both operands
     const auto whole_steps = [&](int count) {
         for (; count > 0; --count) {
@@ -343,7 +348,8 @@ __device__ __forceinline__ void mma_steps(f32x16 (&acc)[S::TF][S::TR], const Gem
         step(std::false_type(), none);
     }
     lds_barrier();   // every wavefront is past its last read: the caller may use the LDS
-    quarter((S::KS - 1) & 1, std::false_type(), 0, std::false_type(), none, none, 0, 0);
+#pragma unroll
+    for (int q = S::KS - S::AHEAD; q < S::KS; ++q) quarter(q, std::false_type(), 0, std::false_type(), none, none, 0, 0);
 }
 
 // Few rows: a tile of 32 TR rows and 32 FT features (of one or two images) per block, each wavefront with every fourth step of the
