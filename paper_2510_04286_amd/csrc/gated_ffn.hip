@@ -441,14 +441,17 @@ static int most_shares(long long tiles, long long slots, int steps)
 }
 static int whole_shares(int steps, int n) { return steps == 0 ? 1 : ceil_div(steps, ceil_div(steps, n)); }   // no empty ones
 
-// What the choice goes by, in us: a step and the rest (first round trip, epilogue, tail of the launch) of a round of tiles, the slots of
-// a CU, and for shares the launch of their addition and their way through memory.
+// What the choice goes by, in us, fitted to kernel traces of the three sizes on the same products: a step of a tile that has its CU to
+// itself and of one that shares it, the rest of a round of tiles (launch, first round trip, epilogue), and for shares the launch of
+// their addition and their way through memory.  (T 8191, d 768, H 2048, big / wide / middle: up 61 / 71 / 70, down in two shares
+// 75 / 48 / 44, dx 86 / 71 / 67, weights in three shares 101 / 105 / 108; T 8192, d 4096, H 11008: up 1070 / 1276 / 1383, weights
+// 1712 / 1889 / 2759, dx 1040 / 1313 / 1514; fp32, T 1000, d 256, H 683: up 45 / 27 / 18.)
 struct TileCost {
-    int rows, features, slots;
-    double step, rest;
+    int rows, features, slots;   // slots: tiles per CU
+    double alone, shared, rest;
 };
-constexpr TileCost kCosts[3] = {{256, 256, 1, 1.5, 8}, {256, 128, 1, 0.85, 6}, {128, 128, 2, 1.4, 5}};
-constexpr double kSumLaunch = 5, kSumPerMB = 0.4;
+constexpr TileCost kCosts[3] = {{256, 256, 1, 1.5, 1.5, 10}, {256, 128, 1, 0.95, 0.95, 8}, {128, 128, 2, 0.6, 1.0, 6}};
+constexpr double kSumLaunch = 4, kSumPerMB = 0.15;
 // n products of nr x nf outputs (dual: two matrices' worth of features) and `steps` steps each.
 static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual, bool may_split, int n = 1)
 {
@@ -462,7 +465,7 @@ static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual,
         const int most = may_split ? most_shares(tiles, slots, steps) : 1;
         for (int m = 1; m <= most; ++m) {
             const int splits = whole_shares(steps, m);
-            double cost = ceil_div(tiles * splits, slots) * (ceil_div(steps, splits) * c.step + c.rest);
+            double cost = ceil_div(tiles * splits, slots) * (ceil_div(steps, splits) * (tiles * splits <= cus ? c.alone : c.shared) + c.rest);
             if (splits > 1) cost += kSumLaunch + kSumPerMB * 4e-6 * splits * n * nr * nf;
             if (least == 0 || cost < least) {
                 least = cost;
