@@ -522,6 +522,8 @@ _dtype_of, _on_gpu = operator.attrgetter("dtype"), operator.attrgetter("is_cuda"
 
 def _check_list(tensors, name):
     for i, t in enumerate(tensors):
+        if t is None:
+            raise TypeError(f"{name}[{i}] must be a CUDA/HIP tensor")
         _ptr(t, None, None, f"{name}[{i}]")
 
 
