@@ -72,11 +72,25 @@ __global__ __launch_bounds__(256) void gated_copy_kernel(CopyJobs jobs)
         const long long row = i / per_row;
         const int col = (int)(i - row * per_row) * 8;
         float v[8];
+        const size_t at = (size_t)row * j.cols + col;
+        if (col + 8 <= j.cols) {   // (a row may start at any element)
+            typedef u32x4 __attribute__((aligned(2))) loose;
+            if (jobs.f32) {
+                const u32x4 a = *(const loose *)((const float *)j.src + at), b = *(const loose *)((const float *)j.src + at + 4);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const size_t at = (size_t)row * j.cols + col + k;
-            v[k] = col + k < j.cols ? (jobs.f32 ? ((const float *)j.src)[at] : bf16_to_f32(((const bf16_t *)j.src)[at])) : 0.f;
-        }
+                for (int k = 0; k < 4; ++k) {
+                    v[k] = __uint_as_float(a[k]);
+                    v[4 + k] = __uint_as_float(b[k]);
+                }
+            } else {
+                const u32x4 a = *(const loose *)((const bf16_t *)j.src + at);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(k & 1 ? a[k >> 1] & 0xffff0000u : a[k >> 1] << 16);
+            }
+        } else
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v[k] = col + k < j.cols ? (jobs.f32 ? ((const float *)j.src)[at + k] : bf16_to_f32(((const bf16_t *)j.src)[at + k])) : 0.f;
         bf16_t *d = j.dst + (size_t)row * j.ld;
         if (jobs.f32) store_terms<3>(d, (size_t)j.rows * j.ld, col, j.cols, v);
         else store_terms<1>(d, 0, col, j.cols, v);
@@ -221,6 +235,87 @@ __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, 
             return a;
         };
         store_rows<S::FT>(lds, gated, [&](int r, int c, const float *v) { put_hidden<TERMS>(h, 0, row + 32 * u + r, col + c, v); });
+    }
+}
+
+// A share of both projections (and, with D, of dy Wd^T): its raw sums, part[split][image][rows][ld] in fp32.
+template <typename S, typename D>
+__global__ __launch_bounds__(256) void gated_up_share_kernel(GemmProblem p, GemmProblem q, Hidden h, float *__restrict__ part)
+{
+    extern __shared__ __align__(1024) char lds[];
+    constexpr int IMAGES = std::is_void<D>::value ? 2 : 3;
+    const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, p.splits);
+    const int row0 = at.r * S::BR, f0 = at.f * S::BF, wave = threadIdx.x >> 6;
+    const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
+    const auto put = [&](int image) {
+        const Out o = {part + (size_t)(IMAGES * at.split + image) * h.rows * h.ld, nullptr, h.rows, h.ld, 1};
+        return [=](int u) { return [=](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); }; };
+    };
+    int s0, s1;
+    {
+        f32x16 acc[S::TF][S::TR];
+        clear<S>(acc);
+        share_of(p, at.split, s0, s1);
+        mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int u = 0; u < S::TR; ++u) store_rows<S::FT>(lds, [&](int t) { return acc[m * S::FT + t][u]; }, put(m)(u));
+    }
+    if constexpr (IMAGES == 3) {
+        lds_barrier();   // the sums have left the LDS
+        f32x16 acc[D::TF][D::TR];
+        clear<D>(acc);
+        share_of(q, at.split, s0, s1);
+        mma_steps<D>(acc, q, row0, f0, s0, s1, lds);
+#pragma unroll
+        for (int u = 0; u < D::TR; ++u) store_rows<D::TF>(lds, [&](int t) { return acc[t][u]; }, put(2)(u));
+    }
+}
+
+// a (and dg, du) from the shares' sums.
+template <int TERMS, bool E4M3, int IMAGES>
+__global__ __launch_bounds__(256) void gated_up_sum_kernel(const float *__restrict__ part, Hidden h, Scales sc, int splits)
+{
+    const int per_row = (h.cols + 7) / 8;
+    const long long n = (long long)h.rows * per_row;
+    const size_t one = (size_t)h.rows * h.ld;
+    for (long long k = (long long)blockIdx.x * 256 + threadIdx.x; k < n; k += (long long)gridDim.x * 256) {
+        const int row = (int)(k / per_row), col = (int)(k - (long long)row * per_row) * 8;
+        float v[IMAGES][8];
+#pragma unroll
+        for (int m = 0; m < IMAGES; ++m)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[m][i] = 0.f;
+        const float *q = part + (size_t)row * h.ld + col;
+        for (int s = 0; s < splits; ++s, q += IMAGES * one)
+#pragma unroll
+            for (int m = 0; m < IMAGES; ++m) {
+                const f32x4 a = *(const f32x4 *)(q + m * one), b = *(const f32x4 *)(q + m * one + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[m][e] += a[e];
+                    v[m][4 + e] += b[e];
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float g = v[0][i], u = v[1][i];
+            if constexpr (E4M3) {
+                const int c = col + i < h.cols ? col + i : h.cols - 1;
+                g *= sc.x[row] * sc.g[c];
+                u *= sc.x[row] * sc.u[c];
+            }
+            const float sg = sigmoid<TERMS == 3>(g), s = g * sg;
+            v[0][i] = s * u;
+            if constexpr (IMAGES == 3) {
+                const float d = v[2][i];
+                v[1][i] = d * u * (sg + s * (1.f - sg));
+                v[2][i] = d * s;
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < (IMAGES == 3 ? 3 : 1); ++m) put_hidden<TERMS>(h, m, row, col, v[m]);
     }
 }
 
@@ -452,8 +547,8 @@ struct TileCost {
 };
 constexpr TileCost kCosts[3] = {{256, 256, 1, 1.5, 1.5, 10}, {256, 128, 1, 0.95, 0.95, 8}, {128, 128, 2, 0.6, 1.0, 6}};
 constexpr double kSumLaunch = 4, kSumPerMB = 0.15;
-// n products of nr x nf outputs (dual: two matrices' worth of features) and `steps` steps each.
-static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual, bool may_split, int n = 1)
+// n products of nr x nf outputs and `steps` steps each.  dual: both projections in a tile (2), and dy Wd^T after them (3).
+static TileChoice choose_tiles(long long nr, long long nf, int steps, int dual, bool may_split, int n = 1)
 {
     const int cus = num_compute_units();
     if (nr <= kFewRows && n == 1) return {kFew, may_split ? whole_shares(steps, most_shares(ceil_div(nf, 64), cus, steps)) : 1};
@@ -461,12 +556,12 @@ static TileChoice choose_tiles(long long nr, long long nf, int steps, bool dual,
     double least = 0;
     for (int k = 0; k < 3; ++k) {
         const TileCost &c = kCosts[k];
-        const long long slots = (long long)c.slots * cus, tiles = (long long)n * ceil_div(nr, c.rows) * ceil_div(dual ? 2 * nf : nf, c.features);
+        const long long slots = (long long)c.slots * cus, tiles = (long long)n * ceil_div(nr, c.rows) * ceil_div(dual ? 2 * nf : nf, c.features), sums = n * nr * nf * (dual ? dual : 1);
         const int most = may_split ? most_shares(tiles, slots, steps) : 1;
         for (int m = 1; m <= most; ++m) {
             const int splits = whole_shares(steps, m);
             double cost = ceil_div(tiles * splits, slots) * (ceil_div(steps, splits) * (tiles * splits <= cus ? c.alone : c.shared) + c.rest);
-            if (splits > 1) cost += kSumLaunch + kSumPerMB * 4e-6 * splits * n * nr * nf;
+            if (splits > 1) cost += kSumLaunch + kSumPerMB * 4e-6 * splits * sums;
             if (least == 0 || cost < least) {
                 least = cost;
                 best = {(TileSize)k, splits};
@@ -492,13 +587,14 @@ static size_t padded(int n) { return ((size_t)n + 63) / 64 * 64; }
 
 // Contractions of a call's products that may be shared out, in steps.
 struct CallSteps {
-    int down, dx, dw;
+    int up, down, dx, dw;
 };
-static CallSteps call_steps(const slicemoe_gated_config &c, int terms)
+static CallSteps call_steps(const slicemoe_gated_config &c, int terms, bool e4m3)
 {
     const int pairs = terms == 3 ? kPairs : 1;
     const auto steps = [](long long bytes) { return (int)((bytes + 127) / 128); };
     CallSteps s;
+    s.up = pairs * steps(e4m3 ? c.d : 2ll * c.d);
     s.down = pairs * steps(2ll * c.H);
     s.dx = 2 * s.down;
     s.dw = pairs * steps(2ll * c.T);
@@ -529,7 +625,7 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
     p.a = take(t2 * T * p.ldh);
     p.dg = take(backward ? t2 * T * p.ldh : 0);
     p.du = take(backward ? t2 * T * p.ldh : 0);
-    const CallSteps st = call_steps(c, p.terms);
+    const CallSteps st = call_steps(c, p.terms, quantized);
     const size_t d8 = (d + 7) / 8 * 8, h8 = (H + 7) / 8 * 8, few = std::min<size_t>(T, kFewRows);
     const long long cus = num_compute_units();
     // (tiles reach past the outputs' edges; what is stored ends there, so the outputs bound the bytes of the first kind too)
@@ -537,9 +633,10 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
         return std::max(share_bytes(cus, kFewRows * 64, steps, few, d8), T > few ? share_bytes(cus, 256 * 256, steps, T, d8) : 0);
     };
     size_t part = 0;
-    if (!backward) part = rows_shares(st.down);
+    const auto up_shares = [&](int steps, int images) { return share_bytes(cus, images * 256 * 128, steps, T, images * (size_t)p.ldh); };
+    if (!backward) part = std::max(rows_shares(st.down), up_shares(st.up, 2));
     else
-        part = std::max(rows_shares(st.dx), 3 * 256 + 2 * share_bytes(cus, 256 * 256, st.dw, d, h8) + share_bytes(cus, 256 * 256, st.dw, H, d8));
+        part = std::max(std::max(rows_shares(st.dx), up_shares(st.up + st.up / 2, 3)), 3 * 256 + 2 * share_bytes(cus, 256 * 256, st.dw, d, h8) + share_bytes(cus, 256 * 256, st.dw, H, d8));
     p.part_bytes = part;
     p.part = take(part);
     p.total = std::max<size_t>(at, 256);
@@ -615,14 +712,40 @@ template <typename S, typename KERNEL> static hipError_t run_up(KERNEL kernel, i
     kernel<<<p.tiles_r * p.tiles_f, 256, lds, s>>>(p, h, sc);
     return hipGetLastError();
 }
-template <int FL, bool E4M3, int TERMS> static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales &sc, hipStream_t s)
+template <typename S, typename D>
+static hipError_t run_up_shares(GemmProblem p, GemmProblem q, const Hidden &h, int splits, float *part, hipStream_t s)
+{
+    set_tiles<S>(p, splits);
+    q.splits = splits;
+    constexpr int lds = lds_of<S>(S::FT);
+    const auto kernel = gated_up_share_kernel<S, D>;
+    const hipError_t e = ready(kernel, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<p.tiles_r * p.tiles_f * splits, 256, lds, s>>>(p, q, h, part);
+    return hipGetLastError();
+}
+template <int TERMS, bool E4M3, int IMAGES>
+static hipError_t launch_up_sum(const float *part, const Hidden &h, const Scales &sc, int splits, hipStream_t s)
+{
+    const long long n = (long long)h.rows * ((h.cols + 7) / 8);
+    gated_up_sum_kernel<TERMS, E4M3, IMAGES><<<(int)std::min<long long>((n + 255) / 256, 8ll * num_compute_units()), 256, 0, s>>>(part, h, sc, splits);
+    return hipGetLastError();
+}
+template <int FL, bool E4M3, int TERMS> static hipError_t launch_up(const GemmProblem &p, const Hidden &h, const Scales &sc, float *part, hipStream_t s)
 {
     typedef typename Shapes<kKContiguous, FL, true, E4M3>::Big Big;
     typedef typename Shapes<kKContiguous, FL, true, E4M3>::Wide Wide;
     typedef typename Shapes<kKContiguous, FL, true, E4M3>::Middle Middle;
-    switch (choose_tiles(p.nr, p.nf, steps_of(p), true, false).size) {
-        case kWide: return run_up<Wide>(gated_up_kernel<Wide, TERMS>, lds_of<Wide>(Wide::FT), p, h, sc, s);
+    const TileChoice t = choose_tiles(p.nr, p.nf, steps_of(p), 2, p.nr > kFewRows);
+    if (t.splits > 1) {
+        const hipError_t e = t.size == kBig    ? run_up_shares<Big, void>(p, p, h, t.splits, part, s)
+                             : t.size == kWide ? run_up_shares<Wide, void>(p, p, h, t.splits, part, s)
+                                               : run_up_shares<Middle, void>(p, p, h, t.splits, part, s);
+        return e == hipSuccess ? launch_up_sum<TERMS, E4M3, 2>(part, h, sc, t.splits, s) : e;
+    }
+    switch (t.size) {
         case kBig: return run_up<Big>(gated_up_kernel<Big, TERMS>, lds_of<Big>(Big::FT), p, h, sc, s);
+        case kWide: return run_up<Wide>(gated_up_kernel<Wide, TERMS>, lds_of<Wide>(Wide::FT), p, h, sc, s);
         case kMiddle: return run_up<Middle>(gated_up_kernel<Middle, TERMS>, lds_of<Middle>(Middle::FT), p, h, sc, s);
         default: break;
     }
@@ -712,7 +835,8 @@ hipError_t launch_gated_ffn(const slicemoe_gated_config &c, const GatedPlan &pla
     GemmProblem p = problem(c.T, c.H, 2ll * c.d, o.ldx, o.ldw);
     add_segments(p, plan.terms, o.x, o.tx, o.Wg, o.tw, o.Wu);
     const Hidden h = hidden_of(c, plan, ws);
-    e = plan.terms == 1 ? launch_up<kKMajor, false, 1>(p, h, Scales(), s) : launch_up<kKMajor, false, 3>(p, h, Scales(), s);
+    float *part = (float *)(ws + plan.part);
+    e = plan.terms == 1 ? launch_up<kKMajor, false, 1>(p, h, Scales(), part, s) : launch_up<kKMajor, false, 3>(p, h, Scales(), part, s);
     if (e != hipSuccess) return e;
     return launch_down(c, plan, o.Wd, o.twd, o.ldwd, addend, y, ws, s);
 }
@@ -727,7 +851,7 @@ hipError_t launch_gated_ffn_quantized(const slicemoe_gated_config &c, const Gate
     if (e != hipSuccess) return e;
     GemmProblem p = problem(c.T, c.H, c.d, c.d, c.d);
     add_segments(p, 1, (const char *)x, 0, (const char *)w.Wg, 0, (const char *)w.Wu);
-    e = launch_up<kKContiguous, true, 1>(p, hidden_of(c, plan, ws), Scales{x_scale, w.Wg_scale, w.Wu_scale}, s);
+    e = launch_up<kKContiguous, true, 1>(p, hidden_of(c, plan, ws), Scales{x_scale, w.Wg_scale, w.Wu_scale}, (float *)(ws + plan.part), s);
     if (e != hipSuccess) return e;
     return launch_down(c, plan, o.Wd, o.twd, o.ldwd, addend, y, ws, s);
 }
@@ -743,16 +867,23 @@ template <typename S, typename D, int TERMS> static hipError_t run_up_backward(G
     kernel<<<p.tiles_r * p.tiles_f, 256, lds, s>>>(p, q, h);
     return hipGetLastError();
 }
-template <int TERMS> static hipError_t launch_up_backward(const GemmProblem &p, const GemmProblem &q, const Hidden &h, hipStream_t s)
+template <int TERMS> static hipError_t launch_up_backward(const GemmProblem &p, const GemmProblem &q, const Hidden &h, float *part, hipStream_t s)
 {
     typedef Shapes<kKContiguous, kKMajor, true, false> Sh;
-    // (the products of a tile come one after the other: the sum of their steps; few rows: the middle tiles)
-    const TileSize size = choose_tiles(std::max(p.nr, kFewRows + 1), p.nf, 3 * steps_of(p) / 2, true, false).size;
-    if (size == kWide)
-        return run_up_backward<typename Sh::Wide, TileShape<4, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
-    if (size == kBig)
-        return run_up_backward<typename Sh::Big, TileShape<4, 2, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
-    return run_up_backward<typename Sh::Middle, TileShape<2, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2>, TERMS>(p, q, h, s);
+    typedef TileShape<4, 2, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2> BigD;
+    typedef TileShape<4, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2> WideD;
+    typedef TileShape<2, 1, 2, 2, kKContiguous, kKContiguous, false, false, 3, 2> MiddleD;
+    // (the products of a tile come one after the other: the sum of their steps; few rows take the middle tiles)
+    const TileChoice t = choose_tiles(std::max(p.nr, kFewRows + 1), p.nf, steps_of(p) + steps_of(q) / 2, 3, true);
+    if (t.splits > 1) {
+        const hipError_t e = t.size == kBig    ? run_up_shares<typename Sh::Big, BigD>(p, q, h, t.splits, part, s)
+                             : t.size == kWide ? run_up_shares<typename Sh::Wide, WideD>(p, q, h, t.splits, part, s)
+                                               : run_up_shares<typename Sh::Middle, MiddleD>(p, q, h, t.splits, part, s);
+        return e == hipSuccess ? launch_up_sum<TERMS, false, 3>(part, h, Scales(), t.splits, s) : e;
+    }
+    if (t.size == kBig) return run_up_backward<typename Sh::Big, BigD, TERMS>(p, q, h, s);
+    if (t.size == kWide) return run_up_backward<typename Sh::Wide, WideD, TERMS>(p, q, h, s);
+    return run_up_backward<typename Sh::Middle, MiddleD, TERMS>(p, q, h, s);
 }
 
 hipError_t launch_gated_ffn_backward(const slicemoe_gated_config &c, const GatedPlan &plan, const void *x, const slicemoe_gated_weights &w,
@@ -770,7 +901,7 @@ hipError_t launch_gated_ffn_backward(const slicemoe_gated_config &c, const Gated
         add_segments(p, terms, o.x, o.tx, o.Wg, o.tw, o.Wu);
         add_segments(q, terms, o.dy, o.tx, o.Wd, o.twd);
         const Hidden h = hidden_of(c, plan, ws);
-        e = terms == 1 ? launch_up_backward<1>(p, q, h, s) : launch_up_backward<3>(p, q, h, s);
+        e = terms == 1 ? launch_up_backward<1>(p, q, h, (float *)part, s) : launch_up_backward<3>(p, q, h, (float *)part, s);
         if (e != hipSuccess) return e;
     }
     // The weight gradients, before dx: dx may then take the place of dy.  (T = 0: contractions of no steps, zeros.)

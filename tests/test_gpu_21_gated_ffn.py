@@ -69,6 +69,13 @@ def test_large_tiles(B, T, d, H):
     run(B, T, d, H, B16)
 
 
+@pytest.mark.parametrize("T,d,H,dt", [(130, 4096, 64, B16), (65, 2048, 100, B16), (513, 3000, 72, B16), (5, 4096, 128, B16), (300, 2705, 244, F32),
+                                      (40, 1000, 33, F32), (1500, 8192, 130, B16)], ids=str)
+def test_projections_in_shares(B, T, d, H, dt):
+    """Few tiles and a long contraction: both projections, and the backward of the gate, from sums of shares."""
+    run(B, T, d, H, dt)
+
+
 def test_large_tiles_fp32(B):
     run(B, 2051, 300, 6500, F32)
 
@@ -79,7 +86,7 @@ def test_without_addends(B):
 
 
 @pytest.mark.parametrize("T,d,H", [(1, 16, 1), (1, 128, 64), (5, 48, 33), (16, 4096, 200), (32, 256, 768), (33, 272, 100), (64, 1024, 2816),
-                                   (65, 128, 130), (200, 400, 1000), (257, 2048, 96), (4100, 512, 2056)])
+                                   (65, 128, 130), (65, 8192, 64), (300, 4096, 100), (200, 400, 1000), (257, 2048, 96), (4100, 512, 2056)])
 def test_eight_bits(B, T, d, H):
     cfg = B.make_gated_config(T, d, H, "bf16")
     w = weights(d, H, B16)
