@@ -53,6 +53,8 @@ template <int TERMS> __device__ __forceinline__ void store_terms(bf16_t *p, size
     for (int k = 0; k < TERMS; ++k) *(uint4 *)(p + k * term + col) = o[k].q;
 }
 
+typedef u32x4 __attribute__((aligned(2))) loose;   // 16 bytes at any element
+
 struct CopyJob {
     const void *src;
     bf16_t *dst;
@@ -74,7 +76,6 @@ __global__ __launch_bounds__(256) void gated_copy_kernel(CopyJobs jobs)
         float v[8];
         const size_t at = (size_t)row * j.cols + col;
         if (col + 8 <= j.cols) {   // (a row may start at any element)
-            typedef u32x4 __attribute__((aligned(2))) loose;
             if (jobs.f32) {
                 const u32x4 a = *(const loose *)((const float *)j.src + at), b = *(const loose *)((const float *)j.src + at + 4);
 #pragma unroll
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void gated_copy_kernel(CopyJobs jobs)
 
 // ---- epilogues -----------------------------------------------------------------------------------------------------------
 // 32 rows of a wavefront's accumulators (of NT feature tiles) leave through its own part of the LDS, so that eight consecutive
-// features of a row come to one lane: put(row of the 32, feature of the tiles, eight values).
+// features of a row come to one lane: put(row of the 32, feature of the tiles, eight values, which of the lane's pieces).
 template <int NT, typename GET, typename PUT> __device__ __forceinline__ void store_rows(char *lds, const GET &get, const PUT &put)
 {
     constexpr int W = 32 * NT, STRIDE = W + 4, PIECES = W / 8;
@@ -117,7 +118,7 @@ template <int NT, typename GET, typename PUT> __device__ __forceinline__ void st
         const int k = i * 64 + lane, r = k / PIECES, c = k % PIECES;
         const f32x4 lo = *(const f32x4 *)(st + r * STRIDE + 8 * c), hi = *(const f32x4 *)(st + r * STRIDE + 8 * c + 4);
         const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        put(r, 8 * c, v);
+        put(r, 8 * c, v, i);
     }
     wave_lds_sync();
     __builtin_amdgcn_sched_barrier(0);   // (the next rows' accumulators stay where they are until then)
@@ -130,28 +131,37 @@ struct Out {
     int rows, cols;
     int f32;
 };
-// out = addend + v for eight columns of a row; rows are whole 16-byte pieces or not.
-__device__ __forceinline__ void put_out(const Out &o, int row, int col, const float *v)
+// The addend of eight columns of a row, where they are whole (zeros elsewhere and without one); 16-byte accesses at any element.
+struct Addend {
+    u32x4 lo, hi;   // hi: fp32 only
+};
+__device__ __forceinline__ Addend fetch_addend(const Out &o, int row, int col)
+{
+    Addend a = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (o.addend && row < o.rows && col + 8 <= o.cols) {
+        const size_t at = (size_t)row * o.cols + col;
+        a.lo = *(const loose *)((const char *)o.addend + at * (o.f32 ? 4 : 2));
+        if (o.f32) a.hi = *(const loose *)((const float *)o.addend + at + 4);
+    }
+    return a;
+}
+// out = addend + v for eight columns of a row; past the row's end value by value.
+__device__ __forceinline__ void put_out(const Out &o, int row, int col, const float *v, const Addend &d)
 {
     if (row >= o.rows || col >= o.cols) return;
     const size_t at = (size_t)row * o.cols + col;
-    if ((o.cols & 7) == 0) {
+    if (col + 8 <= o.cols) {
         if (o.f32) {
-            f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
-            if (o.addend) {
-                a += *(const f32x4 *)((const float *)o.addend + at);
-                b += *(const f32x4 *)((const float *)o.addend + at + 4);
-            }
-            *(f32x4 *)((float *)o.p + at) = a;
-            *(f32x4 *)((float *)o.p + at + 4) = b;
+            const f32x4 a = f32x4{v[0], v[1], v[2], v[3]} + __builtin_bit_cast(f32x4, d.lo), b = f32x4{v[4], v[5], v[6], v[7]} + __builtin_bit_cast(f32x4, d.hi);
+            *(loose *)((float *)o.p + at) = __builtin_bit_cast(u32x4, a);
+            *(loose *)((float *)o.p + at + 4) = __builtin_bit_cast(u32x4, b);
         } else {
-            u32x4 d = {0, 0, 0, 0}, r;
-            if (o.addend) d = *(const u32x4 *)((const bf16_t *)o.addend + at);
+            u32x4 r;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                r[i] = (uint32_t)f32_to_bf16(v[2 * i] + __uint_as_float(d[i] << 16)) |
-                       (uint32_t)f32_to_bf16(v[2 * i + 1] + __uint_as_float(d[i] & 0xffff0000u)) << 16;
-            *(u32x4 *)((bf16_t *)o.p + at) = r;
+                r[i] = (uint32_t)f32_to_bf16(v[2 * i] + __uint_as_float(d.lo[i] << 16)) |
+                       (uint32_t)f32_to_bf16(v[2 * i + 1] + __uint_as_float(d.lo[i] & 0xffff0000u)) << 16;
+            *(loose *)((bf16_t *)o.p + at) = r;
         }
         return;
     }
@@ -162,6 +172,7 @@ __device__ __forceinline__ void put_out(const Out &o, int row, int col, const fl
         else ((bf16_t *)o.p)[at + i] = f32_to_bf16(v[i] + (o.addend ? bf16_to_f32(((const bf16_t *)o.addend)[at + i]) : 0.f));
     }
 }
+__device__ __forceinline__ void put_out(const Out &o, int row, int col, const float *v) { put_out(o, row, col, v, fetch_addend(o, row, col)); }
 
 template <bool PRECISE> __device__ __forceinline__ float sigmoid(float g)
 {
@@ -234,7 +245,7 @@ __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, 
             }
             return a;
         };
-        store_rows<S::FT>(lds, gated, [&](int r, int c, const float *v) { put_hidden<TERMS>(h, 0, row + 32 * u + r, col + c, v); });
+        store_rows<S::FT>(lds, gated, [&](int r, int c, const float *v, int) { put_hidden<TERMS>(h, 0, row + 32 * u + r, col + c, v); });
     }
 }
 
@@ -249,7 +260,7 @@ __global__ __launch_bounds__(256) void gated_up_share_kernel(GemmProblem p, Gemm
     const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
     const auto put = [&](int image) {
         const Out o = {part + (size_t)(IMAGES * at.split + image) * h.rows * h.ld, nullptr, h.rows, h.ld, 1};
-        return [=](int u) { return [=](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); }; };
+        return [=](int u) { return [=](int r, int c, const float *v, int) { put_out(o, row + 32 * u + r, col + c, v); }; };
     };
     int s0, s1;
     {
@@ -358,20 +369,32 @@ template <typename S> __global__ __launch_bounds__(256) void gated_product_kerne
     const GemmProblem &p = ps.p[k];
     const TilePlace at = tile_of(blockIdx.x - ps.first[k], p.tiles_r, p.tiles_f, p.splits);
     const int row0 = at.r * S::BR, f0 = at.f * S::BF, wave = threadIdx.x >> 6;
-    f32x16 acc[S::TF][S::TR];
-    clear<S>(acc);
-    int s0, s1;
-    share_of(p, at.split, s0, s1);
-    mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
+    const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::TF, lane = threadIdx.x & 63;
     Out o = ps.out[k];
     if (ps.part[k]) {
         const int ld = (o.cols + 7) & ~7;
         o = {ps.part[k] + (size_t)at.split * o.rows * ld, nullptr, o.rows, ld, 1};
     }
-    const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::TF;
+    f32x16 acc[S::TF][S::TR];
+    clear<S>(acc);
+    int s0, s1;
+    share_of(p, at.split, s0, s1);
+    mma_steps<S>(acc, p, row0, f0, s0, s1, lds);
+    // the addend of 32 rows is requested while those before them are stored (piece by piece each would wait for its own: 32 waits)
+    constexpr int PIECES = 4 * S::TF, MINE = PIECES / 2;
+    Addend next[MINE], now[MINE];
+    const auto fetch = [&](int u) {
 #pragma unroll
-    for (int u = 0; u < S::TR; ++u)
-        store_rows<S::TF>(lds, [&](int t) { return acc[t][u]; }, [&](int r, int c, const float *v) { put_out(o, row + 32 * u + r, col + c, v); });
+        for (int i = 0; i < MINE; ++i) next[i] = fetch_addend(o, row + 32 * u + (i * 64 + lane) / PIECES, col + (i * 64 + lane) % PIECES * 8);
+    };
+    fetch(0);
+#pragma unroll
+    for (int u = 0; u < S::TR; ++u) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) now[i] = next[i];
+        if (u + 1 < S::TR) fetch(u + 1);
+        store_rows<S::TF>(lds, [&](int t) { return acc[t][u]; }, [&](int r, int c, const float *v, int i) { put_out(o, row + 32 * u + r, col + c, v, now[i]); });
+    }
 }
 
 template <typename S> __global__ __launch_bounds__(256) void gated_product_few_kernel(Products ps)
@@ -446,7 +469,7 @@ __global__ __launch_bounds__(256) void gated_up_backward_kernel(GemmProblem p, G
     const int row = row0 + wave / S::WF * 32 * S::TR, col = f0 + wave % S::WF * 32 * S::FT;
 #pragma unroll
     for (int u = 0; u < S::TR; ++u) {
-        const auto put = [&](int which) { return [&, which](int r, int c, const float *v) { put_hidden<TERMS>(h, which, row + 32 * u + r, col + c, v); }; };
+        const auto put = [&](int which) { return [&, which](int r, int c, const float *v, int) { put_hidden<TERMS>(h, which, row + 32 * u + r, col + c, v); }; };
         const auto first = [&](int t) {   // a; acc and da become dg and du
             f32x16 a;
 #pragma unroll
