@@ -431,11 +431,14 @@ def _bytes_ptr(t, numel, name):
 
 def slicemoe_add_rmsnorm(cfg, x, residual, weight, sum_out, y, y_quantized=None, y_scale=None, stream=None):
     """residual, sum_out and, with y_quantized, y may be None."""
-    dt, n = _tdtype(cfg), cfg.T * cfg.d
-    _check(lib().slicemoe_add_rmsnorm(ctypes.byref(cfg), _ptr(x, dt, n, "x"), _ptr(residual, dt, n, "residual"),
-                                      _ptr(weight, dt, cfg.d, "weight"), _ptr(sum_out, dt, n, "sum_out"), _ptr(y, dt, n, "y"),
-                                      _bytes_ptr(y_quantized, n, "y_quantized"), _ptr(y_scale, torch.float32, cfg.T, "y_scale"),
-                                      _stream(stream)), "slicemoe_add_rmsnorm")
+    d, T = cfg.d, cfg.T
+    dt, n = _tdtype(cfg), T * d
+    st = (_lib or lib()).slicemoe_add_rmsnorm(
+        ctypes.byref(cfg), _ptr(x, dt, n, "x"), _ptr(residual, dt, n, "residual"), _ptr(weight, dt, d, "weight"),
+        _ptr(sum_out, dt, n, "sum_out"), _ptr(y, dt, n, "y"), None if y_quantized is None else _bytes_ptr(y_quantized, n, "y_quantized"),
+        None if y_scale is None else _ptr(y_scale, torch.float32, T, "y_scale"), _stream(stream))
+    if st:
+        _check(st, "slicemoe_add_rmsnorm")
 
 
 def slicemoe_add_rmsnorm_backward_workspace_bytes(cfg) -> int:
@@ -529,10 +532,14 @@ def _check_list(tensors, name):
 
 def _grad_list(grads, out):
     """C array of a list of gradient tensors; out: the list written, the same list for in place, or None to measure only.  (One
-    attribute of all tensors at a time: dozens of small tensors are bound by this marshalling, 40 us for 48 of them tensor by tensor.)"""
+    attribute of all tensors at a time: dozens of small tensors are bound by this marshalling, 40 us for 48 of them tensor by tensor, 25 so.)"""
     T = torch.Tensor
     for tensors, name in ((grads, "grads"),) if out is None or out is grads else ((grads, "grads"), (out, "out")):
-        if not (all(isinstance(t, T) for t in tensors) and all(map(_on_gpu, tensors)) and all(map(T.is_contiguous, tensors))):
+        try:
+            fine = all(map(T.is_contiguous, tensors)) and all(map(_on_gpu, tensors))
+        except TypeError:   # not a tensor
+            fine = False
+        if not fine:
             _check_list(tensors, name)   # raises
     types, sizes, addresses = list(map(_dtype_of, grads)), list(map(T.numel, grads)), list(map(T.data_ptr, grads))
     codes = list(map(_GRAD_CODES.get, types))
