@@ -3,6 +3,17 @@
 //   g = x Wg,  u = x Wu,  a = silu(g) u,  y = addend + a Wd                      (silu(g) = g sg,  sg = 1 / (1 + exp(-g)))
 //   da = dy Wd^T,  dg = da u (sg + g sg (1 - sg)),  du = da g sg
 //   dx = addend + dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  dWd = a^T dy
+//
+// Every product is a tile of gemm_tile.h on the bf16 matrix cores with fp32 accumulation; no transposed copy of anything is made
+// (K-major operands are read transposed from the LDS).  Both projections share a tile, so that the gate is applied to the
+// accumulators; the backward pass computes them again beside da, and the three weight gradients are one launch.  g, u and da never leave
+// the chip; a, dg and du are rounded to bf16 once (bf16 storage), so an output holds that rounding and its own: 1.4 times the
+// error of one.
+//
+// Bound by the matrix cores and, where they are busy, by power: at T 8192, d 4096, H 11008 (bf16) up 1063 us = 1.39 PFLOP/s, down 537 =
+// 1.38, gate backward 1789 = 1.24, weight gradients 1716 = 1.29, dx 1019 = 1.45, with the matrix pipes 70 to 81% busy at 1.65 to
+// 1.8 GHz (a large library product: 1.0 to 1.5 on the same card); 8-bit projections of 4096 rows 355 us = 2.08 PFLOP/s.  Cards differ by
+// 8%.  Short contractions pay their rounds' first trip and epilogue: 16 steps (d = 1024) 31 us a round, 23 of them steps.
 #include <algorithm>
 
 #include "gated_ffn.h"
@@ -15,7 +26,8 @@ namespace slicemoe {
 // fp32 storage: an operand is the sum of three bf16 values, cut off rather than rounded, so that the first two remainders are exact
 // and all 24 bits are kept.  A product is the six products of terms whose orders add up to at most two, largest first (the matrix
 // instruction cuts its accumulator when the products outweigh it); what is left out is below 2^-24 of the product.
-// Six bf16 products run at 2.6 times the rate of the fp32 matrix instruction.
+// Six bf16 products run at 2.6 times the rate of the fp32 matrix instruction; errors against 64 bits 4e-7 (the library's fp32
+// product: 7e-7).
 constexpr int kPairs = 6;
 constexpr int kPairR[kPairs] = {0, 0, 1, 1, 0, 2}, kPairF[kPairs] = {0, 1, 0, 1, 2, 0};
 
@@ -64,7 +76,7 @@ struct CopyJobs {
     CopyJob j[5];
     int f32;
 };
-// One 16-byte piece of the copy per thread.
+// One 16-byte piece of the copy per thread.  Memory-bound: three terms of 3405 x 2705 and three weight matrices of 2705 x 244 23 us.
 __global__ __launch_bounds__(256) void gated_copy_kernel(CopyJobs jobs)
 {
     const CopyJob j = jobs.j[blockIdx.y];
@@ -212,7 +224,8 @@ __device__ __forceinline__ void share_of(const GemmProblem &p, int split, int &s
     s1 = s0 + each < steps ? s0 + each : steps;
 }
 
-// Both projections and the gate.
+// Both projections and the gate (big tiles, T 16384, d 1024, H 2816: 184 to 200 us; the gate's exponential and reciprocal are 4 us
+// of vector work per tile, the rows leave in whole 128-byte lines).
 template <typename S, int TERMS>
 __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, Scales sc)
 {
@@ -330,7 +343,9 @@ __global__ __launch_bounds__(256) void gated_up_sum_kernel(const float *__restri
     }
 }
 
-// The same for few rows.
+// The same for few rows: bound by the weights' arrival (T 16, d 4096, H 11008 in 8 bits: 90 MB in 23 us; T 32, d 1024, H 2816 in bf16: 8 us,
+// two round trips and the launch).  Against 128-feature tiles whose contraction was shared out over blocks and added up by a second kernel:
+// 24 and 12 us.
 template <typename S, int TERMS> __global__ __launch_bounds__(256) void gated_up_few_kernel(GemmProblem p, Hidden h, Scales sc)
 {
     extern __shared__ __align__(1024) char lds[];
@@ -354,7 +369,8 @@ template <typename S, int TERMS> __global__ __launch_bounds__(256) void gated_up
     });
 }
 
-// Up to three products in one launch, into their outputs or, with a split contraction, into fp32 shares.
+// Up to three products in one launch (the weight gradients: together they fill the chip where each alone would not), into their
+// outputs or, with a split contraction, into fp32 shares.
 struct Products {
     GemmProblem p[3];
     Out out[3];
@@ -453,7 +469,7 @@ template <int GROUPS> __global__ __launch_bounds__(256) void gated_sum_kernel(Pr
 }
 
 // Backward of the gate: both projections again, da beside them, and a, dg, du.  S: as gated_up_kernel; D: the same rows and features
-// of dy Wd^T.
+// of dy Wd^T.  Half of its time at small d is the epilogue, three outputs at once (T 8191, d 768, H 2048: 54 us a round, 30 of them steps).
 template <typename S, typename D, int TERMS>
 __global__ __launch_bounds__(256) void gated_up_backward_kernel(GemmProblem p, GemmProblem q, Hidden h)
 {
@@ -569,7 +585,7 @@ struct TileCost {
     double alone, shared, rest;
 };
 constexpr TileCost kCosts[3] = {{256, 256, 1, 1.5, 1.5, 10}, {256, 128, 1, 0.95, 0.95, 8}, {128, 128, 2, 0.6, 1.0, 6}};
-constexpr double kSumLaunch = 4, kSumPerMB = 0.15;
+constexpr double kSumLaunch = 6, kSumPerMB = 0.15;
 // n products of nr x nf outputs and `steps` steps each.  dual: both projections in a tile (2), and dy Wd^T after them (3).
 static TileChoice choose_tiles(long long nr, long long nf, int steps, int dual, bool may_split, int n = 1)
 {
