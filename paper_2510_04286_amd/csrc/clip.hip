@@ -3,15 +3,14 @@
 //   norm = sqrt(sum over all tensors of g^2),   factor = min(1, max_norm / (norm + 1e-6)),   out = g factor
 //
 // Two launches per kTensors tensors: every block squares and sums one chunk of one tensor, then every block adds up all chunks'
-// sums (at most a few thousand, from L2, the same order in every block and every run) and scales its chunk.  Squares and sums are
+// sums (about eight thousand at most, from L2, the same order in every block and every run) and scales its chunk.  Squares and sums are
 // 64-bit: an fp32 value's square is exact there and cannot overflow, and the vector unit has the rate (one fma per four bytes
-// read).  The second pass walks chunks, and the pieces of a chunk, backwards: what the first one
-// read last is still in the last-level cache.
+// read).  The second pass walks chunks, and the pieces of a chunk, backwards: what the first one read last is still in the
+// last-level cache.
 //
 // HBM-bound: each tensor is read twice (less what the cache held) and written once; outputs are stored past the caches.  1.22 GB: 201 +
-// 458 us (6.1 and 5.3 TB/s by what a pass has to move); with cached stores 5% more, from the chunks' beginnings 6%.  Dozens of small tensors
-// are two launches.  A tensor whose values the factor does not
-// change and that is scaled in place is not written.
+// 458 us (6.1 and 5.3 TB/s by what a pass has to move; cached stores take 5% more).  Dozens of small tensors are two launches.  A tensor
+// whose values the factor does not change and that is scaled in place is not written.
 #include <math.h>
 
 #include "clip.h"
