@@ -20,8 +20,8 @@
 // What it took (up projections of T 8192, d 4096, H 11008, us): plain double buffering with the loads and reads in front of the matrix
 // instructions 1363; requests one by one between them 1264; no branch per request, LDS targets set once in four 1105; LDS rows on 64 banks
 // (32 before: a tenth of the cycles were conflicts), the rows' ring a step longer 1063.  Loads alone take 840 of them, matrix
-// instructions and LDS reads without loads 730.  Fragments a step ahead instead of a quarter, deeper rings for the smaller tiles and
-// another grouping of tiles changed nothing; 64-byte pieces of rows halve what a CU draws from L2 (95 to 57 bytes per ns).
+// instructions and LDS reads without loads 730.  Fragments a quarter ahead instead of a step: equal, or up to 7% slower.
+// Groups of 4 to 16 row tiles instead of 8: no gain.  64-byte pieces of rows: a CU draws 57 instead of 95 bytes per ns from L2.
 //
 // Edges: rows and columns past an operand's end are read at its last one (their products are never stored); a step that reaches past
 // the end of K takes those 16-byte pieces from a page of zeros, in both operands.
