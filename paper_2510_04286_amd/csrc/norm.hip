@@ -13,8 +13,9 @@
 // 1e-30 counts as 1e-30, so a row of zeros has a scale and no division by zero; a row that holds a NaN or an infinity has a NaN scale.
 //
 // HBM-bound.  65536 rows of 4096 bf16 values: forward 367 us = 5.9 TB/s, backward 431 + 6 = 4.9 (a copy of the same size: 5.2); 12289 rows
-// of 768 with e4m3 output 13.5 us.  A decoding step's rows are their launch (32 x 1024: 3 us).  Rows that are not whole 16-byte pieces (d not a multiple of 8 for bf16, 4 for fp32) start at any element:
-// their pieces are 16-byte accesses at element alignment, the last piece element by element.
+// of 768 with e4m3 output 13.5 us.  A decoding step's rows are their launch (32 x 1024: 3 us).  Rows that are not whole 16-byte pieces (d
+// not a multiple of 8 for bf16, 4 for fp32) start at any element: their pieces are 16-byte accesses at element alignment, the last
+// piece element by element.
 #include "common.h"
 #include "norm.h"
 #include "wavefront.h"
@@ -103,10 +104,10 @@ template <int W> __device__ __forceinline__ uint32_t row_max(uint32_t v, float *
     return v;
 }
 
-// W wavefronts per row (W = 1: four rows per block of 256 threads), NP pieces per lane.
+// W wavefronts per row (W = 1: four rows per block of 256 threads), NP pieces per lane.  sum and y may be x or residual: a row's
+// owners have all of it in registers before the first of them stores, and nothing tells the compiler that the arrays are apart.
 template <typename T, bool ALIGNED, int W, int NP, bool QUANT>
-__global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_kernel(const T *__restrict__ x, const T *__restrict__ residual,
-                                                                         const T *__restrict__ w, T *__restrict__ sum, T *__restrict__ y,
+__global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_kernel(const T *x, const T *residual, const T *__restrict__ w, T *sum, T *y,
                                                                          uint8_t *__restrict__ yq, float *__restrict__ yscale, int rows,
                                                                          int d, float eps)
 {
@@ -342,6 +343,7 @@ template <typename T, typename F> static hipError_t pick_row(int d, const F &f)
     return d % V == 0 ? go(std::true_type()) : go(std::false_type());
 }
 
+constexpr int kNormLaunchBlocks = 1 << 21;   // a launch ends below 2^32 threads: more rows than these blocks hold are several launches
 struct ForwardCall {
     static constexpr bool kWide = false;
     const void *x, *residual, *w;
@@ -353,15 +355,22 @@ struct ForwardCall {
     hipStream_t s;
     template <typename T, bool A, int W, int NP> hipError_t run() const
     {
-        const unsigned blocks = W == 1 ? (unsigned)((rows + 3ll) / 4) : (unsigned)rows;
-        const int threads = W == 16 ? 1024 : 256;
-        if (yq)
-            add_rmsnorm_kernel<T, A, W, NP, true><<<blocks, threads, 0, s>>>((const T *)x, (const T *)residual, (const T *)w, (T *)sum, (T *)y,
-                                                                           yq, yscale, rows, d, eps);
-        else
-            add_rmsnorm_kernel<T, A, W, NP, false><<<blocks, threads, 0, s>>>((const T *)x, (const T *)residual, (const T *)w, (T *)sum, (T *)y,
-                                                                            nullptr, nullptr, rows, d, eps);
-        return hipGetLastError();
+        constexpr int threads = W == 16 ? 1024 : 256, per_block = W == 1 ? 4 : 1, most = kNormLaunchBlocks * per_block;
+        for (int first = 0;;) {
+            const int n = rows - first < most ? rows - first : most;
+            const unsigned blocks = (unsigned)((n + per_block - 1) / per_block);
+            const size_t at = (size_t)first * d;
+            const T *r = residual ? (const T *)residual + at : nullptr;
+            T *so = sum ? (T *)sum + at : nullptr, *yo = y ? (T *)y + at : nullptr;
+            if (yq)
+                add_rmsnorm_kernel<T, A, W, NP, true><<<blocks, threads, 0, s>>>((const T *)x + at, r, (const T *)w, so, yo, yq + at, yscale + first, n,
+                                                                               d, eps);
+            else
+                add_rmsnorm_kernel<T, A, W, NP, false><<<blocks, threads, 0, s>>>((const T *)x + at, r, (const T *)w, so, yo, nullptr, nullptr, n, d, eps);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || rows - first <= most) return e;
+            first += most;
+        }
     }
 };
 

@@ -180,3 +180,27 @@ def test_rows_behind_the_last_are_left_alone(B):
     s, y = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
     B.slicemoe_add_rmsnorm(B.make_norm_config(T, d, 1e-5, "bf16"), x, x, w, s, y)
     assert bool((s[T:] == 7).all()) and bool((y[T:] == 7).all()) and not bool((y[:T] == 7).all())
+
+
+def test_more_rows_than_one_launch_holds(B):
+    """A wavefront per row: 2^26 rows are 2^32 threads.  Rows of one value against the formula in 64 bits, all of them."""
+    T, eps = (1 << 26) + 5, 0.25
+    cfg = B.make_norm_config(T, 1, eps, "bf16")
+    x = torch.empty((T, 1), dtype=B16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    w = torch.full((1,), 1.5, dtype=B16, device="cuda")
+    y, s = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    q, sc = torch.zeros((T, 1), dtype=torch.uint8, device="cuda"), torch.full((T,), 7.0, device="cuda")
+    B.slicemoe_add_rmsnorm(cfg, x, None, w, s, y)
+    B.slicemoe_add_rmsnorm(cfg, x, x, w, None, None, y_quantized=q, y_scale=sc)
+    torch.cuda.synchronize()
+    assert torch.equal(s, x)
+    for a in range(0, T, 1 << 24):
+        rows = slice(a, min(T, a + (1 << 24)))
+        v = x[rows].double()
+        ref = v / (v * v + eps).sqrt() * 1.5
+        # storage, and some ten fp32 roundings
+        assert bool(((y[rows].double() - ref).abs() <= ref.abs() * (2.0 ** -8 + 10 * 2.0 ** -24)).all())
+        ref = 2 * v / (4 * v * v + eps).sqrt() * 1.5
+        got = q[rows].view(torch.float8_e4m3fn).float().double() * sc[rows, None].double()
+        # its own largest value: 448 of its scale but for fp32 roundings, which may bring the quotient no further than the neighbour's half step
+        assert bool(((got - ref).abs() <= ref.abs() * (2.0 ** -4 + 16 * 2.0 ** -24)).all())
