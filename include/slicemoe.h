@@ -442,7 +442,7 @@ slicemoe_status slicemoe_gated_ffn_quantize_weights(const slicemoe_gated_config 
  * factor = min(1, max_norm / (norm + 1e-6)), out = g * factor, rounded once to the tensor's dtype.  A norm that is not finite
  * carries into the factor as the formula says (NaN, or 0).
  *   grads     HOST array of `count` tensors, read during the call; count may be 0
- *   max_norm  >= 0; INFINITY only measures (factor 1)
+ *   max_norm  >= 0; INFINITY only measures (factor 1, whatever the norm)
  *   norm      out float, 4-byte aligned
  *   workspace >= slicemoe_clip_grads_workspace_bytes(grads, count) (0 on invalid arguments), 256-byte aligned
  * out of a tensor may be its own grad (in place), or NULL (the tensor is measured, not written).  INVALID_ARG if any out overlaps

@@ -1,6 +1,6 @@
 // Global norm of a list of gradient tensors, and its bounding.
 //
-//   norm = sqrt(sum over all tensors of g^2),   factor = min(1, max_norm / (norm + 1e-6)),   out = g factor
+//   norm = sqrt(sum over all tensors of g^2),   factor = min(1, max_norm / (norm + 1e-6)), 1 if max_norm is infinite,   out = g factor
 //
 // Two launches per kTensors tensors: every block squares and sums one chunk of one tensor, then every block adds up all chunks'
 // sums (about eight thousand at most, from L2, the same order in every block and every run) and scales its chunk.  Squares and sums are
@@ -146,7 +146,7 @@ template <bool BF16> __device__ __forceinline__ void scale_chunk(const ClipTable
     for (int k = 0; k < AHEAD; ++k)
         if (i - k * kClipThreads >= 0) p[k] = ((const loose *)base)[i - k * kClipThreads];
     const float norm = total_norm(part, parts, lds);
-    const float q = max_norm / (norm + 1e-6f), f = q > 1.f ? 1.f : q;   // (a NaN stays one)
+    const float q = max_norm / (norm + 1e-6f), f = q > 1.f || max_norm == INFINITY ? 1.f : q;   // (a NaN stays one; inf / inf does not)
     if (norm_out && threadIdx.x == 0) *norm_out = norm;
     if (!out || (f == 1.f && t.out[c.tensor] == t.in[c.tensor])) return;
     out += c.begin * EL;

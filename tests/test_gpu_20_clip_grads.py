@@ -102,3 +102,18 @@ def test_nothing(B):
     assert norm == 0.0
     norm, out = clip(B, [torch.zeros(1000, device="cuda")], 0.0)   # factor 0 / 1e-6
     assert norm == 0.0 and bool((out[0] == 0).all())
+
+
+def test_an_infinite_bound_leaves_every_value(B):
+    """factor 1 also where the norm is infinite or NaN: copies to the last bit, and the tensors themselves in place."""
+    for bad in (math.nan, math.inf):
+        grads = tensors([(500, F32), (300, B16)], 3)
+        grads[0][77] = bad
+        norm, out = clip(B, grads, math.inf)
+        assert not math.isfinite(norm)
+        for g, o in zip(grads, out):
+            fine = torch.isfinite(g)
+            assert torch.equal(o[fine], g[fine]) and torch.equal(torch.isnan(o), torch.isnan(g)) and torch.equal(torch.isinf(o), torch.isinf(g))
+        held = [g.clone() for g in grads]
+        clip(B, held, math.inf, out=held)
+        assert all(torch.equal(h.view(torch.uint8), g.view(torch.uint8)) for h, g in zip(held, grads))
