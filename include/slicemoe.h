@@ -372,7 +372,7 @@ slicemoe_status slicemoe_add_rmsnorm_backward(const slicemoe_norm_config *cfg, c
                                               size_t workspace_bytes, slicemoe_stream_t stream);
 
 typedef struct {
-    int32_t T;     /* rows (tokens), 0 <= T < 2^30                                           */
+    int32_t T;     /* rows (tokens), 0 <= T <= 2^29                                          */
     int32_t d;     /* row width, 1 <= d <= 2^20                                              */
     int32_t H;     /* hidden width, 1 <= H <= 2^20; T * max(d, H) <= 2^40                    */
     int32_t dtype; /* slicemoe_dtype                                                         */

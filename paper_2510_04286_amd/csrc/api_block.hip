@@ -26,8 +26,8 @@ static slicemoe_status validate(const slicemoe_norm_config *c)
 static slicemoe_status validate(const slicemoe_gated_config *c)
 {
     if (!c || c->T < 0 || c->d < 1 || c->H < 1 || !storage_ok(c->dtype)) return SLICEMOE_ERR_INVALID_ARG;
-    // row offsets inside a tile are 32 bits, the contraction over T counts bytes in 31, tiles are counted in 31
-    if (c->T >= 1 << 30 || c->d > 1 << 20 || c->H > 1 << 20) return SLICEMOE_ERR_UNSUPPORTED;
+    // row offsets inside a tile are 32 bits, the contraction over T counts its bytes and the step beyond them in 31, tiles are counted in 31
+    if (c->T > 1 << 29 || c->d > 1 << 20 || c->H > 1 << 20) return SLICEMOE_ERR_UNSUPPORTED;
     return (long long)c->T * std::max(c->d, c->H) > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
 static slicemoe_status validate_quantized(const slicemoe_gated_config *c)

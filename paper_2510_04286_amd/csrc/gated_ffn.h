@@ -12,7 +12,7 @@ struct GatedPlan {
     bool copy_x, copy_h;                    // rows of d / of H are copied
     int ldd, ldh;                           // elements per row of d / H in the copies and in the hidden arrays
     size_t a, dg, du;                       // [terms][T][ldh]
-    size_t part, part_bytes;                // partial sums of split contractions
+    size_t part;                            // partial sums of split contractions
     size_t total;
 };
 GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantized);

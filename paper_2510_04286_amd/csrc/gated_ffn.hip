@@ -676,7 +676,6 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
     if (!backward) part = std::max(rows_shares(st.down), up_shares(st.up, 2));
     else
         part = std::max(std::max(rows_shares(st.dx), up_shares(st.up + st.up / 2, 3)), 3 * 256 + 2 * share_bytes(cus, 256 * 256, st.dw, d, h8) + share_bytes(cus, 256 * 256, st.dw, H, d8));
-    p.part_bytes = part;
     p.part = take(part);
     p.total = std::max<size_t>(at, 256);
     return p;

@@ -172,3 +172,16 @@ def test_binding_refuses_host_tensors_and_wrong_types(B):
     with pytest.raises(TypeError):
         B.slicemoe_clip_grads_workspace_bytes([None])
     assert math.isinf(INF)
+
+
+def test_the_longest_batch(B):
+    """The contraction over the rows counts bytes, and a step of 128 beyond them, in a signed 32-bit number."""
+    sizes = (B.slicemoe_gated_ffn_workspace_bytes, B.slicemoe_gated_ffn_backward_workspace_bytes, B.slicemoe_gated_ffn_quantized_workspace_bytes)
+    assert 2 * (1 << 29) + 128 < 1 << 31
+    for size in sizes:
+        assert size(B.make_gated_config(1 << 29, 16, 8)) > (1 << 29) * 64 * 2
+        for T in ((1 << 29) + 1, (1 << 30) - 1):
+            assert size(B.make_gated_config(T, 16, 8)) == 0
+    c = B.make_gated_config((1 << 30) - 1, 16, 8)
+    w = B.slicemoe_gated_weights(4096, 4096, 4096)
+    assert B.lib().slicemoe_gated_ffn(by(c), P, by(w), P, P, P, BIG, NULL) == B.SLICEMOE_ERR_UNSUPPORTED
