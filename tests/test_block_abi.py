@@ -179,7 +179,8 @@ def test_the_longest_batch(B):
     sizes = (B.slicemoe_gated_ffn_workspace_bytes, B.slicemoe_gated_ffn_backward_workspace_bytes, B.slicemoe_gated_ffn_quantized_workspace_bytes)
     assert 2 * (1 << 29) + 128 < 1 << 31
     for size in sizes:
-        assert size(B.make_gated_config(1 << 29, 16, 8)) > (1 << 29) * 64 * 2
+        # the hidden rows at least, T x 64 bf16 values; nothing else forward, whose contractions of one step have no shares
+        assert size(B.make_gated_config(1 << 29, 16, 8)) >= (1 << 29) * 64 * 2
         for T in ((1 << 29) + 1, (1 << 30) - 1):
             assert size(B.make_gated_config(T, 16, 8)) == 0
     c = B.make_gated_config((1 << 30) - 1, 16, 8)
