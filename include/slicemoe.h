@@ -332,7 +332,8 @@ slicemoe_status slicemoe_backward(const slicemoe_config *cfg, const void *h, con
  * conventions above hold for these entry points too: caller-allocated device memory, 16-byte aligned unless it says otherwise,
  * kernels on `stream` only (nothing here uses another stream), no allocation, no host synchronisation, bit-identical
  * results for the same inputs, and calls may be captured into a HIP graph.  Calls that overlap in time need workspaces of
- * their own.  Arrays are contiguous; an output may take an input's place only where that is said.
+ * their own.  Arrays are contiguous and on the current device, which is the stream's; an output may take an input's place
+ * only where that is said.
  */
 typedef struct {
     int32_t T;     /* rows (tokens), 0 <= T                                                  */

@@ -177,11 +177,13 @@ def config_of(shape, flags=0) -> slicemoe_config:
 
 # A small batch is bound by this marshalling and the launches (32 tokens of the d=1024 layer: 10 of 24 us), so the checks of a tensor
 # are one pass over its attributes, addresses travel as integers, and the stream is asked for as a raw handle.
-def _ptr(t, dtype=None, numel=None, name="tensor"):
-    """Device address of a checked tensor; None for None."""
+def _ptr(t, dtype=None, numel=None, name="tensor", dev=None):
+    """Device address of a checked tensor; None for None.  dev: the device that it has to be on."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or (not t.is_cuda if dev is None else t.get_device() != dev):
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
         raise TypeError(f"{name} must be a CUDA/HIP tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -221,10 +223,10 @@ def _weights(cfg, w) -> slicemoe_weights:
         None if pk is None else _ptr(pk, torch.uint8, (_lib or lib()).slicemoe_packed_bytes(ctypes.byref(cfg)), "packed"))
 
 
-def _ws(workspace):
+def _ws(workspace, dev=None):
     if workspace is None:
         return None, 0
-    return _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel()
+    return _ptr(workspace, torch.uint8, None, "workspace", dev), workspace.numel()
 
 
 def _check(status, what):
@@ -422,21 +424,38 @@ def make_gated_config(T, d, H, dtype="bf16") -> slicemoe_gated_config:
     return slicemoe_gated_config(T, d, H, _dtype_code(dtype))
 
 
-def _bytes_ptr(t, numel, name):
+def _device():
+    """The current device.  Kernels go to it, so the tensors and the stream of a call have to be on it: another card's memory need not be
+    reachable from here, and a launch that reaches for it all the same takes the process down."""
+    try:
+        return torch._C._cuda_getDevice()
+    except (AttributeError, RuntimeError):   # no GPU: no tensor is on it
+        return -2
+
+
+def _stream_on(dev, stream):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"stream is of device {stream.device_index}, the current device is {dev}")
+    return stream.cuda_stream
+
+
+def _bytes_ptr(t, numel, name, dev):
     """Address of e4m3 values: a float8_e4m3fn tensor, or its bytes."""
     if t is not None and isinstance(t, torch.Tensor) and t.dtype == torch.uint8:
-        return _ptr(t, torch.uint8, numel, name)
-    return _ptr(t, torch.float8_e4m3fn, numel, name)
+        return _ptr(t, torch.uint8, numel, name, dev)
+    return _ptr(t, torch.float8_e4m3fn, numel, name, dev)
 
 
 def slicemoe_add_rmsnorm(cfg, x, residual, weight, sum_out, y, y_quantized=None, y_scale=None, stream=None):
     """residual, sum_out and, with y_quantized, y may be None."""
-    d, T = cfg.d, cfg.T
+    d, T, dev = cfg.d, cfg.T, _device()
     dt, n = _tdtype(cfg), T * d
     st = (_lib or lib()).slicemoe_add_rmsnorm(
-        ctypes.byref(cfg), _ptr(x, dt, n, "x"), _ptr(residual, dt, n, "residual"), _ptr(weight, dt, d, "weight"),
-        _ptr(sum_out, dt, n, "sum_out"), _ptr(y, dt, n, "y"), None if y_quantized is None else _bytes_ptr(y_quantized, n, "y_quantized"),
-        None if y_scale is None else _ptr(y_scale, torch.float32, T, "y_scale"), _stream(stream))
+        ctypes.byref(cfg), _ptr(x, dt, n, "x", dev), _ptr(residual, dt, n, "residual", dev), _ptr(weight, dt, d, "weight", dev),
+        _ptr(sum_out, dt, n, "sum_out", dev), _ptr(y, dt, n, "y", dev), None if y_quantized is None else _bytes_ptr(y_quantized, n, "y_quantized", dev),
+        None if y_scale is None else _ptr(y_scale, torch.float32, T, "y_scale", dev), _stream_on(dev, stream))
     if st:
         _check(st, "slicemoe_add_rmsnorm")
 
@@ -446,11 +465,11 @@ def slicemoe_add_rmsnorm_backward_workspace_bytes(cfg) -> int:
 
 
 def slicemoe_add_rmsnorm_backward(cfg, sum_in, weight, d_y, d_x, d_weight, workspace, d_sum=None, stream=None):
-    dt, n = _tdtype(cfg), cfg.T * cfg.d
-    wsp, wsb = _ws(workspace)
-    _check(lib().slicemoe_add_rmsnorm_backward(ctypes.byref(cfg), _ptr(sum_in, dt, n, "sum_in"), _ptr(weight, dt, cfg.d, "weight"),
-                                               _ptr(d_y, dt, n, "d_y"), _ptr(d_sum, dt, n, "d_sum"), _ptr(d_x, dt, n, "d_x"),
-                                               _ptr(d_weight, torch.float32, cfg.d, "d_weight"), wsp, wsb, _stream(stream)),
+    dt, n, dev = _tdtype(cfg), cfg.T * cfg.d, _device()
+    wsp, wsb = _ws(workspace, dev)
+    _check(lib().slicemoe_add_rmsnorm_backward(ctypes.byref(cfg), _ptr(sum_in, dt, n, "sum_in", dev), _ptr(weight, dt, cfg.d, "weight", dev),
+                                               _ptr(d_y, dt, n, "d_y", dev), _ptr(d_sum, dt, n, "d_sum", dev), _ptr(d_x, dt, n, "d_x", dev),
+                                               _ptr(d_weight, torch.float32, cfg.d, "d_weight", dev), wsp, wsb, _stream_on(dev, stream)),
            "slicemoe_add_rmsnorm_backward")
 
 
@@ -466,47 +485,47 @@ def slicemoe_gated_ffn_quantized_workspace_bytes(cfg) -> int:
     return lib().slicemoe_gated_ffn_quantized_workspace_bytes(ctypes.byref(cfg))
 
 
-def _gated_weights(cfg, w, kind=slicemoe_gated_weights, what="", down=True):
+def _gated_weights(cfg, w, dev, kind=slicemoe_gated_weights, what="", down=True):
     dt, n = _tdtype(cfg), cfg.d * cfg.H
-    return kind(_ptr(w["Wg"], dt, n, what + "Wg"), _ptr(w["Wu"], dt, n, what + "Wu"), _ptr(w["Wd"], dt, n, what + "Wd") if down else None)
+    return kind(_ptr(w["Wg"], dt, n, what + "Wg", dev), _ptr(w["Wu"], dt, n, what + "Wu", dev), _ptr(w["Wd"], dt, n, what + "Wd", dev) if down else None)
 
 
 def slicemoe_gated_ffn(cfg, x, w, y, workspace, addend=None, stream=None):
     """w: dict of Wg, Wu [d, H] and Wd [H, d]."""
-    dt, n = _tdtype(cfg), cfg.T * cfg.d
-    wsp, wsb = _ws(workspace)
-    ws = _gated_weights(cfg, w)
-    _check(lib().slicemoe_gated_ffn(ctypes.byref(cfg), _ptr(x, dt, n, "x"), ctypes.byref(ws), _ptr(addend, dt, n, "addend"),
-                                    _ptr(y, dt, n, "y"), wsp, wsb, _stream(stream)), "slicemoe_gated_ffn")
+    dt, n, dev = _tdtype(cfg), cfg.T * cfg.d, _device()
+    wsp, wsb = _ws(workspace, dev)
+    ws = _gated_weights(cfg, w, dev)
+    _check(lib().slicemoe_gated_ffn(ctypes.byref(cfg), _ptr(x, dt, n, "x", dev), ctypes.byref(ws), _ptr(addend, dt, n, "addend", dev),
+                                    _ptr(y, dt, n, "y", dev), wsp, wsb, _stream_on(dev, stream)), "slicemoe_gated_ffn")
 
 
 def slicemoe_gated_ffn_backward(cfg, x, w, d_y, d_x, grads, workspace, addend=None, stream=None):
     """grads: dict of Wg, Wu, Wd in the storage dtype, overwritten."""
-    dt, n = _tdtype(cfg), cfg.T * cfg.d
-    wsp, wsb = _ws(workspace)
-    ws, g = _gated_weights(cfg, w), _gated_weights(cfg, grads, slicemoe_gated_weight_grads, "grads.")
-    _check(lib().slicemoe_gated_ffn_backward(ctypes.byref(cfg), _ptr(x, dt, n, "x"), ctypes.byref(ws), _ptr(d_y, dt, n, "d_y"),
-                                             _ptr(addend, dt, n, "addend"), _ptr(d_x, dt, n, "d_x"), ctypes.byref(g), wsp, wsb,
-                                             _stream(stream)), "slicemoe_gated_ffn_backward")
+    dt, n, dev = _tdtype(cfg), cfg.T * cfg.d, _device()
+    wsp, wsb = _ws(workspace, dev)
+    ws, g = _gated_weights(cfg, w, dev), _gated_weights(cfg, grads, dev, slicemoe_gated_weight_grads, "grads.")
+    _check(lib().slicemoe_gated_ffn_backward(ctypes.byref(cfg), _ptr(x, dt, n, "x", dev), ctypes.byref(ws), _ptr(d_y, dt, n, "d_y", dev),
+                                             _ptr(addend, dt, n, "addend", dev), _ptr(d_x, dt, n, "d_x", dev), ctypes.byref(g), wsp, wsb,
+                                             _stream_on(dev, stream)), "slicemoe_gated_ffn_backward")
 
 
 def slicemoe_gated_ffn_quantized(cfg, x_quantized, x_scale, w, y, workspace, addend=None, stream=None):
     """w: dict of Wg, Wu [H, d] e4m3 with Wg_scale, Wu_scale [H], and Wd [H, d] bf16 (see quantize_gated_weights)."""
-    n, nw, f32 = cfg.T * cfg.d, cfg.d * cfg.H, torch.float32
-    wsp, wsb = _ws(workspace)
-    ws = slicemoe_gated_weights_quantized(_bytes_ptr(w["Wg"], nw, "Wg"), _bytes_ptr(w["Wu"], nw, "Wu"), _ptr(w["Wg_scale"], f32, cfg.H, "Wg_scale"),
-                                          _ptr(w["Wu_scale"], f32, cfg.H, "Wu_scale"), _ptr(w["Wd"], torch.bfloat16, nw, "Wd"))
-    _check(lib().slicemoe_gated_ffn_quantized(ctypes.byref(cfg), _bytes_ptr(x_quantized, n, "x_quantized"), _ptr(x_scale, f32, cfg.T, "x_scale"),
-                                              ctypes.byref(ws), _ptr(addend, torch.bfloat16, n, "addend"),
-                                              _ptr(y, torch.bfloat16, n, "y"), wsp, wsb, _stream(stream)), "slicemoe_gated_ffn_quantized")
+    n, nw, f32, dev = cfg.T * cfg.d, cfg.d * cfg.H, torch.float32, _device()
+    wsp, wsb = _ws(workspace, dev)
+    ws = slicemoe_gated_weights_quantized(_bytes_ptr(w["Wg"], nw, "Wg", dev), _bytes_ptr(w["Wu"], nw, "Wu", dev), _ptr(w["Wg_scale"], f32, cfg.H, "Wg_scale", dev),
+                                          _ptr(w["Wu_scale"], f32, cfg.H, "Wu_scale", dev), _ptr(w["Wd"], torch.bfloat16, nw, "Wd", dev))
+    _check(lib().slicemoe_gated_ffn_quantized(ctypes.byref(cfg), _bytes_ptr(x_quantized, n, "x_quantized", dev), _ptr(x_scale, f32, cfg.T, "x_scale", dev),
+                                              ctypes.byref(ws), _ptr(addend, torch.bfloat16, n, "addend", dev),
+                                              _ptr(y, torch.bfloat16, n, "y", dev), wsp, wsb, _stream_on(dev, stream)), "slicemoe_gated_ffn_quantized")
 
 
 def slicemoe_gated_ffn_quantize_weights(cfg, w, Wg, Wg_scale, Wu, Wu_scale, stream=None):
-    nw, f32 = cfg.d * cfg.H, torch.float32
-    ws = _gated_weights(cfg, w, down=False)
-    _check(lib().slicemoe_gated_ffn_quantize_weights(ctypes.byref(cfg), ctypes.byref(ws), _bytes_ptr(Wg, nw, "Wg"),
-                                                     _ptr(Wg_scale, f32, cfg.H, "Wg_scale"), _bytes_ptr(Wu, nw, "Wu"),
-                                                     _ptr(Wu_scale, f32, cfg.H, "Wu_scale"), _stream(stream)),
+    nw, f32, dev = cfg.d * cfg.H, torch.float32, _device()
+    ws = _gated_weights(cfg, w, dev, down=False)
+    _check(lib().slicemoe_gated_ffn_quantize_weights(ctypes.byref(cfg), ctypes.byref(ws), _bytes_ptr(Wg, nw, "Wg", dev),
+                                                     _ptr(Wg_scale, f32, cfg.H, "Wg_scale", dev), _bytes_ptr(Wu, nw, "Wu", dev),
+                                                     _ptr(Wu_scale, f32, cfg.H, "Wu_scale", dev), _stream_on(dev, stream)),
            "slicemoe_gated_ffn_quantize_weights")
 
 
@@ -520,27 +539,28 @@ def quantize_gated_weights(cfg, w: dict, device="cuda:0") -> dict:
 
 _GRAD_CODES = {torch.float32: SLICEMOE_F32, torch.bfloat16: SLICEMOE_BF16}
 _GRAD_FIELDS = "QQqi4x"   # slicemoe_grad
-_dtype_of, _on_gpu = operator.attrgetter("dtype"), operator.attrgetter("is_cuda")
+_dtype_of = operator.attrgetter("dtype")
 
 
-def _check_list(tensors, name):
+def _check_list(tensors, name, dev):
     for i, t in enumerate(tensors):
         if t is None:
             raise TypeError(f"{name}[{i}] must be a CUDA/HIP tensor")
-        _ptr(t, None, None, f"{name}[{i}]")
+        _ptr(t, None, None, f"{name}[{i}]", dev)
 
 
-def _grad_list(grads, out):
+def _grad_list(grads, out, dev=None):
     """C array of a list of gradient tensors; out: the list written, the same list for in place, or None to measure only.  (One
     attribute of all tensors at a time: dozens of small tensors are bound by this marshalling, 40 us for 48 of them tensor by tensor, 25 so.)"""
     T = torch.Tensor
     for tensors, name in ((grads, "grads"),) if out is None or out is grads else ((grads, "grads"), (out, "out")):
         try:
-            fine = all(map(T.is_contiguous, tensors)) and all(map(_on_gpu, tensors))
+            on = set(map(T.get_device, tensors))
+            fine = all(map(T.is_contiguous, tensors)) and (-1 not in on if dev is None else on <= {dev})   # (-1: host memory)
         except TypeError:   # not a tensor
             fine = False
         if not fine:
-            _check_list(tensors, name)   # raises
+            _check_list(tensors, name, dev)   # raises
     types, sizes, addresses = list(map(_dtype_of, grads)), list(map(T.numel, grads)), list(map(T.data_ptr, grads))
     codes = list(map(_GRAD_CODES.get, types))
     if None in codes:
@@ -567,10 +587,11 @@ def slicemoe_clip_grads_workspace_bytes(grads) -> int:
 
 def slicemoe_clip_grads(grads, max_norm, norm, workspace, out=None, stream=None):
     """out: the tensors written (grads itself for in place); None leaves all of them as they are and only measures."""
-    wsp, wsb = _ws(workspace)
-    packed = _grad_list(grads, out)
-    _check(lib().slicemoe_clip_grads(_grad_pointer(packed), len(grads), max_norm, _ptr(norm, torch.float32, 1, "norm"), wsp, wsb,
-                                     _stream(stream)), "slicemoe_clip_grads")
+    dev = _device()
+    wsp, wsb = _ws(workspace, dev)
+    packed = _grad_list(grads, out, dev)
+    _check(lib().slicemoe_clip_grads(_grad_pointer(packed), len(grads), max_norm, _ptr(norm, torch.float32, 1, "norm", dev), wsp, wsb,
+                                     _stream_on(dev, stream)), "slicemoe_clip_grads")
 
 
 # ------------------------------------------------------------------ plumbing helpers (device memory only)

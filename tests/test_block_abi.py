@@ -186,3 +186,27 @@ def test_the_longest_batch(B):
     c = B.make_gated_config((1 << 30) - 1, 16, 8)
     w = B.slicemoe_gated_weights(4096, 4096, 4096)
     assert B.lib().slicemoe_gated_ffn(by(c), P, by(w), P, P, P, BIG, NULL) == B.SLICEMOE_ERR_UNSUPPORTED
+
+
+class OnDevice:
+    """A tensor's face: what the binding asks of one."""
+    is_cuda = True
+
+    def __init__(self, index):
+        self.index = index
+
+    def get_device(self):
+        return self.index
+
+
+def test_binding_refuses_a_stream_of_another_device(B, monkeypatch):
+    class Stream:
+        cuda_stream, device_index = 4096, 1
+    assert B._stream_on(1, Stream()) == 4096
+    with pytest.raises(ValueError, match="device 1"):
+        B._stream_on(0, Stream())
+    import torch
+    monkeypatch.setattr(B.torch, "Tensor", OnDevice)
+    with pytest.raises(ValueError, match="is on device 1, the current device is 0"):
+        B._ptr(OnDevice(1), None, None, "x", 0)
+    assert isinstance(OnDevice(1), torch.Tensor)

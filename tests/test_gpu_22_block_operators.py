@@ -337,3 +337,31 @@ def test_offsets_beyond_32_bits(B):
         want += xc.t() @ ((yc @ Wd.t()) * up * (sg + gate * sg * (1 - sg)))
     # the rounding of dg to bf16, 2^-8 of each of 1.1 million terms of either sign, and of the result
     assert float((g["Wg"].double() - want).norm()) <= 3 * 2.0 ** -8 * float(want.norm())
+
+
+def test_arrays_of_another_device_are_refused(B, monkeypatch):
+    """With another device current, kernels would reach for this one's memory from there: every call ends in the binding.  (The current
+    device is what the binding is told; nothing is launched.)"""
+    o = Gated(B, 40, 64, 96)
+    ncfg, v = B.make_norm_config(40, 64), torch.empty(64, device="cuda")
+    nws, norm = space(B.slicemoe_add_rmsnorm_backward_workspace_bytes(ncfg)), torch.full((1,), 7.0, device="cuda")
+    q8 = B.quantize_gated_weights(o.cfg, o.w)
+    x8, sc = torch.zeros((40, 64), dtype=torch.float8_e4m3fn, device="cuda"), torch.ones(40, device="cuda")
+    cws = space(B.slicemoe_clip_grads_workspace_bytes([o.x]))
+    before = [t.clone() for t in (*o.out(), norm, v)]
+    held = torch.cuda.current_stream()
+    calls = [lambda: B.slicemoe_add_rmsnorm(ncfg, o.x, None, o.w["Wg"][0], None, o.y), o.run, lambda: o.run(held),
+             lambda: B.slicemoe_add_rmsnorm_backward(ncfg, o.x, o.w["Wg"][0], o.dy, o.dx, v, nws),
+             lambda: B.slicemoe_gated_ffn_backward(o.cfg, o.x, o.w, o.dy, o.dx, o.g, o.bws),
+             lambda: B.slicemoe_gated_ffn_quantized(o.cfg, x8, sc, q8, o.y, o.ws), lambda: B.quantize_gated_weights(o.cfg, o.w),
+             lambda: B.slicemoe_clip_grads([o.x], 1.0, norm, cws), lambda: B.slicemoe_clip_grads([], 1.0, norm, cws)]
+    with monkeypatch.context() as m:
+        m.setattr(B, "_device", lambda: 1)
+        for call in calls:
+            with pytest.raises(ValueError, match="current device is 1"):
+                call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((*o.out(), norm, v), before))
+    for call in calls[:1] + calls[3:]:
+        call()   # the same calls where they belong
+    torch.cuda.synchronize()
