@@ -393,9 +393,10 @@ typedef struct {
  *   x [T, d] in;  addend [T, d] in, may be NULL (zero);  y [T, d] out, may be addend or x
  *   workspace >= slicemoe_gated_ffn_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; its size never falls as T
  *             grows
- * All products run on the bf16 matrix cores with fp32 accumulation.  bf16 storage: the hidden row silu(g) u is rounded to bf16
+ * Products run on the bf16 matrix cores with fp32 accumulation.  bf16 storage: the hidden row silu(g) u is rounded to bf16
  * once between the products.  fp32 storage: every operand enters as three bf16 terms that keep its 24 bits, results of fp32 grade;
- * an infinity in an operand may come out as NaN.  Widths that are not multiples of 8 (and fp32) are laid out again in the workspace first.
+ * an infinity in an operand may come out as NaN; a forward pass of up to 256 fp32 rows runs on the fp32 matrix instruction instead.
+ * Widths that are not multiples of 8 (and fp32, but for those) are laid out again in the workspace first.
  * A row's result does not depend on the other rows, but the order of its sums depends on T.
  */
 size_t slicemoe_gated_ffn_workspace_bytes(const slicemoe_gated_config *cfg);

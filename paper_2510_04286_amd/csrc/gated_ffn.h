@@ -13,6 +13,7 @@ struct GatedPlan {
     int ldd, ldh;                           // elements per row of d / H in the copies and in the hidden arrays
     size_t a, dg, du;                       // [terms][T][ldh]
     size_t part;                            // partial sums of split contractions
+    bool few_f32;                           // fp32 rows few enough to multiply as they are: nothing but fp32 hidden rows and part
     size_t total;
 };
 GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantized);

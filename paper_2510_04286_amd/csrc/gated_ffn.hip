@@ -25,7 +25,8 @@ namespace slicemoe {
 // ---- fp32 values as bf16 terms -------------------------------------------------------------------------------------------
 // fp32 storage: an operand is the sum of three bf16 values, cut off rather than rounded, so that the first two remainders are exact
 // and all 24 bits are kept.  A product is the six products of terms whose orders add up to at most two, largest first (the matrix
-// instruction cuts its accumulator when the products outweigh it); what is left out is below 2^-24 of the product.
+// instruction cuts its accumulator when the products outweigh it); what is left out is below 2^-24 of the product.  (A forward pass
+// of few rows is bound by the weights and takes the fp32 instruction instead: see gated_few_f32_kernel.)
 // Six bf16 products run at 2.6 times the rate of the fp32 matrix instruction; errors against 64 bits 4e-7 (the library's fp32
 // product: 7e-7).
 constexpr int kPairs = 6;
@@ -196,10 +197,16 @@ struct Hidden {
     bf16_t *p[3];         // a, dg, du: [terms][rows][ld]
     int rows, cols, ld;
 };
+constexpr int kAsF32 = 4;   // in place of a number of terms: rows of fp32 values
 template <int TERMS> __device__ __forceinline__ void put_hidden(const Hidden &h, int which, int row, int col, const float *v)
 {
     if (row >= h.rows || col >= h.cols) return;
-    store_terms<TERMS>(h.p[which] + (size_t)row * h.ld, (size_t)h.rows * h.ld, col, h.cols, v);
+    if constexpr (TERMS == kAsF32) {   // (past the row's end, in its padding, is not read)
+        float *q = (float *)h.p[which] + (size_t)row * h.ld + col;
+        *(f32x4 *)q = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4 *)(q + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else
+        store_terms<TERMS>(h.p[which] + (size_t)row * h.ld, (size_t)h.rows * h.ld, col, h.cols, v);
 }
 
 struct Scales {
@@ -330,7 +337,7 @@ __global__ __launch_bounds__(256) void gated_up_sum_kernel(const float *__restri
                 g *= sc.x[row] * sc.g[c];
                 u *= sc.x[row] * sc.u[c];
             }
-            const float sg = sigmoid<TERMS == 3>(g), s = g * sg;
+            const float sg = sigmoid<TERMS >= 3>(g), s = g * sg;
             v[0][i] = s * u;
             if constexpr (IMAGES == 3) {
                 const float d = v[2][i];
@@ -346,7 +353,7 @@ __global__ __launch_bounds__(256) void gated_up_sum_kernel(const float *__restri
 // The same for few rows: bound by the weights' arrival (T 16, d 4096, H 11008 in 8 bits: 90 MB in 23 us; T 32, d 1024, H 2816 in bf16: 8 us,
 // two round trips and the launch).  Against 128-feature tiles whose contraction was shared out over blocks and added up by a second kernel:
 // 24 and 12 us.
-template <typename S, int TERMS> __global__ __launch_bounds__(256) void gated_up_few_kernel(GemmProblem p, Hidden h, Scales sc)
+template <typename S> __global__ __launch_bounds__(256) void gated_up_few_kernel(GemmProblem p, Hidden h, Scales sc)
 {
     extern __shared__ __align__(1024) char lds[];
     const TilePlace at = tile_of(blockIdx.x, p.tiles_r, p.tiles_f, 1);
@@ -363,9 +370,9 @@ template <typename S, int TERMS> __global__ __launch_bounds__(256) void gated_up
                 g *= sc.x[row] * sc.g[k];
                 u *= sc.x[row] * sc.u[k];
             }
-            a[i] = g * sigmoid<TERMS == 3>(g) * u;
+            a[i] = g * sigmoid<false>(g) * u;
         }
-        put_hidden<TERMS>(h, 0, row, col, a);
+        put_hidden<1>(h, 0, row, col, a);
     });
 }
 
@@ -427,6 +434,111 @@ template <typename S> __global__ __launch_bounds__(256) void gated_product_few_k
         o = {ps.part[0] + (size_t)at.split * o.rows * ld, nullptr, o.rows, ld, 1};
     }
     few_rows<S>(p, row0, f0, s0, s1, lds, [&](int r, int c, const float (&v)[1][8]) { put_out(o, row0 + r, f0 + c, v[0]); });
+}
+
+// fp32 with few rows: part[split][image][rows][ldp] = x W for one or two matrices [K][N], on the fp32 matrix instruction, which reads the
+// weights where they are (laid out as terms first they cross memory twice more).  It takes one value of k per lane, so a lane's 16 bytes of
+// a row of W are four feature tiles (tile t has the features 4 i + t of the block's 128) and its 16 bytes of a row of x four
+// instructions: nothing passes through the LDS but the four wavefronts' sums.  A wavefront takes 32 values of k in turn with the
+// others (a cache line of x), eight at a time, the next three eights on their way.
+//
+// Bound by memory up to 32 rows: d 4096, H 11008 (541 MB of weights), the whole forward 123 us for one row, 128 for 22 (4.2 TB/s); as terms
+// 574 and 587.  Above by the fp32 matrix instruction, where the terms' copies still cost more: 64 rows 200 against 615, 128 357 against
+// 652, 256 674 against 675; d 1024, H 2816: 22 rows 25 against 53, 128 44 against 62, 256 66 against 73.  Tiles of 64 rows read the
+// weights half as often and fill the chip worse: 22 rows 183, 64 202, 256 622.
+struct FewF32 {
+    const float *x;
+    const float *w[2];
+    float *part;
+    int rows, K, N, ldx, ldp;
+    int images, tiles_r, tiles_f, splits;
+};
+__global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
+{
+    constexpr int SLOTS = 4;
+    __shared__ __align__(16) float sums[4][32][128];   // piece p of row r (four features) at place p ^ r: no bank conflicts
+    const TilePlace at = tile_of(blockIdx.x, a.tiles_r, a.tiles_f * a.images, a.splits);
+    const int image = at.f / a.tiles_f, f0 = (at.f - image * a.tiles_f) * 128, row0 = at.r * 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, half = lane >> 5, col = f0 + 4 * i;
+    const float *w = image ? a.w[1] : a.w[0];
+    const float *x = a.x + (size_t)(row0 + i < a.rows ? row0 + i : a.rows - 1) * a.ldx;
+    f32x16 acc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+
+    // whole eights of k, those of the share [g0, g1); the wavefront's n-th is eight_of(n)
+    const int eights = a.K >> 3, each = (eights + a.splits - 1) / a.splits, g0 = at.split * each, g1 = g0 + each < eights ? g0 + each : eights;
+    const int share = g1 > g0 ? g1 - g0 : 0, rest = (share & 15) - 4 * wave;
+    const int n = (share >> 4) * 4 + (rest < 0 ? 0 : rest > 4 ? 4 : rest);
+    const auto eight_of = [&](int k) { return g0 + (k >> 2) * 16 + wave * 4 + (k & 3); };
+    const auto run = [&](auto edge) {
+        const auto load_w = [&](int k) -> f32x4 {   // (k < K)
+            const float *q = w + (size_t)k * a.N;
+            if (!decltype(edge)::value || col + 4 <= a.N) return __builtin_bit_cast(f32x4, *(const loose *)(q + col));
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < a.N) v[e] = q[col + e];
+            return v;
+        };
+        f32x4 wv[SLOTS][4], xv[SLOTS];
+        const auto request = [&](int slot, int k) {
+            const int k0 = 8 * eight_of(k) + 4 * half;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) wv[slot][j] = load_w(k0 + j);
+            xv[slot] = __builtin_bit_cast(f32x4, *(const loose *)(x + k0));
+        };
+        const auto multiply = [&](int slot) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(wv[slot][j][t], xv[slot][j], acc[t], 0, 0, 0);
+        };
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k)
+            if (k < n) request(k, k);
+        int k = 0;
+        for (; k + 2 * SLOTS <= n; k += SLOTS)
+#pragma unroll
+            for (int c = 0; c < SLOTS; ++c) {
+                multiply(c);
+                request(c, k + SLOTS + c);
+            }
+#pragma unroll
+        for (int c = 0; c < 2 * SLOTS - 1; ++c)
+            if (k + c < n) {
+                multiply(c % SLOTS);
+                if (c < SLOTS && k + SLOTS + c < n) request(c % SLOTS, k + SLOTS + c);
+            }
+        // what is left of k: the last share's first wavefront, zeros past the end in both operands
+        if ((a.K & 7) && at.split == a.splits - 1 && wave == 0) {
+            const int k0 = 8 * eights + 4 * half;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool there = k0 + j < a.K;
+                wv[0][j] = there ? load_w(k0 + j) : f32x4{0.f, 0.f, 0.f, 0.f};
+                xv[0][j] = there ? x[k0 + j] : 0.f;
+            }
+            multiply(0);
+        }
+    };
+    if (f0 + 128 <= a.N) run(std::false_type());
+    else run(std::true_type());
+
+    float *out = a.part + (size_t)(at.split * a.images + image) * a.rows * a.ldp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) *(f32x4 *)&sums[wave][i][4 * (acc_feature(r, half) ^ i)] = f32x4{acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int piece = c * 256 + (int)threadIdx.x, r = piece >> 5, f = 4 * (piece & 31), place = f ^ 4 * r, row = row0 + r;
+        f32x4 v = *(const f32x4 *)&sums[0][r][place];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) v += *(const f32x4 *)&sums[k][r][place];
+        if (row < a.rows && f0 + f < a.ldp) *(f32x4 *)(out + (size_t)row * a.ldp + f0 + f) = v;
+    }
 }
 
 // The shares' sums, in their order within each of GROUPS groups (neighbours in a block; more of them where there are many shares of few
@@ -563,6 +675,7 @@ static int steps_of(const GemmProblem &p) { return p.segments * ((p.K + 127) >> 
 
 enum TileSize { kBig, kWide, kMiddle, kFew };
 constexpr int kFewRows = 64;   // up to these many rows of x take the kernels for few rows
+constexpr int kFewRowsF32 = 256;   // the forward pass of up to these many fp32 rows multiplies fp32 values as they are (gated_few_f32_kernel)
 struct TileChoice {
     TileSize size;
     int splits;   // shares of the contraction, so that few tiles fill the chip
@@ -640,9 +753,42 @@ static CallSteps call_steps(const slicemoe_gated_config &c, int terms, bool e4m3
     return s;
 }
 
+// fp32 with few rows: shares of each product.  In us: 0.027 per value of k of a block's 128 features (512 bytes of its CU's part of the
+// memory's rate), the rest of a block, and the way of the sums through memory.
+constexpr double kF32PerK = 0.027, kF32Rest = 2;   // (a rest of 4: 64 rows of d 1024 31 instead of 33, 33 rows of d 1001, H 3001 58 instead of 51)
+constexpr int kF32Tile = 32, kF32Most = 4;         // rows of a tile; tiles per CU at most
+static int few_f32_splits(int rows, int images, int K, int N)
+{
+    const int cus = num_compute_units();
+    const long long tiles = (long long)images * ceil_div(rows, kF32Tile) * ceil_div(N, 128);
+    const int most = (int)std::max<long long>(1, std::min<long long>(kF32Most * cus / tiles, K / 128));
+    int best = 1;
+    double least = 0;
+    for (int n = 1; n <= most; ++n) {
+        const double cost = ceil_div(tiles * n, cus) * (kF32PerK * K / n + kF32Rest) + kSumPerMB * 4e-6 * n * images * rows * N;
+        if (n == 1 || cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    return best;
+}
+
 GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantized)
 {
     GatedPlan p = {};
+    if (!backward && c.dtype != SLICEMOE_BF16 && c.T <= kFewRowsF32) {   // the hidden rows as fp32, and the shares
+        p.few_f32 = true;
+        p.ldh = (int)padded(c.H);
+        p.part = align_up((size_t)c.T * p.ldh * 4, 256);
+        // at most; neither bound falls as T grows
+        const auto shares = [&](int images, int K, int N, int ld) {
+            const size_t room = (size_t)c.T * images * ld * 4, least = std::max(1, K / 128);
+            return std::max(room, std::min<size_t>((size_t)kF32Most * num_compute_units() * kF32Tile * 128 * 4, least * room));
+        };
+        p.total = std::max<size_t>(256, align_up(p.part + std::max(shares(2, c.d, c.H, p.ldh), shares(1, c.H, c.d, (c.d + 7) / 8 * 8)), 256));
+        return p;
+    }
     const size_t T = c.T, d = c.d, H = c.H;
     p.terms = c.dtype == SLICEMOE_BF16 ? 1 : 3;
     p.copy_x = c.dtype != SLICEMOE_BF16 || c.d % 8 != 0;
@@ -678,6 +824,11 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
         part = std::max(std::max(rows_shares(st.dx), up_shares(st.up + st.up / 2, 3)), 3 * 256 + 2 * share_bytes(cus, 256 * 256, st.dw, d, h8) + share_bytes(cus, 256 * 256, st.dw, H, d8));
     p.part = take(part);
     p.total = std::max<size_t>(at, 256);
+    if (!backward && p.terms == 3) {   // not below what the longest batch of few rows takes
+        slicemoe_gated_config few_rows = c;
+        few_rows.T = kFewRowsF32;
+        p.total = std::max(p.total, gated_plan(few_rows, false, false).total);
+    }
     return p;
 }
 
@@ -787,17 +938,20 @@ template <int FL, bool E4M3, int TERMS> static hipError_t launch_up(const GemmPr
         case kMiddle: return run_up<Middle>(gated_up_kernel<Middle, TERMS>, lds_of<Middle>(Middle::FT), p, h, sc, s);
         default: break;
     }
-    const auto few = [&](auto shape) {
-        typedef decltype(shape) S;
-        return run_up<S>(gated_up_few_kernel<S, TERMS>, S::LDS, p, h, sc, s);
-    };
-    const bool many = ceil_div(p.nf, 32) > num_compute_units();
-    if constexpr (E4M3) {
-        if (p.nr <= 32) return many ? few(FewShape<1, 1, FL, true, true, 2>()) : few(FewShape<1, 1, FL, true, true, 1>());
-        return many ? few(FewShape<2, 1, FL, true, true, 2>()) : few(FewShape<2, 1, FL, true, true, 1>());
-    } else {
-        if (p.nr <= 32) return many ? few(FewShape<1, 2, FL, true, false, 1>()) : few(FewShape<1, 1, FL, true, false, 1>());
-        return many ? few(FewShape<2, 2, FL, true, false, 1>()) : few(FewShape<2, 1, FL, true, false, 1>());
+    if constexpr (TERMS == 3) return hipErrorInvalidValue;   // (fp32 with few rows: see launch_few_f32)
+    else {
+        const auto few = [&](auto shape) {
+            typedef decltype(shape) S;
+            return run_up<S>(gated_up_few_kernel<S>, S::LDS, p, h, sc, s);
+        };
+        const bool many = ceil_div(p.nf, 32) > num_compute_units();
+        if constexpr (E4M3) {
+            if (p.nr <= 32) return many ? few(FewShape<1, 1, FL, true, true, 2>()) : few(FewShape<1, 1, FL, true, true, 1>());
+            return many ? few(FewShape<2, 1, FL, true, true, 2>()) : few(FewShape<2, 1, FL, true, true, 1>());
+        } else {
+            if (p.nr <= 32) return many ? few(FewShape<1, 2, FL, true, false, 1>()) : few(FewShape<1, 1, FL, true, false, 1>());
+            return many ? few(FewShape<2, 2, FL, true, false, 1>()) : few(FewShape<2, 1, FL, true, false, 1>());
+        }
     }
 }
 
@@ -811,6 +965,13 @@ template <typename S, typename KERNEL> static hipError_t run_products(KERNEL ker
     const hipError_t e = ready(kernel, lds);
     if (e != hipSuccess) return e;
     kernel<<<ps.first[n], 256, lds, s>>>(ps);
+    return hipGetLastError();
+}
+// The sums of n products' shares; pieces: eight outputs each, of the largest.
+static hipError_t launch_sum(const Products &ps, int n, long long pieces, int splits, hipStream_t s)
+{
+    if (splits >= 4) gated_sum_kernel<8><<<dim3((int)std::min<long long>((pieces + 31) / 32, 16ll * num_compute_units()), n), 256, 0, s>>>(ps);
+    else gated_sum_kernel<1><<<dim3((int)std::min<long long>((pieces + 255) / 256, 8ll * num_compute_units()), n), 256, 0, s>>>(ps);
     return hipGetLastError();
 }
 // n products of one tile size (few rows: one product, R K-contiguous); part: room for the shares.
@@ -842,10 +1003,7 @@ template <int RL, int FL> static hipError_t launch_products(Products &ps, int n,
                              : run_products<Two>(gated_product_few_kernel<Two>, Two::LDS, ps, n, s);
     } else
         e = hipErrorInvalidValue;
-    if (e != hipSuccess || t.splits == 1) return e;
-    if (t.splits >= 4) gated_sum_kernel<8><<<dim3((int)std::min<long long>((most + 31) / 32, 16ll * num_compute_units()), n), 256, 0, s>>>(ps);
-    else gated_sum_kernel<1><<<dim3((int)std::min<long long>((most + 255) / 256, 8ll * num_compute_units()), n), 256, 0, s>>>(ps);
-    return hipGetLastError();
+    return e != hipSuccess || t.splits == 1 ? e : launch_sum(ps, n, most, t.splits, s);
 }
 
 static hipError_t launch_down(const slicemoe_gated_config &c, const GatedPlan &plan, const char *Wd, size_t twd, long long ldwd, const void *addend,
@@ -863,10 +1021,42 @@ static Hidden hidden_of(const slicemoe_gated_config &c, const GatedPlan &p, char
     return {{(bf16_t *)(ws + p.a), (bf16_t *)(ws + p.dg), (bf16_t *)(ws + p.du)}, c.T, c.H, p.ldh};
 }
 
+static hipError_t run_few_f32(FewF32 a, hipStream_t s)
+{
+    a.tiles_r = ceil_div(a.rows, kF32Tile);
+    a.tiles_f = ceil_div(a.N, 128);
+    a.splits = few_f32_splits(a.rows, a.images, a.K, a.N);
+    const int blocks = a.tiles_r * a.tiles_f * a.images * a.splits;
+    gated_few_f32_kernel<<<blocks, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+static hipError_t launch_few_f32(const slicemoe_gated_config &c, const GatedPlan &plan, const float *x, const slicemoe_gated_weights &w,
+                                 const void *addend, void *y, char *ws, hipStream_t s)
+{
+    float *part = (float *)(ws + plan.part), *a = (float *)ws;
+    FewF32 up = {x, {(const float *)w.Wg, (const float *)w.Wu}, part, c.T, c.d, c.H, c.d, plan.ldh, 2};
+    hipError_t e = run_few_f32(up, s);
+    if (e != hipSuccess) return e;
+    const Hidden h = {{(bf16_t *)a}, c.T, c.H, plan.ldh};
+    e = launch_up_sum<kAsF32, false, 2>(part, h, Scales(), few_f32_splits(c.T, 2, c.d, c.H), s);
+    if (e != hipSuccess) return e;
+    const int ld = (c.d + 7) & ~7;
+    FewF32 down = {a, {(const float *)w.Wd, nullptr}, part, c.T, c.H, c.d, plan.ldh, ld, 1};
+    e = run_few_f32(down, s);
+    if (e != hipSuccess) return e;
+    Products ps = {};
+    ps.out[0] = {y, addend, c.T, c.d, 1};
+    ps.part[0] = part;
+    ps.p[0].splits = few_f32_splits(c.T, 1, c.H, c.d);
+    const long long pieces = (long long)c.T * ld / 8;
+    return launch_sum(ps, 1, pieces, ps.p[0].splits, s);
+}
+
 hipError_t launch_gated_ffn(const slicemoe_gated_config &c, const GatedPlan &plan, const void *x, const slicemoe_gated_weights &w,
                             const void *addend, void *y, char *ws, hipStream_t s)
 {
     if (c.T == 0) return hipSuccess;
+    if (plan.few_f32) return launch_few_f32(c, plan, (const float *)x, w, addend, y, ws, s);
     Operands o;
     hipError_t e = make_operands(c, plan, x, nullptr, w, ws, &o, s);
     if (e != hipSuccess) return e;

@@ -107,3 +107,30 @@ def test_eight_bits(B, T, d, H):
         v, e = R.gated_quantized(xq, xs, q, addend)
         R.within(y, v, e, "y")
         assert float((y.double() - v).norm()) <= 3 * 2.0 ** -8 * float(v.norm())
+
+
+# rows on either side of a tile of 32 and of the limit; contractions that end inside an eight, inside a share and at both; features that end
+# inside a tile and inside four; shares that are empty
+@pytest.mark.parametrize("T,d,H", [(1, 7, 129), (2, 4099, 130), (17, 129, 1000), (31, 8, 3), (32, 2048, 127), (33, 1003, 515), (64, 640, 4100),
+                                   (200, 1003, 515), (255, 136, 33), (256, 640, 260), (257, 640, 260)])
+def test_fp32_of_few_rows(B, T, d, H):
+    run(B, T, d, H, F32, backward=False)
+    run(B, T, d, H, F32, backward=False, seed=5, addend=False)
+
+
+def test_fp32_of_few_rows_in_place_and_infinite(B):
+    """y in the place of x; an infinity that meets only finite values stays one (nothing is taken apart into terms), next to a padded k."""
+    T, d, H = 40, 131, 70
+    cfg, w = B.make_gated_config(T, d, H, "f32"), weights(d, H, F32)
+    x, ws = tensor((T, d), 9, 1.0, F32), space(B.slicemoe_gated_ffn_workspace_bytes(cfg))
+    y = torch.empty_like(x)
+    B.slicemoe_gated_ffn(cfg, x, w, y, ws)
+    held = x.clone()
+    B.slicemoe_gated_ffn(cfg, held, w, held, ws)
+    assert torch.equal(held, y)
+    w["Wg"][3, 5], w["Wd"][5] = float("inf"), 1.0       # gate 5 of row t is inf with the sign of x[t, 3]
+    x[:, 3] = torch.where(torch.arange(T, device="cuda") % 2 == 0, 1.0, 0.5)
+    w["Wu"][:, 5] = 0.0
+    w["Wu"][3, 5] = 1.0                                  # up 5 is x[t, 3]: hidden 5 is inf, y is inf in all columns
+    B.slicemoe_gated_ffn(cfg, x, w, y, ws)
+    assert bool((y == float("inf")).all())
