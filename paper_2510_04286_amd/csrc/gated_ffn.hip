@@ -436,24 +436,27 @@ template <typename S> __global__ __launch_bounds__(256) void gated_product_few_k
     few_rows<S>(p, row0, f0, s0, s1, lds, [&](int r, int c, const float (&v)[1][8]) { put_out(o, row0 + r, f0 + c, v[0]); });
 }
 
-// fp32 with few rows: part[split][image][rows][ldp] = x W for one or two matrices [K][N], on the fp32 matrix instruction, which reads the
-// weights where they are (laid out as terms first they cross memory twice more).  It takes one value of k per lane, so a lane's 16 bytes of
-// a row of W are four feature tiles (tile t has the features 4 i + t of the block's 128) and its 16 bytes of a row of x four
-// instructions: nothing passes through the LDS but the four wavefronts' sums.  A wavefront takes 32 values of k in turn with the
+// fp32 with few rows: part[split][image][rows][ldp] = x W for one or two matrices [K][N] (K-major) or [N][K] (K-contiguous), on the fp32
+// matrix instruction, which reads the weights where they are (laid out as terms first they cross memory twice more).  It takes one value
+// of k per lane, so a lane's 16 bytes of a row of K-major W are four feature tiles (tile t has the features 4 i + t of the block's 128; of
+// K-contiguous W 32 t + i, from four rows) and its 16 bytes of a row of x four instructions: nothing passes through the LDS but the four wavefronts' sums.  A wavefront takes 32 values of k in turn with the
 // others (a cache line of x), eight at a time, the next three eights on their way.
 //
 // Bound by memory up to 32 rows: d 4096, H 11008 (541 MB of weights), the whole forward 123 us for one row, 128 for 22 (4.2 TB/s); as terms
 // 574 and 587.  Above by the fp32 matrix instruction, where the terms' copies still cost more: 64 rows 200 against 615, 128 357 against
 // 652, 256 674 against 675; d 1024, H 2816: 22 rows 25 against 53, 128 44 against 62, 256 66 against 73.  Tiles of 64 rows read the
-// weights half as often and fill the chip worse: 22 rows 183, 64 202, 256 622.
+// weights half as often and fill the chip worse: 22 rows 183, 64 202, 256 622.  The backward's K-contiguous products run at 2.1 TB/s, the
+// K-major ones at 4.6 (one row: 172 us for 360 MB against 78); the 128 bytes of a row requested at once instead of eight by eight: 3%
+// worse at d 4096, 2% better at d 1024.
 struct FewF32 {
-    const float *x;
+    const float *x[2];
     const float *w[2];
     float *part;
     int rows, K, N, ldx, ldp;
-    int images, tiles_r, tiles_f, splits;
+    int images, first, of;   // images here, which of part's `of` images the first of them is
+    int splits, tiles_r, tiles_f;
 };
-__global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
+template <int FL> __global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
 {
     constexpr int SLOTS = 4;
     __shared__ __align__(16) float sums[4][32][128];   // piece p of row r (four features) at place p ^ r: no bank conflicts
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
     const int image = at.f / a.tiles_f, f0 = (at.f - image * a.tiles_f) * 128, row0 = at.r * 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, half = lane >> 5, col = f0 + 4 * i;
     const float *w = image ? a.w[1] : a.w[0];
-    const float *x = a.x + (size_t)(row0 + i < a.rows ? row0 + i : a.rows - 1) * a.ldx;
+    const float *x = (image ? a.x[1] : a.x[0]) + (size_t)(row0 + i < a.rows ? row0 + i : a.rows - 1) * a.ldx;
     f32x16 acc[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -474,7 +477,11 @@ __global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
     const int n = (share >> 4) * 4 + (rest < 0 ? 0 : rest > 4 ? 4 : rest);
     const auto eight_of = [&](int k) { return g0 + (k >> 2) * 16 + wave * 4 + (k & 3); };
     const auto run = [&](auto edge) {
-        const auto load_w = [&](int k) -> f32x4 {   // (k < K)
+        const float *wr[4];   // K-contiguous: the lane's rows
+        if constexpr (FL == kKContiguous)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) wr[t] = w + (size_t)(f0 + 32 * t + i < a.N ? f0 + 32 * t + i : a.N - 1) * a.K;
+        const auto load_w = [&](int k) -> f32x4 {   // K-major, k < K
             const float *q = w + (size_t)k * a.N;
             if (!decltype(edge)::value || col + 4 <= a.N) return __builtin_bit_cast(f32x4, *(const loose *)(q + col));
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -487,14 +494,18 @@ __global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
         const auto request = [&](int slot, int k) {
             const int k0 = 8 * eight_of(k) + 4 * half;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) wv[slot][j] = load_w(k0 + j);
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (FL == kKMajor) wv[slot][j] = load_w(k0 + j);
+                else wv[slot][j] = __builtin_bit_cast(f32x4, *(const loose *)(wr[j] + k0));
+            }
             xv[slot] = __builtin_bit_cast(f32x4, *(const loose *)(x + k0));
         };
         const auto multiply = [&](int slot) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(wv[slot][j][t], xv[slot][j], acc[t], 0, 0, 0);
+                for (int t = 0; t < 4; ++t)
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(FL == kKMajor ? wv[slot][j][t] : wv[slot][t][j], xv[slot][j], acc[t], 0, 0, 0);
         };
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k)
@@ -518,18 +529,28 @@ __global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bool there = k0 + j < a.K;
-                wv[0][j] = there ? load_w(k0 + j) : f32x4{0.f, 0.f, 0.f, 0.f};
+                if constexpr (FL == kKMajor) wv[0][j] = there ? load_w(k0 + j) : f32x4{0.f, 0.f, 0.f, 0.f};
+                else
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) wv[0][t][j] = there ? wr[t][k0 + j] : 0.f;
                 xv[0][j] = there ? x[k0 + j] : 0.f;
             }
             multiply(0);
         }
     };
-    if (f0 + 128 <= a.N) run(std::false_type());
+    if (FL == kKContiguous || f0 + 128 <= a.N) run(std::false_type());
     else run(std::true_type());
 
-    float *out = a.part + (size_t)(at.split * a.images + image) * a.rows * a.ldp;
+    float *out = a.part + (size_t)(at.split * a.of + a.first + image) * a.rows * a.ldp;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) *(f32x4 *)&sums[wave][i][4 * (acc_feature(r, half) ^ i)] = f32x4{acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
+    for (int r = 0; r < 16; ++r) {
+        if constexpr (FL == kKMajor) *(f32x4 *)&sums[wave][i][4 * (acc_feature(r, half) ^ i)] = f32x4{acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
+        else {
+            const f32x16 &v = acc[r >> 2];   // quarter r % 4 of its tile
+            const int q = r & 3;
+            *(f32x4 *)&sums[wave][i][4 * ((8 * (r >> 2) + 2 * q + half) ^ i)] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        }
+    }
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -538,6 +559,63 @@ __global__ __launch_bounds__(256) void gated_few_f32_kernel(FewF32 a)
 #pragma unroll
         for (int k = 1; k < 4; ++k) v += *(const f32x4 *)&sums[k][r][place];
         if (row < a.rows && f0 + f < a.ldp) *(f32x4 *)(out + (size_t)row * a.ldp + f0 + f) = v;
+    }
+}
+
+// Weight gradients of few fp32 rows (d 4096, H 11008: 541 MB in 84 us for one row, 234 for 64): out[r][f] = sum over t of l[t][r] m[t][f], three of them.  A wavefront has 32 of r and 128 of f: the
+// features are the matrix instruction's second operand, so a lane holds four neighbours of a row and stores go out as rows.  Bound
+// by the outputs' way to memory, from some 64 rows on by the instruction; l and m are small and come from the caches.
+struct FewF32Weights {
+    const float *l[3], *m[3];
+    float *out[3];
+    int nr[3], nf[3], ldl[3], ldm[3];
+    int rows;
+};
+__global__ __launch_bounds__(256) void gated_few_f32_weights_kernel(FewF32Weights a)
+{
+    const int k = blockIdx.y, nr = a.nr[k], nf = a.nf[k], tiles_f = (nf + 127) / 128, tile = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 31, half = lane >> 5;
+    const int row0 = (tile / tiles_f * 4 + wave) * 32, col = tile % tiles_f * 128 + 4 * i;
+    if (row0 >= nr) return;   // (a whole wavefront; there is no barrier)
+    const float *l = a.l[k] + (row0 + i < nr ? row0 + i : nr - 1), *m = a.m[k];
+    const size_t ldl = a.ldl[k], ldm = a.ldm[k];
+    f32x16 acc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+    for (int t0 = 4 * half; t0 - 4 * half < a.rows; t0 += 8) {
+        float lv[4];
+        f32x4 mv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = t0 + j;
+            lv[j] = 0.f;
+            mv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (t >= a.rows) continue;
+            lv[j] = l[t * ldl];
+            if (col + 4 <= nf) mv[j] = __builtin_bit_cast(f32x4, *(const loose *)(m + t * ldm + col));
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < nf) mv[j][e] = m[t * ldm + col + e];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(lv[j], mv[j][t], acc[t], 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int row = row0 + acc_feature(r, half);
+        if (row >= nr) continue;
+        float *q = a.out[k] + (size_t)row * nf + col;
+        const f32x4 v = {acc[0][r], acc[1][r], acc[2][r], acc[3][r]};
+        if (col + 4 <= nf) *(loose *)q = __builtin_bit_cast(u32x4, v);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < nf) q[e] = v[e];
     }
 }
 
@@ -675,7 +753,10 @@ static int steps_of(const GemmProblem &p) { return p.segments * ((p.K + 127) >> 
 
 enum TileSize { kBig, kWide, kMiddle, kFew };
 constexpr int kFewRows = 64;   // up to these many rows of x take the kernels for few rows
-constexpr int kFewRowsF32 = 256;   // the forward pass of up to these many fp32 rows multiplies fp32 values as they are (gated_few_f32_kernel)
+constexpr int kFewRowsF32 = 256;   // the forward pass of up to these many fp32 rows multiplies fp32 values as they are (gated_few_f32_kernel),
+// the backward pass up to these (both passes together, as they are against terms: d 4096, H 11008, 64 rows 892 against 1322, 128 rows 1487
+// against 1620; d 1024, H 2816, 64 rows 114 against 136, 128 rows 165 against 159; d 1001, H 3001, 100 rows 211 against 192)
+constexpr int kFewRowsF32Backward = 64;
 struct TileChoice {
     TileSize size;
     int splits;   // shares of the contraction, so that few tiles fill the chip
@@ -777,16 +858,21 @@ static int few_f32_splits(int rows, int images, int K, int N)
 GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantized)
 {
     GatedPlan p = {};
-    if (!backward && c.dtype != SLICEMOE_BF16 && c.T <= kFewRowsF32) {   // the hidden rows as fp32, and the shares
+    if (c.dtype != SLICEMOE_BF16 && c.T <= (backward ? kFewRowsF32Backward : kFewRowsF32)) {   // the hidden rows as fp32, and the shares
         p.few_f32 = true;
         p.ldh = (int)padded(c.H);
-        p.part = align_up((size_t)c.T * p.ldh * 4, 256);
+        const size_t hidden = align_up((size_t)c.T * p.ldh * 4, 256);
+        p.dg = hidden;   // (after a, at the beginning)
+        p.du = 2 * hidden;
+        p.part = (backward ? 3 : 1) * hidden;
         // at most; neither bound falls as T grows
         const auto shares = [&](int images, int K, int N, int ld) {
             const size_t room = (size_t)c.T * images * ld * 4, least = std::max(1, K / 128);
             return std::max(room, std::min<size_t>((size_t)kF32Most * num_compute_units() * kF32Tile * 128 * 4, least * room));
         };
-        p.total = std::max<size_t>(256, align_up(p.part + std::max(shares(2, c.d, c.H, p.ldh), shares(1, c.H, c.d, (c.d + 7) / 8 * 8)), 256));
+        const int d8 = (c.d + 7) / 8 * 8;
+        const size_t part = backward ? std::max(shares(3, c.d, c.H, p.ldh), shares(2, c.H, c.d, d8)) : std::max(shares(2, c.d, c.H, p.ldh), shares(1, c.H, c.d, d8));
+        p.total = std::max<size_t>(256, align_up(p.part + part, 256));
         return p;
     }
     const size_t T = c.T, d = c.d, H = c.H;
@@ -824,10 +910,10 @@ GatedPlan gated_plan(const slicemoe_gated_config &c, bool backward, bool quantiz
         part = std::max(std::max(rows_shares(st.dx), up_shares(st.up + st.up / 2, 3)), 3 * 256 + 2 * share_bytes(cus, 256 * 256, st.dw, d, h8) + share_bytes(cus, 256 * 256, st.dw, H, d8));
     p.part = take(part);
     p.total = std::max<size_t>(at, 256);
-    if (!backward && p.terms == 3) {   // not below what the longest batch of few rows takes
+    if (p.terms == 3) {   // not below what the longest batch of few rows takes
         slicemoe_gated_config few_rows = c;
-        few_rows.T = kFewRowsF32;
-        p.total = std::max(p.total, gated_plan(few_rows, false, false).total);
+        few_rows.T = backward ? kFewRowsF32Backward : kFewRowsF32;
+        p.total = std::max(p.total, gated_plan(few_rows, backward, false).total);
     }
     return p;
 }
@@ -1021,35 +1107,61 @@ static Hidden hidden_of(const slicemoe_gated_config &c, const GatedPlan &p, char
     return {{(bf16_t *)(ws + p.a), (bf16_t *)(ws + p.dg), (bf16_t *)(ws + p.du)}, c.T, c.H, p.ldh};
 }
 
-static hipError_t run_few_f32(FewF32 a, hipStream_t s)
+template <int FL> static hipError_t run_few_f32(FewF32 a, hipStream_t s)
 {
     a.tiles_r = ceil_div(a.rows, kF32Tile);
     a.tiles_f = ceil_div(a.N, 128);
-    a.splits = few_f32_splits(a.rows, a.images, a.K, a.N);
-    const int blocks = a.tiles_r * a.tiles_f * a.images * a.splits;
-    gated_few_f32_kernel<<<blocks, 256, 0, s>>>(a);
+    gated_few_f32_kernel<FL><<<a.tiles_r * a.tiles_f * a.images * a.splits, 256, 0, s>>>(a);
     return hipGetLastError();
+}
+// out = addend + the shares' sums, [T][d].
+static hipError_t sum_few_f32(const slicemoe_gated_config &c, float *part, int shares, const void *addend, void *out, hipStream_t s)
+{
+    Products ps = {};
+    ps.out[0] = {out, addend, c.T, c.d, 1};
+    ps.part[0] = part;
+    ps.p[0].splits = shares;
+    return launch_sum(ps, 1, (long long)c.T * ((c.d + 7) / 8), shares, s);
 }
 static hipError_t launch_few_f32(const slicemoe_gated_config &c, const GatedPlan &plan, const float *x, const slicemoe_gated_weights &w,
                                  const void *addend, void *y, char *ws, hipStream_t s)
 {
     float *part = (float *)(ws + plan.part), *a = (float *)ws;
-    FewF32 up = {x, {(const float *)w.Wg, (const float *)w.Wu}, part, c.T, c.d, c.H, c.d, plan.ldh, 2};
-    hipError_t e = run_few_f32(up, s);
+    const int up_splits = few_f32_splits(c.T, 2, c.d, c.H), down_splits = few_f32_splits(c.T, 1, c.H, c.d);
+    hipError_t e = run_few_f32<kKMajor>({{x, x}, {(const float *)w.Wg, (const float *)w.Wu}, part, c.T, c.d, c.H, c.d, plan.ldh, 2, 0, 2, up_splits}, s);
     if (e != hipSuccess) return e;
     const Hidden h = {{(bf16_t *)a}, c.T, c.H, plan.ldh};
-    e = launch_up_sum<kAsF32, false, 2>(part, h, Scales(), few_f32_splits(c.T, 2, c.d, c.H), s);
+    e = launch_up_sum<kAsF32, false, 2>(part, h, Scales(), up_splits, s);
     if (e != hipSuccess) return e;
-    const int ld = (c.d + 7) & ~7;
-    FewF32 down = {a, {(const float *)w.Wd, nullptr}, part, c.T, c.H, c.d, plan.ldh, ld, 1};
-    e = run_few_f32(down, s);
-    if (e != hipSuccess) return e;
-    Products ps = {};
-    ps.out[0] = {y, addend, c.T, c.d, 1};
-    ps.part[0] = part;
-    ps.p[0].splits = few_f32_splits(c.T, 1, c.H, c.d);
-    const long long pieces = (long long)c.T * ld / 8;
-    return launch_sum(ps, 1, pieces, ps.p[0].splits, s);
+    e = run_few_f32<kKMajor>({{a}, {(const float *)w.Wd}, part, c.T, c.H, c.d, plan.ldh, (c.d + 7) & ~7, 1, 0, 1, down_splits}, s);
+    return e == hipSuccess ? sum_few_f32(c, part, down_splits, addend, y, s) : e;
+}
+static hipError_t launch_few_f32_backward(const slicemoe_gated_config &c, const GatedPlan &plan, const float *x, const slicemoe_gated_weights &w,
+                                          const float *dy, const void *addend, void *dx, const slicemoe_gated_weight_grads &g, char *ws,
+                                          hipStream_t s)
+{
+    float *part = (float *)(ws + plan.part), *a = (float *)(ws + plan.a), *dg = (float *)(ws + plan.dg), *du = (float *)(ws + plan.du);
+    const float *Wg = (const float *)w.Wg, *Wu = (const float *)w.Wu, *Wd = (const float *)w.Wd;
+    hipError_t e;
+    if (c.T > 0) {
+        const int splits = few_f32_splits(c.T, 3, c.d, c.H);
+        e = run_few_f32<kKMajor>({{x, x}, {Wg, Wu}, part, c.T, c.d, c.H, c.d, plan.ldh, 2, 0, 3, splits}, s);
+        if (e != hipSuccess) return e;
+        e = run_few_f32<kKContiguous>({{dy}, {Wd}, part, c.T, c.d, c.H, c.d, plan.ldh, 1, 2, 3, splits}, s);
+        if (e != hipSuccess) return e;
+        e = launch_up_sum<kAsF32, false, 3>(part, hidden_of(c, plan, ws), Scales(), splits, s);
+        if (e != hipSuccess) return e;
+    }
+    // before dx, which may take the place of dy
+    const FewF32Weights p = {{x, x, a}, {dg, du, dy}, {(float *)g.Wg, (float *)g.Wu, (float *)g.Wd}, {c.d, c.d, c.H}, {c.H, c.H, c.d},
+                             {c.d, c.d, plan.ldh}, {plan.ldh, plan.ldh, c.d}, c.T};
+    const int tiles = std::max(ceil_div(c.d, 128) * ceil_div(c.H, 128), 1);   // of all three: 128 x 128 either way round
+    gated_few_f32_weights_kernel<<<dim3(tiles, 3), 256, 0, s>>>(p);
+    e = hipGetLastError();
+    if (e != hipSuccess || c.T == 0) return e;
+    const int splits = few_f32_splits(c.T, 2, c.H, c.d);
+    e = run_few_f32<kKContiguous>({{dg, du}, {Wg, Wu}, part, c.T, c.H, c.d, plan.ldh, (c.d + 7) & ~7, 2, 0, 2, splits}, s);
+    return e == hipSuccess ? sum_few_f32(c, part, 2 * splits, addend, dx, s) : e;
 }
 
 hipError_t launch_gated_ffn(const slicemoe_gated_config &c, const GatedPlan &plan, const void *x, const slicemoe_gated_weights &w,
@@ -1118,6 +1230,7 @@ hipError_t launch_gated_ffn_backward(const slicemoe_gated_config &c, const Gated
                                      const void *dy, const void *addend, void *dx, const slicemoe_gated_weight_grads &g, char *ws,
                                      hipStream_t s)
 {
+    if (plan.few_f32) return launch_few_f32_backward(c, plan, (const float *)x, w, (const float *)dy, addend, dx, g, ws, s);
     Operands o;
     hipError_t e = make_operands(c, plan, x, dy, w, ws, &o, s);
     if (e != hipSuccess) return e;

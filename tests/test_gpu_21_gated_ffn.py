@@ -134,3 +134,12 @@ def test_fp32_of_few_rows_in_place_and_infinite(B):
     w["Wu"][3, 5] = 1.0                                  # up 5 is x[t, 3]: hidden 5 is inf, y is inf in all columns
     B.slicemoe_gated_ffn(cfg, x, w, y, ws)
     assert bool((y == float("inf")).all())
+
+
+# the same for the backward pass, whose limit is 64 rows: contractions over d, over H and over the rows that end inside an eight; edges of the
+# 32 and 128 outputs of a wavefront
+@pytest.mark.parametrize("T,d,H", [(1, 7, 129), (2, 4099, 130), (9, 130, 131), (17, 129, 1000), (31, 8, 3), (32, 2048, 127), (33, 1003, 515),
+                                   (63, 127, 640), (64, 640, 4100), (65, 640, 4100)])
+def test_fp32_of_few_rows_backward(B, T, d, H):
+    run(B, T, d, H, F32)
+    run(B, T, d, H, F32, seed=5, addend=False)
