@@ -365,3 +365,17 @@ def test_arrays_of_another_device_are_refused(B, monkeypatch):
     for call in calls[:1] + calls[3:]:
         call()   # the same calls where they belong
     torch.cuda.synchronize()
+
+
+def test_few_fp32_rows_captured(B):
+    test_captured_into_a_graph(B, 50, F32)
+
+
+@pytest.mark.parametrize("T,d,H", [(40, 131, 70), (64, 300, 257)])
+def test_few_fp32_rows_in_place(B, T, d, H):
+    test_gated_outputs_in_place_of_inputs(B, T, d, H, F32)
+
+
+@pytest.mark.parametrize("T,d,H", [(1, 9, 5), (33, 71, 101), (64, 136, 259)])
+def test_few_fp32_rows_next_to_memory_that_must_not_be_read(B, T, d, H):
+    test_nothing_beyond_the_arrays_is_read_or_written(B, T, d, H, F32)
