@@ -344,7 +344,8 @@ typedef struct {
 
 /*
  * Root-mean-square norm with the residual's addition: s = x + residual, y = s / sqrt(mean(s^2) + eps) * weight, in fp32
- * throughout; y is taken of the fp32 sum and rounded once.
+ * throughout; y is taken of the fp32 sum and rounded once.  Any finite s will do: rows whose squares leave the range of fp32 are
+ * scaled by a power of two first.  (A row of zeros with eps = 0 is 0 / 0, NaN.)
  *   x         [T, d] in
  *   residual  [T, d] in, may be NULL: then s = x
  *   weight    [d]    in

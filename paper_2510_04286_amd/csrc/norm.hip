@@ -9,6 +9,11 @@
 // again, so the forward keeps nothing for it.  d_w: persistent blocks, a column sum per lane in registers over the block's rows, one
 // row of partial sums per block, added in block order by a second kernel (bit-reproducible).
 //
+// Range: squares and their mean are fp32, so a row is squared as it is only where mean + eps lies in [2^-60, 2^60).  Any other row (values
+// of 1e9 and more, or of 1e-9 and less with an eps as small) is multiplied by the power of two k that brings the larger of its largest
+// value and sqrt(eps) to 1, summed again, and r is taken of k s and k^2 eps: n = (k s) r holds for every finite row.  All lanes of a row
+// decide alike, by s and eps; k is 1 elsewhere and changes no bit.
+//
 // The e4m3 row: scale = max|y| / 448 (448: the largest e4m3 value), values y / scale rounded to nearest even.  A largest value below
 // 1e-30 counts as 1e-30, so a row of zeros has a scale and no division by zero; a row that holds a NaN or an infinity has a NaN scale.
 //
@@ -104,6 +109,15 @@ template <int W> __device__ __forceinline__ uint32_t row_max(uint32_t v, float *
     return v;
 }
 
+// Below, squares lose bits that count for the mean; above, they or dy w s may overflow.
+__device__ __forceinline__ bool in_range(float mean) { return mean >= 0x1p-60f && mean < 0x1p60f; }
+// The power of two for a row whose largest magnitude has the bits `most`.  (An infinity or a NaN: any; 2^127 and 2^-126 are the ends.)
+__device__ __forceinline__ float range_factor(uint32_t most, float eps)
+{
+    const uint32_t root = __float_as_uint(sqrtf(eps)), e = (most > root ? most : root) >> 23;
+    return __uint_as_float((e < 253 ? 254 - e : 1) << 23);
+}
+
 // W wavefronts per row (W = 1: four rows per block of 256 threads), NP pieces per lane.  sum and y may be x or residual: a row's
 // owners have all of it in registers before the first of them stores, and nothing tells the compiler that the arrays are apart.
 template <typename T, bool ALIGNED, int W, int NP, bool QUANT>
@@ -136,8 +150,25 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_kernel(const
             if (residual) s[c][i] += RowPiece<T>::get(pr[c], i);   // (without one, -0 stays -0)
             ss += s[c][i] * s[c][i];
         }
-    ss = row_sum<W>(ss, lds);
-    const float r = 1.f / sqrtf(ss / d + eps);
+    float mean = row_sum<W>(ss, lds) / d + eps, k = 1.f;
+    if (!in_range(mean)) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < NP; ++c)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t a = __float_as_uint(s[c][i]) & 0x7fffffffu;
+                top = a > top ? a : top;
+            }
+        k = range_factor(row_max<W>(top, lds), eps);
+        ss = 0.f;
+#pragma unroll
+        for (int c = 0; c < NP; ++c)
+#pragma unroll
+            for (int i = 0; i < V; ++i) ss += s[c][i] * k * (s[c][i] * k);
+        mean = row_sum<W>(ss, lds) / d + eps * k * k;
+    }
+    const float r = 1.f / sqrtf(mean);
     uint32_t most = 0;
 #pragma unroll
     for (int c = 0; c < NP; ++c) {
@@ -145,7 +176,7 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_kernel(const
         if (at < d && sum) store_piece<T, ALIGNED>(sum + at0, at, d, s[c]);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            s[c][i] = s[c][i] * r * RowPiece<T>::get(pw[c], i);
+            s[c][i] = s[c][i] * k * r * RowPiece<T>::get(pw[c], i);
             const uint32_t a = __float_as_uint(s[c][i]) & 0x7fffffffu;
             if (QUANT && at + i < d) most = a > most ? a : most;
         }
@@ -198,6 +229,24 @@ template <int W> __device__ __forceinline__ void row_sums(float &a, float &b, fl
     }
 }
 
+// Largest value over the same wavefronts.  l: LDS that the row has not used yet.
+template <int W> __device__ __forceinline__ uint32_t row_most(uint32_t v, float *l)
+{
+    v = row_max<1>(v, nullptr);
+    if constexpr (W == 1) return v;
+    if ((threadIdx.x & 63) == 0) l[threadIdx.x >> 6] = __uint_as_float(v);
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const uint32_t o = __float_as_uint(l[i]);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+// Hides where a piece comes from: its values are unpacked again from here on, not kept in registers.
+__device__ __forceinline__ void keep_packed(u32x4 &p) { asm volatile("" : "+v"(p)); }
+
 // Block b takes the rows b, b + gridDim.x, .. (W = 1: its four wavefronts the row groups), so that a block's share differs by
 // at most one row (group).  A row's pieces are requested while the row before it is worked on.  part[b][d]: its column sums of dy n.
 template <typename T, bool ALIGNED, int W, int NP>
@@ -231,7 +280,9 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_backward_ker
     }
     const float inv_d = 1.f / d;
     const long long stride = (long long)gridDim.x * ROWS;
-    long long row = (long long)blockIdx.x * ROWS + (W == 1 ? wave : 0);
+    const long long first = (long long)blockIdx.x * ROWS + (W == 1 ? wave : 0);
+    long long row = first;
+    bool left = false;   // rows out of range, whose turn comes at the end
     constexpr bool AHEAD = W < 16 && NP < 8;   // (where the registers hold two rows)
     if (AHEAD && row < rows) request(row);
     int flip = 0;
@@ -247,27 +298,86 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void add_rmsnorm_backward_ker
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float s = RowPiece<T>::get(cs[c], i);
-                ss += s * s;
+                ss = fmaf(s, s, ss);
                 along += RowPiece<T>::get(cg[c], i) * RowPiece<T>::get(pw[c], i) * s;
             }
         }
         if (AHEAD && row + stride < rows) request(row + stride);
         row_sums<W>(ss, along, lds, flip);
-        const float r = 1.f / sqrtf(ss * inv_d + eps);
-        const float k = along * r * inv_d;   // mean(m n)
+        const float mean = fmaf(ss, inv_d, eps);
+        if (!in_range(mean)) {
+            left = true;
+            continue;
+        }
+        const float r = 1.f / sqrtf(mean);
+        const float mn = along * r * inv_d;   // mean(m n)
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
             const int at = (lane + c * LANES) * V;
             float v[V];
+            if constexpr (NP >= 4) {   // (bf16 rows of 8192: 226 registers, two blocks per CU; without it 284, one)
+                keep_packed(cs[c]);
+                keep_packed(cg[c]);
+            }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float n = RowPiece<T>::get(cs[c], i) * r, g = RowPiece<T>::get(cg[c], i);
                 acc[c][i] += g * n;
-                v[i] = RowPiece<T>::get(cd[c], i) + r * (g * RowPiece<T>::get(pw[c], i) - n * k);
+                v[i] = RowPiece<T>::get(cd[c], i) + r * (g * RowPiece<T>::get(pw[c], i) - n * mn);
             }
             if (at < d) store_piece<T, ALIGNED>(dx + (size_t)row * d, at, d, v);
         }
     }
+    // The rows out of range, if there were any, in a loop of their own: handled above they cost every row registers and instructions (16384 x
+    // 8192: 221 us became 234 to 253).  For the same reason each of their passes loads the pieces again, from an address that hides where it
+    // is from.  Which rows they are is told by s alone (dy of the others may be their d_x by now), in the very operations of the loop above.
+    if (left)
+        for (row = first; row < rows; row += stride, flip ^= 1) {
+            const auto each = [&](const auto &f) {   // f(piece, its first element, pieces of s, dy, w)
+                size_t at0 = (size_t)row * d;
+                asm volatile("" : "+v"(at0));
+#pragma unroll
+                for (int c = 0; c < NP; ++c) {
+                    const int at = (lane + c * LANES) * V;
+                    f(c, at, load_piece<T, ALIGNED>(sum + at0, at, d), load_piece<T, ALIGNED>(dy + at0, at, d), load_piece<T, ALIGNED>(w, at, d));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            float ss, along, k = 1.f;
+            uint32_t top = 0;
+            const auto sums = [&]() {
+                ss = along = 0.f;
+                each([&](int, int, const u32x4 &a, const u32x4 &b, const u32x4 &e) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float v = RowPiece<T>::get(a, i), s = v * k;
+                        const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
+                        top = u > top ? u : top;
+                        ss = fmaf(s, s, ss);
+                        along += RowPiece<T>::get(b, i) * RowPiece<T>::get(e, i) * s;
+                    }
+                });
+                row_sums<W>(ss, along, lds, flip);
+            };
+            sums();
+            if (in_range(fmaf(ss, inv_d, eps))) continue;
+            // (every wavefront has read the last row's sums, which `flip ^ 1` held, and behind the next barrier this row's)
+            k = range_factor(row_most<W>(top, lds[flip ^ 1]), eps);
+            sums();
+            const float r = 1.f / sqrtf(ss * inv_d + eps * k * k), mn = along * r * inv_d;   // of the scaled row
+            each([&](int c, int at, const u32x4 &a, const u32x4 &b, const u32x4 &e) {
+                u32x4 old = {0, 0, 0, 0};
+                if (dsum) old = load_piece<T, ALIGNED>(dsum + (size_t)row * d, at, d);
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float n = RowPiece<T>::get(a, i) * k * r, g = RowPiece<T>::get(b, i);
+                    acc[c][i] += g * n;
+                    v[i] = RowPiece<T>::get(old, i) + r * ((g * RowPiece<T>::get(e, i) - n * mn) * k);
+                }
+                if (at < d) store_piece<T, ALIGNED>(dx + (size_t)row * d, at, d, v);
+            });
+        }
     // the block's column sums; with a row per wavefront the four wavefronts' are added in their order
     float *out = part + (size_t)blockIdx.x * d;
 #pragma unroll
@@ -378,14 +488,24 @@ struct BackwardCall {
     static constexpr bool kWide = true;
     const void *sum, *w, *dy, *dsum;
     void *dx;
-    float *part;
+    float *dw, *part;
     int rows, d, blocks;
     float eps;
     hipStream_t s;
+    // Blocks at most, those that are resident together: with more the last ones run beside half a chip (16384 x 8192 bf16, 512 / 768: 206 / 233
+    // us; 16384 x 4096 fp32 196 / 216; 8192 x 16384 bf16, 256 / 512 / 768: 312 / 327 / 344; 16384 x 8192 fp32 393 to 407 with any).
+    template <typename T, int W, int NP> static constexpr int most()
+    {
+        return W == 16 || (NP == 8 && RowPiece<T>::V == 8) ? kNormBackwardBlocks / 3 : NP >= 4 ? kNormBackwardBlocks * 2 / 3 : kNormBackwardBlocks;
+    }
     template <typename T, bool A, int W, int NP> hipError_t run() const
     {
-        add_rmsnorm_backward_kernel<T, A, W, NP><<<blocks, W == 16 ? 1024 : 256, 0, s>>>((const T *)sum, (const T *)w, (const T *)dy, (const T *)dsum,
-                                                                                       (T *)dx, part, rows, d, eps);
+        const int n = blocks < most<T, W, NP>() ? blocks : most<T, W, NP>();
+        add_rmsnorm_backward_kernel<T, A, W, NP><<<n, W == 16 ? 1024 : 256, 0, s>>>((const T *)sum, (const T *)w, (const T *)dy, (const T *)dsum,
+                                                                                  (T *)dx, part, rows, d, eps);   // (no rows: writes zeros to part)
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        norm_weight_sum_kernel<<<(d + 63) / 64, 1024, 0, s>>>(part, dw, n, d);
         return hipGetLastError();
     }
 };
@@ -403,12 +523,8 @@ hipError_t launch_add_rmsnorm(const slicemoe_norm_config &c, const void *x, cons
 hipError_t launch_add_rmsnorm_backward(const slicemoe_norm_config &c, const void *sum, const void *weight, const void *dy,
                                        const void *dsum, void *dx, float *dw, float *part, hipStream_t s)
 {
-    const int blocks = norm_backward_blocks(c.T);
-    const BackwardCall f{sum, weight, dy, dsum, dx, part, c.T, c.d, blocks, c.eps, s};
-    const hipError_t e = c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);   // T = 0 writes zeros to part
-    if (e != hipSuccess) return e;
-    norm_weight_sum_kernel<<<(c.d + 63) / 64, 1024, 0, s>>>(part, dw, blocks, c.d);
-    return hipGetLastError();
+    const BackwardCall f{sum, weight, dy, dsum, dx, dw, part, c.T, c.d, norm_backward_blocks(c.T), c.eps, s};
+    return c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);
 }
 
 }  // namespace slicemoe
