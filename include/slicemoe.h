@@ -396,8 +396,8 @@ typedef struct {
  *             grows
  * Products run on the bf16 matrix cores with fp32 accumulation.  bf16 storage: the hidden row silu(g) u is rounded to bf16
  * once between the products.  fp32 storage: every operand enters as three bf16 terms that keep its 24 bits, results of fp32 grade;
- * an infinity in an operand may come out as NaN; a forward pass of up to 256 fp32 rows and a backward pass of up to 64 run on the fp32
- * matrix instruction instead.
+ * a forward pass of up to 256 fp32 rows and a backward pass of up to 64 run on the fp32 matrix instruction instead.  Either way an
+ * infinity in an operand comes out as in fp32 arithmetic (as terms: unless it meets a nonzero value below 2^-86, which is NaN).
  * Widths that are not multiples of 8 (and fp32, but for those) are laid out again in the workspace first.
  * A row's result does not depend on the other rows, but the order of its sums depends on T.
  */

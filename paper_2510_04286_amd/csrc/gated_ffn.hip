@@ -23,10 +23,14 @@
 namespace slicemoe {
 
 // ---- fp32 values as bf16 terms -------------------------------------------------------------------------------------------
-// fp32 storage: an operand is the sum of three bf16 values, cut off rather than rounded, so that the first two remainders are exact
-// and all 24 bits are kept.  A product is the six products of terms whose orders add up to at most two, largest first (the matrix
-// instruction cuts its accumulator when the products outweigh it); what is left out is below 2^-24 of the product.  (A forward pass
-// of few rows is bound by the weights and takes the fp32 instruction instead: see gated_few_f32_kernel.)
+// fp32 storage: an operand is the sum of three bf16 values, cut off rather than rounded, so that the remainders are exact and all 24 bits
+// are kept.  A product is the six products of terms whose orders add up to at most two, largest first (the matrix instruction cuts its
+// accumulator when the products outweigh it); what is left out is below 2^-21 of the product and has its sign (for normal random operands
+// 2^-25 in the mean).  (A forward pass of few rows is bound by the weights and takes the fp32 instruction instead: see
+// gated_few_f32_kernel.)
+// An infinity is infinite in all three terms, and no term of a nonzero value is zero, since 2^-40 of the value is added to either
+// remainder: the six products then are infinities of the product's sign, as in fp32 arithmetic, where infinity times a zero term would be
+// NaN.  A NaN is one at least in the last term, whatever its payload.
 // Six bf16 products run at 2.6 times the rate of the fp32 matrix instruction; errors against 64 bits 4e-7 (the library's fp32
 // product: 7e-7).
 constexpr int kPairs = 6;
@@ -35,13 +39,13 @@ constexpr int kPairR[kPairs] = {0, 0, 1, 1, 0, 2}, kPairF[kPairs] = {0, 1, 0, 1,
 __device__ __forceinline__ void split_terms(float v, bf16_t (&t)[3])
 {
     const uint32_t b = __float_as_uint(v);
-    t[0] = (bf16_t)(b >> 16);
     const bool finite = (b & 0x7f800000u) != 0x7f800000u;
-    if ((b & 0x7fffffffu) > 0x7f800000u) t[0] |= 0x40;   // a NaN whose payload is in the lower half stays one
-    const float r1 = finite ? v - __uint_as_float(b & 0xffff0000u) : 0.f;
+    const float r1 = finite ? fmaf(v, 0x1p-40f, v - __uint_as_float(b & 0xffff0000u)) : v;
     const uint32_t b1 = __float_as_uint(r1);
+    const float r2 = finite ? fmaf(v, 0x1p-40f, r1 - __uint_as_float(b1 & 0xffff0000u)) : v;
+    t[0] = (bf16_t)(b >> 16);
     t[1] = (bf16_t)(b1 >> 16);
-    t[2] = f32_to_bf16(r1 - __uint_as_float(b1 & 0xffff0000u));
+    t[2] = f32_to_bf16(r2);
 }
 
 // Eight values of a row as bf16 terms, zeros past the row's end (up to a whole 16-byte piece).
