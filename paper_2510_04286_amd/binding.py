@@ -529,8 +529,9 @@ def slicemoe_gated_ffn_quantize_weights(cfg, w, Wg, Wg_scale, Wu, Wu_scale, stre
            "slicemoe_gated_ffn_quantize_weights")
 
 
-def quantize_gated_weights(cfg, w: dict, device="cuda:0") -> dict:
-    """The weight dict that slicemoe_gated_ffn_quantized takes, from the bf16 one (Wd is shared)."""
+def quantize_gated_weights(cfg, w: dict, device=None) -> dict:
+    """The weight dict that slicemoe_gated_ffn_quantized takes, from the bf16 one (Wd is shared), on the device of w."""
+    device = w["Wg"].device if device is None else device
     q = {n: torch.empty((cfg.H, cfg.d), dtype=torch.float8_e4m3fn, device=device) for n in ("Wg", "Wu")}
     q.update({n: torch.empty(cfg.H, dtype=torch.float32, device=device) for n in ("Wg_scale", "Wu_scale")})
     slicemoe_gated_ffn_quantize_weights(cfg, w, q["Wg"], q["Wg_scale"], q["Wu"], q["Wu_scale"])

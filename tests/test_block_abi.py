@@ -210,3 +210,16 @@ def test_binding_refuses_a_stream_of_another_device(B, monkeypatch):
     with pytest.raises(ValueError, match="is on device 1, the current device is 0"):
         B._ptr(OnDevice(1), None, None, "x", 0)
     assert isinstance(OnDevice(1), torch.Tensor)
+
+
+def test_quantized_weights_are_made_where_the_weights_are(B, monkeypatch):
+    import torch
+    made = {}
+
+    def pack(cfg, w, Wg, Wg_scale, Wu, Wu_scale, stream=None):
+        made.update(Wg=Wg, Wg_scale=Wg_scale, Wu=Wu, Wu_scale=Wu_scale)
+    monkeypatch.setattr(B, "slicemoe_gated_ffn_quantize_weights", pack)
+    w = {n: torch.empty((16, 8) if n != "Wd" else (8, 16), dtype=torch.bfloat16, device="meta") for n in ("Wg", "Wu", "Wd")}
+    q = B.quantize_gated_weights(B.make_gated_config(4, 16, 8), w)
+    assert sorted(made) == ["Wg", "Wg_scale", "Wu", "Wu_scale"] and all(q[n] is t and t.device.type == "meta" for n, t in made.items())
+    assert q["Wd"] is w["Wd"] and B.quantize_gated_weights(B.make_gated_config(4, 16, 8), w, device="cpu")["Wg"].device.type == "cpu"
