@@ -412,8 +412,15 @@ def slicemoe_backward(cfg, h, w, forward_workspace, d_out, d_h, grads: dict, wor
 
 
 # ------------------------------------------------------------------ operators around the layer
+_DTYPE_CODES = {**dict.fromkeys(("bf16", "bfloat16", torch.bfloat16, SLICEMOE_BF16), SLICEMOE_BF16),
+                **dict.fromkeys(("f32", "fp32", "float32", torch.float32, SLICEMOE_F32), SLICEMOE_F32)}
+
+
 def _dtype_code(dtype):
-    return SLICEMOE_BF16 if dtype in ("bf16", SLICEMOE_BF16) else SLICEMOE_F32
+    try:
+        return _DTYPE_CODES[dtype]
+    except (KeyError, TypeError):   # (TypeError: nothing that can be a name)
+        raise ValueError(f"dtype must be one of 'bf16', 'f32', torch.bfloat16 and torch.float32, got {dtype!r}") from None
 
 
 def make_norm_config(T, d, eps=1e-5, dtype="bf16") -> slicemoe_norm_config:

@@ -223,3 +223,13 @@ def test_quantized_weights_are_made_where_the_weights_are(B, monkeypatch):
     q = B.quantize_gated_weights(B.make_gated_config(4, 16, 8), w)
     assert sorted(made) == ["Wg", "Wg_scale", "Wu", "Wu_scale"] and all(q[n] is t and t.device.type == "meta" for n, t in made.items())
     assert q["Wd"] is w["Wd"] and B.quantize_gated_weights(B.make_gated_config(4, 16, 8), w, device="cpu")["Wg"].device.type == "cpu"
+
+
+def test_storage_types_by_name(B):
+    import torch
+    for make in (lambda t: B.make_norm_config(4, 16, 1e-5, t), lambda t: B.make_gated_config(4, 16, 8, t)):
+        assert all(make(t).dtype == B.SLICEMOE_BF16 for t in ("bf16", "bfloat16", torch.bfloat16, B.SLICEMOE_BF16))
+        assert all(make(t).dtype == B.SLICEMOE_F32 for t in ("f32", "fp32", "float32", torch.float32, B.SLICEMOE_F32))
+        for t in ("fp16", "BF16", torch.float16, torch.float64, torch.float8_e4m3fn, 2, -1, None, ["bf16"]):
+            with pytest.raises(ValueError, match="dtype must be"):
+                make(t)
