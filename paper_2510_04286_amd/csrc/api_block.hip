@@ -101,7 +101,7 @@ slicemoe_status slicemoe_add_rmsnorm(const slicemoe_norm_config *cfg, const void
 size_t slicemoe_add_rmsnorm_backward_workspace_bytes(const slicemoe_norm_config *cfg)
 {
     if (validate(cfg) != SLICEMOE_OK) return 0;
-    return align_up((size_t)norm_backward_blocks(cfg->T) * cfg->d * 4, 256);
+    return align_up((size_t)norm_backward_blocks(*cfg) * cfg->d * 4, 256);
 }
 
 slicemoe_status slicemoe_add_rmsnorm_backward(const slicemoe_norm_config *cfg, const void *sum, const void *weight, const void *d_y,

@@ -18,7 +18,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
 
 constexpr int kNormMaxWidth = 16384;        // what sixteen wavefronts hold of an fp32 row (four of a bf16 one)
 constexpr int kNormBackwardBlocks = 768;    // persistent blocks of the backward pass at most, three per CU (its registers): rows of partial weight gradients
-int norm_backward_blocks(int rows);
+int norm_backward_blocks(const slicemoe_norm_config &c);
 hipError_t launch_add_rmsnorm(const slicemoe_norm_config &c, const void *x, const void *residual, const void *weight, void *sum, void *y,
                               uint8_t *yq, float *yscale, hipStream_t s);
 hipError_t launch_add_rmsnorm_backward(const slicemoe_norm_config &c, const void *sum, const void *weight, const void *dy,

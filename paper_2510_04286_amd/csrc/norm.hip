@@ -510,7 +510,16 @@ struct BackwardCall {
     }
 };
 
-int norm_backward_blocks(int rows) { return rows < 1 ? 1 : rows < 4 * kNormBackwardBlocks ? (rows + 3) / 4 : kNormBackwardBlocks; }
+// Four rows per block: as many as it takes at once where a wavefront owns a row (up to 128 pieces: see pick_row).  Wider rows follow one
+// another in a block, so there a row each as long as that makes no more than a block per CU (256 x 4096 bf16: 11.3 -> 10.3 us, 16 x 16384:
+// 27 -> 16); with more blocks their partial rows cost more than they bring (1024 x 4096: 256 blocks 13.4, 768 20.0).
+int norm_backward_blocks(const slicemoe_norm_config &c)
+{
+    const int pieces = c.dtype == SLICEMOE_BF16 ? (c.d + 7) / 8 : (c.d + 3) / 4, fours = c.T / 4 + (c.T % 4 != 0);
+    const int each = pieces <= 128 ? 0 : c.T < kNormBackwardBlocks / 3 ? c.T : kNormBackwardBlocks / 3;
+    const int blocks = fours > each ? fours : each;
+    return blocks < 1 ? 1 : blocks < kNormBackwardBlocks ? blocks : kNormBackwardBlocks;
+}
 
 hipError_t launch_add_rmsnorm(const slicemoe_norm_config &c, const void *x, const void *residual, const void *weight, void *sum, void *y,
                               uint8_t *yq, float *yscale, hipStream_t s)
@@ -523,7 +532,7 @@ hipError_t launch_add_rmsnorm(const slicemoe_norm_config &c, const void *x, cons
 hipError_t launch_add_rmsnorm_backward(const slicemoe_norm_config &c, const void *sum, const void *weight, const void *dy,
                                        const void *dsum, void *dx, float *dw, float *part, hipStream_t s)
 {
-    const BackwardCall f{sum, weight, dy, dsum, dx, dw, part, c.T, c.d, norm_backward_blocks(c.T), c.eps, s};
+    const BackwardCall f{sum, weight, dy, dsum, dx, dw, part, c.T, c.d, norm_backward_blocks(c), c.eps, s};
     return c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);
 }
 

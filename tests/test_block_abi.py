@@ -233,3 +233,15 @@ def test_storage_types_by_name(B):
         for t in ("fp16", "BF16", torch.float16, torch.float64, torch.float8_e4m3fn, 2, -1, None, ["bf16"]):
             with pytest.raises(ValueError, match="dtype must be"):
                 make(t)
+
+
+@pytest.mark.parametrize("dtype,narrow", [("bf16", 1024), ("f32", 512)])
+def test_backward_blocks_of_wide_rows(B, dtype, narrow):
+    """A row of partial weight gradients per block: four rows a block where they go side by side, but a row each, up to one block per CU,
+    where a block takes one after the other."""
+    def blocks(T, d):
+        return B.slicemoe_add_rmsnorm_backward_workspace_bytes(B.make_norm_config(T, d, 1e-5, dtype)) // (4 * d)
+    for d, wide in ((narrow, False), (64, False), (2 * narrow, True), (16384, True)):
+        assert [blocks(T, d) for T in (0, 1, 5, 100, 256)] == ([1, 1, 5, 100, 256] if wide else [1, 1, 2, 25, 64])
+        assert [blocks(T, d) for T in (500, 1024)] == ([256, 256] if wide else [125, 256])
+        assert [blocks(T, d) for T in (1025, 3071, 10 ** 6, 2 ** 31 - 1)] == [257, 768, 768, 768]
