@@ -3,7 +3,10 @@
 //   norm = sqrt(sum over all tensors of g^2),   factor = min(1, max_norm / (norm + 1e-6)), 1 if max_norm is infinite,   out = g factor
 //
 // Two launches per kTensors tensors: every block squares and sums one chunk of one tensor, then every block adds up all chunks'
-// sums (about eight thousand at most, from L2, the same order in every block and every run) and scales its chunk.  Squares and sums are
+// sums (from L2, the same order in every block and every run) and scales its chunk.  There are kClipChunks of them and one more for each
+// tensor at most: from the third table on one block adds them up in between, since blocks times sums grow with the square of a list's
+// length (in each block / once, us: 96 tensors of 10000 values 7.8 / 8.9, 193 of 100000 70 / 60, 10000 of 1000 1294 / 806, 100000 of 1000
+// 54397 / 9322).  Squares and sums are
 // 64-bit: an fp32 value's square is exact there and cannot overflow, and the vector unit has the rate (one fma per four bytes
 // read).  The second pass walks chunks, and the pieces of a chunk, backwards: what the first one read last is still in the
 // last-level cache.
@@ -132,8 +135,9 @@ template <bool BF16> __device__ __forceinline__ u32x4 scaled(const u32x4 &p, flo
     return r;
 }
 
+// part: all chunks' sums, or none: the norm is in *norm already.
 template <bool BF16> __device__ __forceinline__ void scale_chunk(const ClipTable &t, const Chunk &c, const double *__restrict__ part, int parts,
-                                                                 float max_norm, float *norm_out, double *lds)
+                                                                 float max_norm, float *norm_out, bool write_norm, double *lds)
 {
     constexpr int V = BF16 ? 8 : 4, EL = BF16 ? 2 : 4, AHEAD = 8;
     const char *base = (const char *)t.in[c.tensor] + c.begin * EL;
@@ -145,9 +149,9 @@ template <bool BF16> __device__ __forceinline__ void scale_chunk(const ClipTable
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
         if (i - k * kClipThreads >= 0) p[k] = ((const loose *)base)[i - k * kClipThreads];
-    const float norm = total_norm(part, parts, lds);
+    const float norm = part ? total_norm(part, parts, lds) : *norm_out;
     const float q = max_norm / (norm + 1e-6f), f = q > 1.f || max_norm == INFINITY ? 1.f : q;   // (a NaN stays one; inf / inf does not)
-    if (norm_out && threadIdx.x == 0) *norm_out = norm;
+    if (write_norm && threadIdx.x == 0) *norm_out = norm;
     if (!out || (f == 1.f && t.out[c.tensor] == t.in[c.tensor])) return;
     out += c.begin * EL;
     while (i >= 0) {
@@ -166,13 +170,13 @@ template <bool BF16> __device__ __forceinline__ void scale_chunk(const ClipTable
 }
 
 __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipTable t, const double *__restrict__ part, int parts, float max_norm,
-                                                                  float *norm_out)
+                                                                  float *norm, bool write_norm)
 {
     __shared__ double lds[kClipThreads / 64];
     const Chunk c = find_chunk(t, (int)(gridDim.x - 1 - blockIdx.x));
-    float *no = blockIdx.x == 0 ? norm_out : nullptr;
-    if (c.bf16) scale_chunk<true>(t, c, part, parts, max_norm, no, lds);
-    else scale_chunk<false>(t, c, part, parts, max_norm, no, lds);
+    write_norm = write_norm && blockIdx.x == 0;
+    if (c.bf16) scale_chunk<true>(t, c, part, parts, max_norm, norm, write_norm, lds);
+    else scale_chunk<false>(t, c, part, parts, max_norm, norm, write_norm, lds);
 }
 
 __global__ __launch_bounds__(kClipThreads) void clip_norm_kernel(const double *__restrict__ part, int parts, float *norm_out)
@@ -187,7 +191,12 @@ ClipPlan clip_plan(const slicemoe_grad *g, int count)
 {
     ClipPlan p;
     double total = 0;
-    for (int i = 0; i < count; ++i) total += (double)g[i].n;
+    int tensors = 0;
+    for (int i = 0; i < count; ++i) {
+        total += (double)g[i].n;
+        tensors += g[i].n > 0;
+    }
+    p.once = tensors > 2 * kTensors;
     const double each = ceil(total / kClipChunks / 4096.) * 4096.;
     p.chunk = each < 4096. ? 4096 : each > (double)(1 << 29) ? 1 << 29 : (int)each;
     p.chunks = 0;
@@ -200,7 +209,7 @@ hipError_t launch_clip_grads(const slicemoe_grad *g, int count, const ClipPlan &
     bool scale = false;   // whether any tensor is written
     for (int pass = 0; pass < 2; ++pass) {
         int at = 0, done = 0;
-        bool norm_written = false;
+        bool norm_written = plan.once;
         while (done < count) {
             ClipTable t;
             t.count = 0;
@@ -221,16 +230,17 @@ hipError_t launch_clip_grads(const slicemoe_grad *g, int count, const ClipPlan &
             const int blocks = t.first[t.count];
             if (pass == 0) clip_squares_kernel<<<blocks, kClipThreads, 0, s>>>(t, part + at);
             else {
-                clip_scale_kernel<<<blocks, kClipThreads, 0, s>>>(t, part, (int)plan.chunks, max_norm, norm_written ? nullptr : norm);
+                clip_scale_kernel<<<blocks, kClipThreads, 0, s>>>(t, plan.once ? nullptr : part, (int)plan.chunks, max_norm, norm, !norm_written);
                 norm_written = true;
             }
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             at += blocks;
         }
-        if (pass == 0 && !scale) {   // nothing to scale: the norm alone
+        if (pass == 0 && (plan.once || !scale)) {   // (nothing to scale: the norm alone)
             clip_norm_kernel<<<1, kClipThreads, 0, s>>>(part, (int)plan.chunks, norm);
-            return hipGetLastError();
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || !scale) return e;
         }
     }
     return hipSuccess;
