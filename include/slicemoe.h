@@ -330,7 +330,7 @@ slicemoe_status slicemoe_backward(const slicemoe_config *cfg, const void *h, con
  * The layer reads normalised rows and adds to a residual stream (both outside of it, as in the paper), often beside a
  * feed-forward network that every token takes, and its gradients are bounded before an optimizer uses them.  The
  * conventions above hold for these entry points too: caller-allocated device memory, 16-byte aligned unless it says otherwise,
- * kernels on `stream` only (nothing here uses another stream), no allocation, no host synchronisation, bit-identical
+ * kernels on `stream` only (nothing here uses another stream), no device allocation, no host synchronisation, bit-identical
  * results for the same inputs, and calls may be captured into a HIP graph.  Calls that overlap in time need workspaces of
  * their own.  Arrays are contiguous and on the current device, which is the stream's; an output may take an input's place
  * only where that is said.
@@ -450,7 +450,8 @@ slicemoe_status slicemoe_gated_ffn_quantize_weights(const slicemoe_gated_config 
  *   norm      out float, 4-byte aligned
  *   workspace >= slicemoe_clip_grads_workspace_bytes(grads, count) (0 on invalid arguments), 256-byte aligned
  * out of a tensor may be its own grad (in place), or NULL (the tensor is measured, not written).  INVALID_ARG if any out overlaps
- * another tensor or its own grad in part: the same tensor listed twice, for instance.
+ * another tensor or its own grad in part: the same tensor listed twice, for instance.  (For that check a list of more than 512 tensors
+ * takes 48 bytes of host memory for each during the call, the one allocation of these entry points; SLICEMOE_ERR_HIP if there is none.)
  */
 typedef struct {
     const void *grad; /* n elements, aligned to its element size; may be NULL if n is 0 */

@@ -3,8 +3,8 @@
 #include <math.h>
 
 #include <algorithm>
+#include <memory>
 #include <new>
-#include <vector>
 
 #include "clip.h"
 #include "gated_ffn.h"
@@ -56,28 +56,40 @@ static slicemoe_status validate(const slicemoe_grad *g, int32_t count)
     return total > 1e12 || count > 1 << 20 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
 
-// Whether an array that is written overlaps any other array of the call but the very one it replaces.
-static bool writes_overlap(const slicemoe_grad *g, int32_t count)
+struct Range {
+    uintptr_t begin, end;
+    bool written;
+};
+constexpr int kOnStack = 512;   // tensors whose ranges (two each) are sorted on the stack, 24 KB; longer lists take host memory
+
+// Whether an array that is written overlaps any other array of the call but the very one it replaces.  r: room for 2 count ranges.
+static bool writes_overlap(const slicemoe_grad *g, int32_t count, Range *r)
 {
-    struct Range {
-        uintptr_t begin, end;
-        bool written;
-    };
-    std::vector<Range> r;
+    Range *last = r;
     for (int32_t i = 0; i < count; ++i) {
         if (g[i].n == 0) continue;
         const uintptr_t bytes = (uintptr_t)g[i].n * (g[i].dtype == SLICEMOE_BF16 ? 2 : 4);
         const uintptr_t a = (uintptr_t)g[i].grad, o = (uintptr_t)g[i].out;
-        r.push_back({a, a + bytes, o == a});
-        if (o && o != a) r.push_back({o, o + bytes, true});
+        *last++ = {a, a + bytes, o == a};
+        if (o && o != a) *last++ = {o, o + bytes, true};
     }
-    std::sort(r.begin(), r.end(), [](const Range &x, const Range &y) { return x.begin < y.begin; });
+    std::sort(r, last, [](const Range &x, const Range &y) { return x.begin < y.begin; });
     uintptr_t read_end = 0, write_end = 0;   // of the ranges so far
-    for (const Range &x : r) {
-        if (x.begin < write_end || (x.written && x.begin < read_end)) return true;
-        (x.written ? write_end : read_end) = std::max(x.written ? write_end : read_end, x.end);
+    for (const Range *x = r; x < last; ++x) {
+        if (x->begin < write_end || (x->written && x->begin < read_end)) return true;
+        (x->written ? write_end : read_end) = std::max(x->written ? write_end : read_end, x->end);
     }
     return false;
+}
+static slicemoe_status check_overlaps(const slicemoe_grad *g, int32_t count)
+{
+    if (count <= kOnStack) {
+        Range r[2 * kOnStack];
+        return writes_overlap(g, count, r) ? SLICEMOE_ERR_INVALID_ARG : SLICEMOE_OK;
+    }
+    const std::unique_ptr<Range[]> r(new (std::nothrow) Range[2 * (size_t)count]);
+    if (!r) return SLICEMOE_ERR_HIP;
+    return writes_overlap(g, count, r.get()) ? SLICEMOE_ERR_INVALID_ARG : SLICEMOE_OK;
 }
 
 }  // namespace slicemoe
@@ -208,11 +220,8 @@ slicemoe_status slicemoe_clip_grads(const slicemoe_grad *grads, int32_t count, f
     const ClipPlan plan = clip_plan(grads, count);
     st = check_workspace(workspace, workspace_bytes, align_up((size_t)plan.chunks * 8 + 1, 256));
     if (st != SLICEMOE_OK) return st;
-    try {
-        if (writes_overlap(grads, count)) return SLICEMOE_ERR_INVALID_ARG;
-    } catch (const std::bad_alloc &) {
-        return SLICEMOE_ERR_HIP;
-    }
+    st = check_overlaps(grads, count);
+    if (st != SLICEMOE_OK) return st;
     return status_of(launch_clip_grads(grads, count, plan, max_norm, norm, (double *)workspace, (hipStream_t)stream));
 }
 

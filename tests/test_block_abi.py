@@ -245,3 +245,36 @@ def test_backward_blocks_of_wide_rows(B, dtype, narrow):
         assert [blocks(T, d) for T in (0, 1, 5, 100, 256)] == ([1, 1, 5, 100, 256] if wide else [1, 1, 2, 25, 64])
         assert [blocks(T, d) for T in (500, 1024)] == ([256, 256] if wide else [125, 256])
         assert [blocks(T, d) for T in (1025, 3071, 10 ** 6, 2 ** 31 - 1)] == [257, 768, 768, 768]
+
+
+NO_MEMORY = """
+import ctypes, resource, sys
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+L = ctypes.CDLL(sys.argv[1])
+f = L.slicemoe_clip_grads
+f.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+lists = []
+for count in (512, 513, 1 << 20):   # each ends with its first tensor once more: refused, whatever memory there is, before anything is launched
+    a = (Grad * count)()
+    for i in range(count):
+        a[i].grad = a[i].out = (1 << 20) + 4096 * (i % (count - 1))
+        a[i].n = 4
+    lists.append((a, count))
+def call(a, count):
+    return f(ctypes.addressof(a), count, 1.0, 4096, 1 << 20, 1 << 40, None)
+print([call(*l) for l in lists])
+pages = int(open("/proc/self/statm").read().split()[0])
+resource.setrlimit(resource.RLIMIT_AS, (pages * 4096 + (8 << 20),) * 2)
+print([call(*l) for l in lists])
+"""
+
+
+def test_lists_are_checked_without_memory(B):
+    """Up to 512 tensors on the stack; a longer list that finds no memory is an error, not an exception through the C boundary."""
+    import subprocess
+    import sys
+    out = subprocess.run([sys.executable, "-c", NO_MEMORY, B.LIB_PATH], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0, out.stderr
+    inv, hip = B.SLICEMOE_ERR_INVALID_ARG, 4
+    assert out.stdout.split("\n")[:2] == [str([inv, inv, inv]), str([inv, inv, hip])]
