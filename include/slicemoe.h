@@ -424,7 +424,8 @@ slicemoe_status slicemoe_gated_ffn_backward(const slicemoe_gated_config *cfg, co
 /*
  * The network for serving with 8-bit operands in its first two products, the larger part of its work: x as
  * slicemoe_add_rmsnorm leaves it (e4m3 rows and their scales), Wg and Wu as slicemoe_gated_ffn_quantize_weights leaves them (row h
- * holds column h of the matrix, with a scale).  g = (x_quantized . Wg[h]) x_scale Wg_scale[h]; hidden rows, Wd, addend and y are bf16.
+ * holds column h of the matrix, with a scale).  g = (x_quantized . Wg[h]) x_scale Wg_scale[h]; hidden rows, Wd, addend (may be NULL)
+ * and y (may be addend) are bf16.
  * dtype must be SLICEMOE_BF16 and d a multiple of 16 (UNSUPPORTED otherwise).
  */
 typedef struct {
