@@ -351,7 +351,8 @@ typedef struct {
  *   weight    [d]    in
  *   sum       [T, d] out, s in the storage dtype; may be NULL; may be x or residual
  *   y         [T, d] out, storage dtype; may be NULL when y_quantized is given; may be x or residual if sum is not that one
- *   y_quantized [T, d] out, may be NULL: the same rows as OCP e4m3 bytes, y / y_scale rounded to nearest even
+ *   y_quantized [T, d] out, may be NULL: the same rows (y before its rounding) as OCP e4m3 bytes, y times the fp32 reciprocal of
+ *             y_scale, rounded to nearest even
  *   y_scale   [T] out float, with y_quantized: max|y| of the row / 448, where a maximum below 1e-30 counts as 1e-30 (a row
  *             of zeros); NaN for a row that holds a NaN or an infinity
  */
@@ -437,7 +438,7 @@ size_t slicemoe_gated_ffn_quantized_workspace_bytes(const slicemoe_gated_config 
 slicemoe_status slicemoe_gated_ffn_quantized(const slicemoe_gated_config *cfg, const void *x_quantized, const float *x_scale,
                                              const slicemoe_gated_weights_quantized *w, const void *addend, void *y,
                                              void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
-/* One-time conversion of Wg and Wu (cfg->T is not read): scale = max|column| / 448 as in slicemoe_add_rmsnorm. */
+/* One-time conversion of Wg and Wu (cfg->T is not read): scale = max|column| / 448, values and NaN scales as in slicemoe_add_rmsnorm. */
 slicemoe_status slicemoe_gated_ffn_quantize_weights(const slicemoe_gated_config *cfg, const slicemoe_gated_weights *w,
                                                     void *Wg, float *Wg_scale, void *Wu, float *Wu_scale,
                                                     slicemoe_stream_t stream);
