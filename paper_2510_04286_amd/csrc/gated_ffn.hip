@@ -4,16 +4,17 @@
 //   da = dy Wd^T,  dg = da u (sg + g sg (1 - sg)),  du = da g sg
 //   dx = addend + dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  dWd = a^T dy
 //
-// Every product is a tile of gemm_tile.h on the bf16 matrix cores with fp32 accumulation; no transposed copy of anything is made
-// (K-major operands are read transposed from the LDS).  Both projections share a tile, so that the gate is applied to the
-// accumulators; the backward pass computes them again beside da, and the three weight gradients are one launch.  g, u and da never leave
-// the chip; a, dg and du are rounded to bf16 once (bf16 storage), so an output holds that rounding and its own: 1.4 times the
-// error of one.
+// A product is a tile of gemm_tile.h on the bf16 matrix cores with fp32 accumulation (few fp32 rows: on the fp32 matrix instruction); no
+// transposed copy of anything is made (K-major operands are read transposed from the LDS).  Both projections share a tile, so that the
+// gate is applied to the accumulators; the backward pass computes them again beside da, and the three weight gradients are one launch.  g, u
+// and da stay on the chip, but where few tiles share out a long contraction: then their sums pass through memory in fp32.  a, dg and du are
+// rounded to bf16 once (bf16 storage), so an output holds that rounding and its own: 1.4 times the error of one.
 //
-// Bound by the matrix cores and, where they are busy, by power: at T 8192, d 4096, H 11008 (bf16) up 1063 us = 1.39 PFLOP/s, down 537 =
-// 1.38, gate backward 1789 = 1.24, weight gradients 1716 = 1.29, dx 1019 = 1.45, with the matrix pipes 70 to 81% busy at 1.65 to
-// 1.8 GHz (a large library product: 1.0 to 1.5 on the same card); 8-bit projections of 4096 rows 355 us = 2.08 PFLOP/s.  Cards differ by
-// 8%.  Short contractions pay their rounds' first trip and epilogue: 16 steps (d = 1024) 31 us a round, 23 of them steps.
+// Bound by the matrix cores and, where they are busy, by power: at T 8192, d 4096, H 11008 (bf16) up 1118 us = 1.32 PFLOP/s, down 562 =
+// 1.31, gate backward 1866 = 1.19, weight gradients 1779 = 1.25, dx 1074 = 1.38, with the matrix pipes 63 to 81% busy at 1.65 to
+// 1.8 GHz (a large library product: 1.0 to 1.5 on the same card); 8-bit projections of 4096 rows 374 us = 1.98 PFLOP/s.  Cards differ by
+// 8% (up: 1063 to 1148 us).  Short contractions pay their rounds' first trip and epilogue: 16 steps (d = 1024) 31 us a round, 23 of them
+// steps.
 #include <algorithm>
 
 #include "gated_ffn.h"
@@ -235,7 +236,7 @@ __device__ __forceinline__ void share_of(const GemmProblem &p, int split, int &s
     s1 = s0 + each < steps ? s0 + each : steps;
 }
 
-// Both projections and the gate (big tiles, T 16384, d 1024, H 2816: 184 to 200 us; the gate's exponential and reciprocal are 4 us
+// Both projections and the gate (big tiles, T 16384, d 1024, H 2816: 184 to 215 us; the gate's exponential and reciprocal are 4 us
 // of vector work per tile, the rows leave in whole 128-byte lines).
 template <typename S, int TERMS>
 __global__ __launch_bounds__(256) void gated_up_kernel(GemmProblem p, Hidden h, Scales sc)
@@ -699,7 +700,8 @@ __global__ __launch_bounds__(256) void gated_up_backward_kernel(GemmProblem p, G
 
 // ---- weights in e4m3 -----------------------------------------------------------------------------------------------------
 // Column h of W [d][H] becomes row h of the copy, with the scale of its largest value.  A block takes 32 columns: once for the
-// largest values, once more (from the cache) for the values, which turn in the LDS.
+// largest values, once more (from the cache) for the values, which turn in the LDS.  Done once for a set of weights: d 4096, H 11008 344 us,
+// d 1024, H 2816 38 us; 64-byte pieces of W's rows and few blocks keep it at 0.2 to 1.6 TB/s.
 __global__ __launch_bounds__(256) void gated_quantize_kernel(const bf16_t *__restrict__ Wg, const bf16_t *__restrict__ Wu, uint8_t *__restrict__ Qg,
                                                              uint8_t *__restrict__ Qu, float *__restrict__ sg, float *__restrict__ su, int d, int H)
 {
@@ -777,7 +779,8 @@ static int whole_shares(int steps, int n) { return steps == 0 ? 1 : ceil_div(ste
 // itself and of one that shares it, the rest of a round of tiles (launch, first round trip, epilogue), and for shares the launch of
 // their addition and their way through memory.  (T 8191, d 768, H 2048, big / wide / middle: up 61 / 71 / 70, down in two shares
 // 75 / 48 / 44, dx 86 / 71 / 67, weights in three shares 101 / 105 / 108; T 8192, d 4096, H 11008: up 1070 / 1276 / 1383, weights
-// 1712 / 1889 / 2759, dx 1040 / 1313 / 1514; fp32, T 1000, d 256, H 683: up 45 / 27 / 18.)
+// 1712 / 1889 / 2759, dx 1040 / 1313 / 1514; fp32, T 1000, d 256, H 683: up 45 / 27 / 18.)  Batches of 65 to some 2000 bf16 rows were not
+// among them.
 struct TileCost {
     int rows, features, slots;   // slots: tiles per CU
     double alone, shared, rest;
@@ -1034,6 +1037,9 @@ template <int FL, bool E4M3, int TERMS> static hipError_t launch_up(const GemmPr
             typedef decltype(shape) S;
             return run_up<S>(gated_up_few_kernel<S>, S::LDS, p, h, sc, s);
         };
+        // 64 features a block in bf16, two blocks per CU in 8 bits, where tiles of 32 features are more than the CUs; else the other form, on
+        // more of them.  (The call, T 8, d 4096, H 8192, then 8256, this form / the other, us: bf16 58.7 / 55.6, 49.6 / 57.3; 8 bits 32.2 / 32.0,
+        // 34.2 / 38.3; T 64: bf16 67.9 / 62.5, 60.3 / 68.3; H 2816 and 16384 of bf16: 43.0 / 39.9, 89.2 / 104.8.)
         const bool many = ceil_div(p.nf, 32) > num_compute_units();
         if constexpr (E4M3) {
             if (p.nr <= 32) return many ? few(FewShape<1, 1, FL, true, true, 2>()) : few(FewShape<1, 1, FL, true, true, 1>());

@@ -17,8 +17,8 @@
 // The e4m3 row: scale = max|y| / 448 (448: the largest e4m3 value), values y (1 / scale) rounded to nearest even.  A largest value below
 // 1e-30 counts as 1e-30, so a row of zeros has a scale and no division by zero; a row that holds a NaN or an infinity has a NaN scale.
 //
-// HBM-bound.  65536 rows of 4096 bf16 values: forward 367 us = 5.9 TB/s, backward 431 + 6 = 4.9 (a copy of the same size: 5.2); 12289 rows
-// of 768 with e4m3 output 13.5 us.  A decoding step's rows are their launch (32 x 1024: 3 us).  Rows that are not whole 16-byte pieces (d
+// HBM-bound.  65536 rows of 4096 bf16 values: forward 363 us = 5.9 TB/s, backward 430 + 6 = 4.9 (a copy of the same size: 5.2); 12289 rows
+// of 768 with e4m3 output 13.8 us.  A decoding step's rows are their launch (32 x 1024: 3 us).  Rows that are not whole 16-byte pieces (d
 // not a multiple of 8 for bf16, 4 for fp32) start at any element: their pieces are 16-byte accesses at element alignment, the last
 // piece element by element.
 #include "common.h"
