@@ -396,7 +396,8 @@ typedef struct {
  *   workspace >= slicemoe_gated_ffn_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; its size never falls as T
  *             grows
  * Products run on the bf16 matrix cores with fp32 accumulation.  bf16 storage: the hidden row silu(g) u is rounded to bf16
- * once between the products.  fp32 storage: every operand enters as three bf16 terms that keep its 24 bits, results of fp32 grade;
+ * once between the products.  fp32 storage: every operand enters as three bf16 terms that keep its 24 bits, results of fp32 grade
+ * (operands below some 2^-108 keep the bits above 2^-133: 2e-6 at 2^-116);
  * a forward pass of up to 256 fp32 rows and a backward pass of up to 64 run on the fp32 matrix instruction instead.  Either way an
  * infinity in an operand comes out as in fp32 arithmetic (as terms: unless it meets a nonzero value below 2^-86, which is NaN).
  * Widths that are not multiples of 8 (and fp32, but for those) are laid out again in the workspace first.

@@ -25,7 +25,7 @@ namespace slicemoe {
 
 // ---- fp32 values as bf16 terms -------------------------------------------------------------------------------------------
 // fp32 storage: an operand is the sum of three bf16 values, cut off rather than rounded, so that the remainders are exact and all 24 bits
-// are kept.  A product is the six products of terms whose orders add up to at most two, largest first (the matrix instruction cuts its
+// are kept (of a value below some 2^-108 those above 2^-133, bf16's smallest number).  A product is the six products of terms whose orders add up to at most two, largest first (the matrix instruction cuts its
 // accumulator when the products outweigh it); what is left out is below 2^-21 of the product and has its sign (for normal random operands
 // 2^-25 in the mean).  (A forward pass of few rows is bound by the weights and takes the fp32 instruction instead: see
 // gated_few_f32_kernel.)
