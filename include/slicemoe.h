@@ -259,6 +259,20 @@ slicemoe_status slicemoe_forward(const slicemoe_config *cfg, const void *h, cons
                                  slicemoe_stream_t stream);
 
 /*
+ * The whole layer for a few tokens (a decoding step) in one launch, without a workspace: h[T, d] -> h_out[T, d] as slicemoe_forward, which
+ * takes four launches whatever the batch.  A block has a slice from its router to its sum.  On the matrix-core path (slicemoe_uses_mfma)
+ * it reads w->packed, which has to be there (the logical tensors may be NULL), and gives the bits of slicemoe_forward; otherwise it reads the logical
+ * tensors, in fp32.
+ *   topk_idx, topk_p [T*S, k] out, as slicemoe_route leaves them; may be NULL, each
+ *   h_out     may be h
+ * UNSUPPORTED for more than SLICEMOE_FEW_ASSIGNMENTS assignments (T*S*k), for a capacity limit, and where the k He hidden units of a slice do not fit
+ * the LDS (k * He > 61 thousand): these are slicemoe_forward's.
+ */
+#define SLICEMOE_FEW_ASSIGNMENTS 4096
+slicemoe_status slicemoe_forward_few(const slicemoe_config *cfg, const void *h, const slicemoe_weights *w, void *h_out,
+                                     int32_t *topk_idx, float *topk_p, slicemoe_stream_t stream);
+
+/*
  * Whole layer with the training-time router: slicemoe_forward with slicemoe_route_train in place of slicemoe_route
  * (same parameters and tables of draws); dispatch, expert FFN (Eq. 1 with the dropped-and-renormalised probabilities)
  * and combine are unchanged.
@@ -465,6 +479,114 @@ typedef struct {
 size_t slicemoe_clip_grads_workspace_bytes(const slicemoe_grad *grads, int32_t count);
 slicemoe_status slicemoe_clip_grads(const slicemoe_grad *grads, int32_t count, float max_norm, float *norm,
                                     void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
+
+/*
+ * Microscaled values: 32 consecutive columns of a row share a power of two 2^e, each is an OCP e2m1 (4 bits) or e4m3 (8 bits) value
+ * times it, rounded to nearest even.  2^e is the least power of two that brings the block's largest magnitude to at most 6 (448), so
+ * nothing saturates; at least 2^-127 (a block of zeros).  A block that holds an infinity or a NaN is NaN throughout.
+ * A matrix lies in the order of the matrix instruction, in tiles of 32 rows x 256 columns (Kt = ceil(cols / 256); zeros past the last
+ * column; what is past the last row is not read for any result): tile (rt, kt) is number rt Kt + kt and has 1024 bits bytes; its block
+ * b = 2 ks + h (columns 32 b ..) of row i holds column c at position p = 16 (c / 4 % 2) + 4 (c / 8 % 4) + c % 4,
+ *   bits = 4   in nibble p % 2 of byte 1024 ks + 16 (i + 32 h) + p / 2 (low nibble first)
+ *   bits = 8   in byte 2048 ks + 1024 h + 16 (i + 32 (p / 16)) + p % 16
+ * and behind the last tile's values follow 256 bytes of scales per tile: byte 4 (i + 32 h) + ks holds e + 127, or 255 for NaN.
+ */
+typedef struct {
+    int32_t rows;       /* 0 <= rows                                                             */
+    int32_t cols;       /* the contracted width, 1 <= cols <= 2^20; rows * cols <= 2^40          */
+    int32_t bits;       /* 4 or 8                                                                */
+    int32_t dtype;      /* slicemoe_dtype of the plain matrix                                    */
+    int32_t transposed; /* the plain matrix is [cols, rows]: a weight stored [in, out]           */
+} slicemoe_mx_config;
+
+/* Bytes of the packed matrix (0 on an invalid config); 256-byte aligned. */
+size_t slicemoe_mx_bytes(const slicemoe_mx_config *cfg);
+/* x [rows, cols] (or [cols, rows]) in -> mx out, and back (each value rounded once to dtype; e2m1 and e4m3 values are bf16 ones). */
+slicemoe_status slicemoe_mx_quantize(const slicemoe_mx_config *cfg, const void *x, void *mx, slicemoe_stream_t stream);
+slicemoe_status slicemoe_mx_dequantize(const slicemoe_mx_config *cfg, const void *mx, void *x, slicemoe_stream_t stream);
+
+/*
+ * Product of microscaled matrices: y = addend + X W^T on the scaled matrix instruction, fp32 accumulation.  (With 8-bit rows the instruction
+ * aligns the products of eight columns to the largest and drops what is below 2^-13 of it: some 1e-5 of the magnitudes that are added
+ * up.  With 4-bit rows every product counts whole.)
+ *   x_mx  T rows of K columns, in cfg->bits;  w_mx  N rows of K columns, in 4 bits
+ *   addend [T, N] in, storage dtype, may be NULL (zero);  y [T, N] out, one rounding; may be addend
+ *   workspace >= slicemoe_mx_product_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; may be NULL where that is 0
+ * A row's result does not depend on the other rows, but the order of its sums depends on T.
+ */
+typedef struct {
+    int32_t T;     /* rows, 0 <= T <= 2^24                              */
+    int32_t K;     /* contracted width, 1 <= K <= 2^20                  */
+    int32_t N;     /* outputs, 1 <= N <= 2^20; T * max(K, N) <= 2^40    */
+    int32_t bits;  /* of the rows: 4 or 8                               */
+    int32_t dtype; /* slicemoe_dtype of addend and y                    */
+} slicemoe_mx_product_config;
+size_t slicemoe_mx_product_workspace_bytes(const slicemoe_mx_product_config *cfg);
+slicemoe_status slicemoe_mx_product(const slicemoe_mx_product_config *cfg, const void *x_mx, const void *w_mx, const void *addend, void *y,
+                                    void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
+
+/*
+ * The gated network on microscaled operands: y = addend + (silu(x Wg) * (x Wu)) Wd with x_mx and the hidden rows in `bits` (the hidden
+ * rows are taken in fp32, rounded once), the weights in 4 bits.
+ *   cfg   dtype must be SLICEMOE_BF16, T <= 2^24 (UNSUPPORTED otherwise)
+ *   x_mx  T rows of d columns, in `bits`
+ *   w     Wg, Wu: H rows of d columns; Wd: d rows of H columns, all in 4 bits (from the [in, out] matrices with transposed = 1)
+ *   addend [T, d] in, may be NULL;  y [T, d] out, may be addend
+ *   workspace >= slicemoe_gated_ffn_mx_workspace_bytes(cfg, bits) (0 on invalid arguments), 256-byte aligned
+ */
+typedef struct {
+    const void *Wg, *Wu, *Wd;
+} slicemoe_gated_weights_mx;
+size_t slicemoe_gated_ffn_mx_workspace_bytes(const slicemoe_gated_config *cfg, int32_t bits);
+slicemoe_status slicemoe_gated_ffn_mx(const slicemoe_gated_config *cfg, int32_t bits, const void *x_mx, const slicemoe_gated_weights_mx *w,
+                                      const void *addend, void *y, void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
+
+/*
+ * Norms on both sides of a block's addition to the residual stream, with the block's gate and the stream's scale:
+ *   n = x / rms(x) * post_weight,  s = residual_scale * residual + gate * n,  y = s / rms(s) * pre_weight,  rms(v) = sqrt(mean(v^2) + eps)
+ * in fp32 throughout; y is taken of the fp32 sum and rounded once.  Rows whose squares leave the range of fp32 are scaled as in
+ * slicemoe_add_rmsnorm.
+ *   x           [T, d] in, the block's output
+ *   post_weight [d]    in; NULL: no norm behind the block, n = x
+ *   gate        [d] or [T, d] in (cfg->gate), NULL with SLICEMOE_GATE_NONE (a gate of ones)
+ *   residual    [T, d] in
+ *   pre_weight  [d]    in; NULL: no norm in front of the next block (y and y_mx NULL too)
+ *   sum         [T, d] out, s in the storage dtype; may be x or residual
+ *   y           [T, d] out, storage dtype; may be NULL; may be x or residual if sum is not that one
+ *   y_mx        out, the same rows (y before its rounding) as microscaled values of y_bits bits: slicemoe_mx_bytes of T rows and d columns,
+ *               256-byte aligned; may be NULL.  Rows past T are left as they were.  With pre_weight y or y_mx has to be there.
+ *   stats       [T, 2] out float, 8-byte aligned, for the backward pass: 1 / rms(x) (1 without post_weight) and 1 / rms(s); may be NULL.
+ *               (Infinite for a row below 2^-126 with eps = 0; its gradients are then not finite.)
+ */
+typedef enum { SLICEMOE_GATE_NONE = 0, SLICEMOE_GATE_CHANNEL = 1, SLICEMOE_GATE_TOKEN = 2 } slicemoe_gate;
+typedef struct {
+    int32_t T;            /* rows (tokens), 0 <= T                      */
+    int32_t d;            /* row width, 1 <= d <= 16384                 */
+    float eps;            /* >= 0, finite                               */
+    float residual_scale; /* finite                                     */
+    int32_t gate;         /* slicemoe_gate                              */
+    int32_t dtype;        /* slicemoe_dtype                             */
+} slicemoe_block_norm_config;
+slicemoe_status slicemoe_block_norm(const slicemoe_block_norm_config *cfg, const void *x, const void *post_weight, const void *gate,
+                                    const void *residual, const void *pre_weight, void *sum, void *y, void *y_mx, int32_t y_bits,
+                                    float *stats, slicemoe_stream_t stream);
+
+/*
+ * Its backward pass:
+ *   x, post_weight, gate, pre_weight  as given to the forward (post_weight and gate may be NULL as there; pre_weight may not);
+ *   sum, stats                        as the forward left them
+ *   d_y   [T, d] in, dL/dy
+ *   d_sum [T, d] in, the gradient that reaches s along the residual stream; may be NULL (zero)
+ *   d_x, d_residual [T, d] out, storage dtype, one rounding; each may be d_y or d_sum (not both the same)
+ *   d_post_weight, d_pre_weight [d] out float, overwritten (zeros for T = 0); d_post_weight is not written without post_weight
+ *   d_gate SLICEMOE_GATE_CHANNEL: [d] out float, overwritten; SLICEMOE_GATE_TOKEN: [T, d] out, storage dtype; else not written
+ *   workspace >= slicemoe_block_norm_backward_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; its size never falls as T grows
+ */
+size_t slicemoe_block_norm_backward_workspace_bytes(const slicemoe_block_norm_config *cfg);
+slicemoe_status slicemoe_block_norm_backward(const slicemoe_block_norm_config *cfg, const void *x, const void *post_weight, const void *gate,
+                                             const void *sum, const void *pre_weight, const float *stats, const void *d_y, const void *d_sum,
+                                             void *d_x, void *d_residual, float *d_post_weight, void *d_gate, float *d_pre_weight,
+                                             void *workspace, size_t workspace_bytes, slicemoe_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,10 @@ SLICEMOE_ERR_WORKSPACE = 3
 SLICEMOE_ERR_HIP = 4
 SLICEMOE_F32 = 0
 SLICEMOE_BF16 = 1
+SLICEMOE_GATE_NONE = 0
+SLICEMOE_GATE_CHANNEL = 1
+SLICEMOE_GATE_TOKEN = 2
+SLICEMOE_FEW_ASSIGNMENTS = 4096
 SLICEMOE_FLAG_FORCE_GENERIC = 1
 SLICEMOE_FLAG_REQUIRE_MFMA = 2
 SLICEMOE_FLAG_SINGLE_STREAM = 4
@@ -39,6 +43,9 @@ EXPORTS = [
     "slicemoe_gated_ffn_workspace_bytes", "slicemoe_gated_ffn", "slicemoe_gated_ffn_backward_workspace_bytes",
     "slicemoe_gated_ffn_backward", "slicemoe_gated_ffn_quantized_workspace_bytes", "slicemoe_gated_ffn_quantized",
     "slicemoe_gated_ffn_quantize_weights", "slicemoe_clip_grads_workspace_bytes", "slicemoe_clip_grads",
+    "slicemoe_forward_few", "slicemoe_block_norm", "slicemoe_block_norm_backward_workspace_bytes", "slicemoe_block_norm_backward",
+    "slicemoe_mx_bytes", "slicemoe_mx_quantize", "slicemoe_mx_dequantize", "slicemoe_mx_product_workspace_bytes", "slicemoe_mx_product",
+    "slicemoe_gated_ffn_mx_workspace_bytes", "slicemoe_gated_ffn_mx",
 ]
 
 
@@ -94,6 +101,23 @@ class slicemoe_gated_weights_quantized(ctypes.Structure):
 
 class slicemoe_grad(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class slicemoe_block_norm_config(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("gate", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class slicemoe_mx_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "bits", "dtype", "transposed")]
+
+
+class slicemoe_mx_product_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "K", "N", "bits", "dtype")]
+
+
+class slicemoe_gated_weights_mx(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("Wg", "Wu", "Wd")]
 
 
 _lib = None
@@ -159,6 +183,17 @@ def lib() -> ctypes.CDLL:
                      (L.slicemoe_gated_ffn_quantized, [gcp, vp, vp, ctypes.POINTER(slicemoe_gated_weights_quantized), vp, vp, vp, st, vp]),
                      (L.slicemoe_gated_ffn_quantize_weights, [gcp, gwp, vp, vp, vp, vp, vp]),
                      (L.slicemoe_clip_grads, [grp, ctypes.c_int32, ctypes.c_float, vp, vp, st, vp])):
+            f.restype, f.argtypes = ctypes.c_int, a
+        i32, bnp, mxp, mpp = ctypes.c_int32, ctypes.POINTER(slicemoe_block_norm_config), ctypes.POINTER(slicemoe_mx_config), ctypes.POINTER(slicemoe_mx_product_config)
+        for f, a in ((L.slicemoe_block_norm_backward_workspace_bytes, [bnp]), (L.slicemoe_mx_bytes, [mxp]),
+                     (L.slicemoe_mx_product_workspace_bytes, [mpp]), (L.slicemoe_gated_ffn_mx_workspace_bytes, [gcp, i32])):
+            f.restype, f.argtypes = st, a
+        for f, a in ((L.slicemoe_forward_few, [cfgp, vp, wp, vp, vp, vp, vp]),
+                     (L.slicemoe_block_norm, [bnp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp]),
+                     (L.slicemoe_block_norm_backward, [bnp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, st, vp]),
+                     (L.slicemoe_mx_quantize, [mxp, vp, vp, vp]), (L.slicemoe_mx_dequantize, [mxp, vp, vp, vp]),
+                     (L.slicemoe_mx_product, [mpp, vp, vp, vp, vp, vp, st, vp]),
+                     (L.slicemoe_gated_ffn_mx, [gcp, i32, vp, ctypes.POINTER(slicemoe_gated_weights_mx), vp, vp, vp, st, vp])):
             f.restype, f.argtypes = ctypes.c_int, a
         _lib = L
     return _lib
@@ -335,6 +370,23 @@ def slicemoe_forward(cfg, h, w, h_out, workspace, stream=None):
     _check(lib().slicemoe_forward(ctypes.byref(cfg), _ptr(h, _tdtype(cfg), cfg.T * cfg.d, "h"), ctypes.byref(ws),
                                   _ptr(h_out, _tdtype(cfg), cfg.T * cfg.d, "h_out"), wsp, wsb, _stream(stream)),
            "slicemoe_forward")
+
+
+def slicemoe_forward_few(cfg, h, w, h_out, topk_idx=None, topk_p=None, stream=None):
+    """The layer for a few tokens in one launch; on the matrix-core path w needs its 'packed' buffer and nothing else."""
+    L, dev, Na = _lib or lib(), _device(), cfg.T * cfg.S * cfg.k
+    dt, n = _tdtype(cfg), cfg.T * cfg.d
+    need = L.slicemoe_packed_bytes(ctypes.byref(cfg))   # 0: generic
+    if need:
+        ws = slicemoe_weights(None, None, None, None, None, None, None, None, _ptr(w.get("packed"), torch.uint8, need, "packed", dev))
+    else:
+        for name, t in w.items():
+            _ptr(t, None, None, name, dev)
+        ws = _weights(cfg, w)
+    st = L.slicemoe_forward_few(ctypes.byref(cfg), _ptr(h, dt, n, "h", dev), ctypes.byref(ws), _ptr(h_out, dt, n, "h_out", dev),
+                                _ptr(topk_idx, torch.int32, Na, "topk_idx", dev), _ptr(topk_p, torch.float32, Na, "topk_p", dev), _stream_on(dev, stream))
+    if st:
+        _check(st, "slicemoe_forward_few")
 
 
 def _train_args(cfg, temperature, noise_std, dropout_rate, noise, drop_u, capacity_alpha=0.0):
@@ -600,6 +652,127 @@ def slicemoe_clip_grads(grads, max_norm, norm, workspace, out=None, stream=None)
     packed = _grad_list(grads, out, dev)
     _check(lib().slicemoe_clip_grads(_grad_pointer(packed), len(grads), max_norm, _ptr(norm, torch.float32, 1, "norm", dev), wsp, wsb,
                                      _stream_on(dev, stream)), "slicemoe_clip_grads")
+
+
+_GATE_CODES = {None: SLICEMOE_GATE_NONE, "channel": SLICEMOE_GATE_CHANNEL, "token": SLICEMOE_GATE_TOKEN}
+
+
+def make_block_norm_config(T, d, eps=1e-5, residual_scale=1.0, gate="channel", dtype="bf16") -> slicemoe_block_norm_config:
+    """gate: None, "channel" (one row [d] for all tokens) or "token" (a row for each, [T, d])."""
+    if gate not in _GATE_CODES:
+        raise ValueError(f"gate must be None, 'channel' or 'token', got {gate!r}")
+    return slicemoe_block_norm_config(T, d, float(eps), float(residual_scale), _GATE_CODES[gate], _dtype_code(dtype))
+
+
+def make_mx_config(rows, cols, bits=4, dtype="bf16", transposed=False) -> slicemoe_mx_config:
+    return slicemoe_mx_config(rows, cols, bits, _dtype_code(dtype), int(transposed))
+
+
+def make_mx_product_config(T, K, N, bits=4, dtype="bf16") -> slicemoe_mx_product_config:
+    return slicemoe_mx_product_config(T, K, N, bits, _dtype_code(dtype))
+
+
+def slicemoe_mx_bytes(cfg) -> int:
+    return (_lib or lib()).slicemoe_mx_bytes(ctypes.byref(cfg))
+
+
+def _mx_ptr(t, rows, cols, bits, name, dev):
+    """Address of a packed matrix of microscaled values."""
+    return _ptr(t, torch.uint8, -(-rows // 32) * -(-cols // 256) * (1024 * bits + 256), name, dev)
+
+
+def _gate_numel(cfg):
+    return cfg.T * cfg.d if cfg.gate == SLICEMOE_GATE_TOKEN else cfg.d
+
+
+def slicemoe_block_norm(cfg, x, post_weight, gate, residual, pre_weight, sum_out, y, y_mx=None, y_bits=0, stats=None, stream=None):
+    """post_weight, gate (as cfg says), y with y_mx, and pre_weight with both of them, may be None."""
+    d, T, dev = cfg.d, cfg.T, _device()
+    dt, n = _tdtype(cfg), T * d
+    st = (_lib or lib()).slicemoe_block_norm(
+        ctypes.byref(cfg), _ptr(x, dt, n, "x", dev), _ptr(post_weight, dt, d, "post_weight", dev), _ptr(gate, dt, _gate_numel(cfg), "gate", dev),
+        _ptr(residual, dt, n, "residual", dev), _ptr(pre_weight, dt, d, "pre_weight", dev), _ptr(sum_out, dt, n, "sum_out", dev), _ptr(y, dt, n, "y", dev),
+        None if y_mx is None else _mx_ptr(y_mx, T, d, y_bits, "y_mx", dev), y_bits,
+        None if stats is None else _ptr(stats, torch.float32, 2 * T, "stats", dev), _stream_on(dev, stream))
+    if st:
+        _check(st, "slicemoe_block_norm")
+
+
+def slicemoe_block_norm_backward_workspace_bytes(cfg) -> int:
+    return lib().slicemoe_block_norm_backward_workspace_bytes(ctypes.byref(cfg))
+
+
+def slicemoe_block_norm_backward(cfg, x, post_weight, gate, sum_in, pre_weight, stats, d_y, d_x, d_residual, d_post_weight, d_gate, d_pre_weight,
+                                 workspace, d_sum=None, stream=None):
+    """d_gate: float32 [d] with a "channel" gate, [T, d] of the storage type with a "token" one; None without; d_post_weight likewise."""
+    d, T, dev = cfg.d, cfg.T, _device()
+    dt, n, f32 = _tdtype(cfg), T * d, torch.float32
+    wsp, wsb = _ws(workspace, dev)
+    st = (_lib or lib()).slicemoe_block_norm_backward(
+        ctypes.byref(cfg), _ptr(x, dt, n, "x", dev), _ptr(post_weight, dt, d, "post_weight", dev), _ptr(gate, dt, _gate_numel(cfg), "gate", dev),
+        _ptr(sum_in, dt, n, "sum_in", dev), _ptr(pre_weight, dt, d, "pre_weight", dev), _ptr(stats, f32, 2 * T, "stats", dev), _ptr(d_y, dt, n, "d_y", dev),
+        _ptr(d_sum, dt, n, "d_sum", dev), _ptr(d_x, dt, n, "d_x", dev), _ptr(d_residual, dt, n, "d_residual", dev),
+        _ptr(d_post_weight, f32, d, "d_post_weight", dev), _ptr(d_gate, dt if cfg.gate == SLICEMOE_GATE_TOKEN else f32, _gate_numel(cfg), "d_gate", dev),
+        _ptr(d_pre_weight, f32, d, "d_pre_weight", dev), wsp, wsb, _stream_on(dev, stream))
+    if st:
+        _check(st, "slicemoe_block_norm_backward")
+
+
+def slicemoe_mx_quantize(cfg, x, mx, stream=None):
+    """x: [rows, cols], or [cols, rows] with cfg.transposed -> mx, a uint8 buffer of slicemoe_mx_bytes."""
+    dev = _device()
+    st = (_lib or lib()).slicemoe_mx_quantize(ctypes.byref(cfg), _ptr(x, _tdtype(cfg), cfg.rows * cfg.cols, "x", dev),
+                                              _mx_ptr(mx, cfg.rows, cfg.cols, cfg.bits, "mx", dev), _stream_on(dev, stream))
+    if st:
+        _check(st, "slicemoe_mx_quantize")
+
+
+def slicemoe_mx_dequantize(cfg, mx, x, stream=None):
+    dev = _device()
+    _check((_lib or lib()).slicemoe_mx_dequantize(ctypes.byref(cfg), _mx_ptr(mx, cfg.rows, cfg.cols, cfg.bits, "mx", dev),
+                                                  _ptr(x, _tdtype(cfg), cfg.rows * cfg.cols, "x", dev), _stream_on(dev, stream)), "slicemoe_mx_dequantize")
+
+
+def quantize_mx(t, bits=4, transposed=False) -> torch.Tensor:
+    """The packed matrix of a 2-d tensor (of its transpose: a weight stored [in, out]), on its device."""
+    rows, cols = (t.shape[1], t.shape[0]) if transposed else t.shape
+    cfg = make_mx_config(rows, cols, bits, t.dtype, transposed)
+    mx = torch.empty(slicemoe_mx_bytes(cfg), dtype=torch.uint8, device=t.device)
+    slicemoe_mx_quantize(cfg, t, mx)
+    return mx
+
+
+def slicemoe_mx_product_workspace_bytes(cfg) -> int:
+    return lib().slicemoe_mx_product_workspace_bytes(ctypes.byref(cfg))
+
+
+def slicemoe_mx_product(cfg, x_mx, w_mx, y, workspace=None, addend=None, stream=None):
+    dt, n, dev = _tdtype(cfg), cfg.T * cfg.N, _device()
+    wsp, wsb = _ws(workspace, dev)
+    st = (_lib or lib()).slicemoe_mx_product(ctypes.byref(cfg), _mx_ptr(x_mx, cfg.T, cfg.K, cfg.bits, "x_mx", dev), _mx_ptr(w_mx, cfg.N, cfg.K, 4, "w_mx", dev),
+                                             _ptr(addend, dt, n, "addend", dev), _ptr(y, dt, n, "y", dev), wsp, wsb, _stream_on(dev, stream))
+    if st:
+        _check(st, "slicemoe_mx_product")
+
+
+def slicemoe_gated_ffn_mx_workspace_bytes(cfg, bits) -> int:
+    return lib().slicemoe_gated_ffn_mx_workspace_bytes(ctypes.byref(cfg), bits)
+
+
+def slicemoe_gated_ffn_mx(cfg, bits, x_mx, w, y, workspace, addend=None, stream=None):
+    """w: dict of packed Wg, Wu (H rows of d columns) and Wd (d rows of H columns), see quantize_gated_weights_mx."""
+    dt, n, dev, d, H = _tdtype(cfg), cfg.T * cfg.d, _device(), cfg.d, cfg.H
+    wsp, wsb = _ws(workspace, dev)
+    ws = slicemoe_gated_weights_mx(_mx_ptr(w["Wg"], H, d, 4, "Wg", dev), _mx_ptr(w["Wu"], H, d, 4, "Wu", dev), _mx_ptr(w["Wd"], d, H, 4, "Wd", dev))
+    st = (_lib or lib()).slicemoe_gated_ffn_mx(ctypes.byref(cfg), bits, _mx_ptr(x_mx, cfg.T, d, bits, "x_mx", dev), ctypes.byref(ws),
+                                               _ptr(addend, dt, n, "addend", dev), _ptr(y, dt, n, "y", dev), wsp, wsb, _stream_on(dev, stream))
+    if st:
+        _check(st, "slicemoe_gated_ffn_mx")
+
+
+def quantize_gated_weights_mx(w: dict) -> dict:
+    """The weight dict that slicemoe_gated_ffn_mx takes, from Wg, Wu [d, H] and Wd [H, d]."""
+    return {n: quantize_mx(w[n], 4, transposed=True) for n in ("Wg", "Wu", "Wd")}
 
 
 # ------------------------------------------------------------------ plumbing helpers (device memory only)

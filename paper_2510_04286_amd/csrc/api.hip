@@ -440,6 +440,20 @@ slicemoe_status slicemoe_forward(const slicemoe_config *cfg, const void *h, cons
     return forward_common(cfg, h, w, RouteVariant(), h_out, workspace, workspace_bytes, stream);
 }
 
+slicemoe_status slicemoe_forward_few(const slicemoe_config *cfg, const void *h, const slicemoe_weights *w, void *h_out, int32_t *topk_idx,
+                                     float *topk_p, slicemoe_stream_t stream)
+{
+    const slicemoe_status st = validate(cfg);
+    if (st != SLICEMOE_OK) return st;
+    const bool mfma = use_mfma(*cfg);
+    if ((long long)cfg->T * cfg->S * cfg->k > SLICEMOE_FEW_ASSIGNMENTS || cfg->capacity_factor > 0.f || few_lds_bytes(*cfg, mfma) > kFewMaxLds)
+        return SLICEMOE_ERR_UNSUPPORTED;
+    if (!w || (cfg->T > 0 && (!h || !h_out))) return SLICEMOE_ERR_INVALID_ARG;
+    if (mfma ? !w->packed || misaligned(w->packed, 256) : !logical_weights_ok(*w, true, true)) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(h, 16) || misaligned(h_out, 16) || misaligned(topk_idx, 4) || misaligned(topk_p, 4)) return SLICEMOE_ERR_INVALID_ARG;
+    return launch_forward_few(*cfg, h, *w, mfma, h_out, topk_idx, topk_p, (hipStream_t)stream) == hipSuccess ? SLICEMOE_OK : SLICEMOE_ERR_HIP;
+}
+
 slicemoe_status slicemoe_forward_train(const slicemoe_config *cfg, const void *h, const slicemoe_weights *w,
                                        const slicemoe_route_train_params *params, const float *noise,
                                        const float *drop_u, void *h_out, void *workspace, size_t workspace_bytes,

@@ -6,8 +6,11 @@
 #include <memory>
 #include <new>
 
+#include "block_norm.h"
 #include "clip.h"
 #include "gated_ffn.h"
+#include "mx.h"
+#include "mx_gemm.h"
 #include "norm.h"
 
 namespace slicemoe {
@@ -35,6 +38,35 @@ static slicemoe_status validate_quantized(const slicemoe_gated_config *c)
     const slicemoe_status st = validate(c);
     if (st != SLICEMOE_OK) return st;
     return c->dtype != SLICEMOE_BF16 || c->d % 16 != 0 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+}
+
+static slicemoe_status validate(const slicemoe_block_norm_config *c)
+{
+    if (!c || c->T < 0 || c->d < 1 || !storage_ok(c->dtype)) return SLICEMOE_ERR_INVALID_ARG;
+    if (!(c->eps >= 0.f) || isinf(c->eps) || !(fabsf(c->residual_scale) < INFINITY)) return SLICEMOE_ERR_INVALID_ARG;
+    if (c->gate != SLICEMOE_GATE_NONE && c->gate != SLICEMOE_GATE_CHANNEL && c->gate != SLICEMOE_GATE_TOKEN) return SLICEMOE_ERR_INVALID_ARG;
+    return c->d > kNormMaxWidth ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+}
+
+static bool bits_ok(int bits) { return bits == 4 || bits == 8; }
+static slicemoe_status validate(const slicemoe_mx_config *c)
+{
+    if (!c || c->rows < 0 || c->cols < 1 || !bits_ok(c->bits) || !storage_ok(c->dtype)) return SLICEMOE_ERR_INVALID_ARG;
+    if (c->transposed != 0 && c->transposed != 1) return SLICEMOE_ERR_INVALID_ARG;
+    return c->cols > 1 << 20 || (long long)c->rows * c->cols > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+}
+static slicemoe_status validate(const slicemoe_mx_product_config *c)
+{
+    if (!c || c->T < 0 || c->K < 1 || c->N < 1 || !bits_ok(c->bits) || !storage_ok(c->dtype)) return SLICEMOE_ERR_INVALID_ARG;
+    if (c->T > 1 << 24 || c->K > 1 << 20 || c->N > 1 << 20) return SLICEMOE_ERR_UNSUPPORTED;   // (tiles are counted in 31 bits)
+    return (long long)c->T * std::max(c->K, c->N) > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+}
+static slicemoe_status validate_mx(const slicemoe_gated_config *c, int bits)
+{
+    const slicemoe_status st = validate(c);
+    if (st != SLICEMOE_OK) return st;
+    if (!bits_ok(bits)) return SLICEMOE_ERR_INVALID_ARG;
+    return c->dtype != SLICEMOE_BF16 || c->T > 1 << 24 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
 // A workspace of at least `need` bytes on the alignment every workspace has.
 static slicemoe_status check_workspace(const void *ws, size_t bytes, size_t need)
@@ -223,6 +255,117 @@ slicemoe_status slicemoe_clip_grads(const slicemoe_grad *grads, int32_t count, f
     st = check_overlaps(grads, count);
     if (st != SLICEMOE_OK) return st;
     return status_of(launch_clip_grads(grads, count, plan, max_norm, norm, (double *)workspace, (hipStream_t)stream));
+}
+
+slicemoe_status slicemoe_block_norm(const slicemoe_block_norm_config *cfg, const void *x, const void *post_weight, const void *gate,
+                                    const void *residual, const void *pre_weight, void *sum, void *y, void *y_mx, int32_t y_bits,
+                                    float *stats, slicemoe_stream_t stream)
+{
+    const slicemoe_status st = validate(cfg);
+    if (st != SLICEMOE_OK) return st;
+    if ((gate != nullptr) != (cfg->gate != SLICEMOE_GATE_NONE) && cfg->T > 0) return SLICEMOE_ERR_INVALID_ARG;
+    if (cfg->T > 0 && (!x || !residual || !sum)) return SLICEMOE_ERR_INVALID_ARG;
+    if (pre_weight ? cfg->T > 0 && !y && !y_mx : y || y_mx) return SLICEMOE_ERR_INVALID_ARG;
+    if (y_mx && (!bits_ok(y_bits) || misaligned(y_mx, 256))) return SLICEMOE_ERR_INVALID_ARG;
+    for (const void *p : {x, post_weight, gate, residual, pre_weight, (const void *)sum, (const void *)y})
+        if (misaligned(p, 16)) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(stats, 8) || (y && y == sum)) return SLICEMOE_ERR_INVALID_ARG;
+    return status_of(launch_block_norm(*cfg, x, post_weight, gate, residual, pre_weight, sum, y, (uint8_t *)y_mx, y_bits, stats, (hipStream_t)stream));
+}
+
+size_t slicemoe_block_norm_backward_workspace_bytes(const slicemoe_block_norm_config *cfg)
+{
+    if (validate(cfg) != SLICEMOE_OK) return 0;
+    return align_up((size_t)block_norm_backward_blocks(*cfg) * cfg->d * 8, 256);
+}
+
+slicemoe_status slicemoe_block_norm_backward(const slicemoe_block_norm_config *cfg, const void *x, const void *post_weight, const void *gate,
+                                             const void *sum, const void *pre_weight, const float *stats, const void *d_y, const void *d_sum,
+                                             void *d_x, void *d_residual, float *d_post_weight, void *d_gate, float *d_pre_weight,
+                                             void *workspace, size_t workspace_bytes, slicemoe_stream_t stream)
+{
+    slicemoe_status st = validate(cfg);
+    if (st != SLICEMOE_OK) return st;
+    const bool token = cfg->gate == SLICEMOE_GATE_TOKEN, some = cfg->T > 0;
+    if (!pre_weight || !d_pre_weight || (post_weight && !d_post_weight)) return SLICEMOE_ERR_INVALID_ARG;
+    if ((gate != nullptr) != (cfg->gate != SLICEMOE_GATE_NONE) && (some || cfg->gate == SLICEMOE_GATE_CHANNEL)) return SLICEMOE_ERR_INVALID_ARG;
+    if (cfg->gate != SLICEMOE_GATE_NONE && !d_gate && (some || !token)) return SLICEMOE_ERR_INVALID_ARG;
+    if (some && (!x || !sum || !stats || !d_y || !d_x || !d_residual)) return SLICEMOE_ERR_INVALID_ARG;
+    for (const void *p : {x, post_weight, gate, sum, pre_weight, d_y, d_sum, (const void *)d_x, (const void *)d_residual})
+        if (misaligned(p, 16)) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(stats, 8) || misaligned(d_post_weight, 4) || misaligned(d_pre_weight, 4) || misaligned(d_gate, token ? 16 : 4)) return SLICEMOE_ERR_INVALID_ARG;
+    // the outputs of rows are apart from one another and from the inputs that the row's other outputs need
+    if (some) {
+        const void *in[] = {x, sum};
+        for (const void *p : in)
+            if (d_x == p || d_residual == p || (token && d_gate == p)) return SLICEMOE_ERR_INVALID_ARG;
+        if (d_x == d_residual || (token && (d_gate == d_x || d_gate == d_residual || d_gate == d_y || d_gate == d_sum || d_gate == gate || d_x == gate || d_residual == gate)))
+            return SLICEMOE_ERR_INVALID_ARG;
+    }
+    st = check_workspace(workspace, workspace_bytes, slicemoe_block_norm_backward_workspace_bytes(cfg));
+    if (st != SLICEMOE_OK) return st;
+    return status_of(launch_block_norm_backward(*cfg, x, post_weight, gate, sum, pre_weight, stats, d_y, d_sum, d_x, d_residual,
+                                                post_weight ? d_post_weight : nullptr, d_gate, d_pre_weight, (float *)workspace, (hipStream_t)stream));
+}
+
+size_t slicemoe_mx_bytes(const slicemoe_mx_config *cfg)
+{
+    return validate(cfg) == SLICEMOE_OK ? std::max<size_t>(256, mx_total_bytes(cfg->rows, cfg->cols, cfg->bits)) : 0;
+}
+
+slicemoe_status slicemoe_mx_quantize(const slicemoe_mx_config *cfg, const void *x, void *mx, slicemoe_stream_t stream)
+{
+    const slicemoe_status st = validate(cfg);
+    if (st != SLICEMOE_OK) return st;
+    if (cfg->rows > 0 && (!x || !mx)) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(x, 16) || misaligned(mx, 256)) return SLICEMOE_ERR_INVALID_ARG;
+    return status_of(launch_mx_quantize(*cfg, x, (uint8_t *)mx, (hipStream_t)stream));
+}
+
+slicemoe_status slicemoe_mx_dequantize(const slicemoe_mx_config *cfg, const void *mx, void *x, slicemoe_stream_t stream)
+{
+    const slicemoe_status st = validate(cfg);
+    if (st != SLICEMOE_OK) return st;
+    if (cfg->rows > 0 && (!x || !mx)) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(x, 16) || misaligned(mx, 256)) return SLICEMOE_ERR_INVALID_ARG;
+    return status_of(launch_mx_dequantize(*cfg, (const uint8_t *)mx, x, (hipStream_t)stream));
+}
+
+size_t slicemoe_mx_product_workspace_bytes(const slicemoe_mx_product_config *cfg)
+{
+    return validate(cfg) == SLICEMOE_OK ? mx_product_workspace(*cfg) : 0;
+}
+
+slicemoe_status slicemoe_mx_product(const slicemoe_mx_product_config *cfg, const void *x_mx, const void *w_mx, const void *addend, void *y,
+                                    void *workspace, size_t workspace_bytes, slicemoe_stream_t stream)
+{
+    slicemoe_status st = validate(cfg);
+    if (st != SLICEMOE_OK) return st;
+    if (!w_mx || (cfg->T > 0 && (!x_mx || !y))) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(x_mx, 256) || misaligned(w_mx, 256) || misaligned(addend, 16) || misaligned(y, 16)) return SLICEMOE_ERR_INVALID_ARG;
+    const size_t need = mx_product_workspace(*cfg);
+    if (need > 0) st = check_workspace(workspace, workspace_bytes, need);
+    if (st != SLICEMOE_OK) return st;
+    return status_of(launch_mx_product(*cfg, (const uint8_t *)x_mx, (const uint8_t *)w_mx, addend, y, (char *)workspace, (hipStream_t)stream));
+}
+
+size_t slicemoe_gated_ffn_mx_workspace_bytes(const slicemoe_gated_config *cfg, int32_t bits)
+{
+    return validate_mx(cfg, bits) == SLICEMOE_OK ? gated_mx_workspace(*cfg, bits) : 0;
+}
+
+slicemoe_status slicemoe_gated_ffn_mx(const slicemoe_gated_config *cfg, int32_t bits, const void *x_mx, const slicemoe_gated_weights_mx *w,
+                                      const void *addend, void *y, void *workspace, size_t workspace_bytes, slicemoe_stream_t stream)
+{
+    slicemoe_status st = validate_mx(cfg, bits);
+    if (st != SLICEMOE_OK) return st;
+    if (!w || !w->Wg || !w->Wu || !w->Wd || (cfg->T > 0 && (!x_mx || !y))) return SLICEMOE_ERR_INVALID_ARG;
+    for (const void *p : {x_mx, w->Wg, w->Wu, w->Wd})
+        if (misaligned(p, 256)) return SLICEMOE_ERR_INVALID_ARG;
+    if (misaligned(addend, 16) || misaligned(y, 16)) return SLICEMOE_ERR_INVALID_ARG;
+    st = check_workspace(workspace, workspace_bytes, gated_mx_workspace(*cfg, bits));
+    if (st != SLICEMOE_OK) return st;
+    return status_of(launch_gated_mx(*cfg, bits, (const uint8_t *)x_mx, *w, addend, y, (char *)workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

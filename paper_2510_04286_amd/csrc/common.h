@@ -217,6 +217,12 @@ hipError_t launch_ffn_generic(const slicemoe_config &c, const void *h, const flo
 hipError_t launch_ffn_mfma(const slicemoe_config &c, const void *h, const float *p,
                            const int32_t *offsets, const int32_t *perm, const void *packed,
                            void *y, hipStream_t s);
+bool ffn_bias_first(const slicemoe_config &c);   // whether the sums of an expert's output start from its bias (see ffn_mfma.hip)
+// The whole layer for few tokens in one launch (few.hip).  packed: of the matrix-core path, or null.
+constexpr size_t kFewMaxLds = 128 * 1024;   // of a block, beside its static arrays
+size_t few_lds_bytes(const slicemoe_config &c, bool mfma);
+hipError_t launch_forward_few(const slicemoe_config &c, const void *h, const slicemoe_weights &w, bool mfma, void *h_out, int32_t *idx, float *p,
+                              hipStream_t s);
 hipError_t launch_combine(const slicemoe_config &c, const void *y, const int32_t *inv, void *h_out,
                           hipStream_t s);
 hipError_t launch_load_stats(const slicemoe_config &c, const int32_t *counts_raw, const int32_t *counts,

@@ -45,82 +45,17 @@
 #include <type_traits>
 #include <utility>
 
+#include "expert_activation.h"
 #include "mfma.h"
 #include "wavefront.h"
 
 namespace slicemoe {
-
-typedef _Float16 half_t;
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// Packed fp16 constants of the activation stage, passed by value (uniform: they live in SGPRs).
-struct EpiConst {
-    uint32_t neg_w0;
-    uint32_t q[kGeluM + 1];
-    uint32_t half;
-};
-
-static uint32_t pack2_f16(float f)
-{
-    const _Float16 h = (_Float16)f;
-    uint16_t u;
-    __builtin_memcpy(&u, &h, 2);
-    return (uint32_t)u | ((uint32_t)u << 16);
-}
-
-static EpiConst make_epi_const()
-{
-    EpiConst K;
-    K.neg_w0 = pack2_f16(-kGeluW0);
-    for (int i = 0; i <= kGeluM; ++i) K.q[i] = pack2_f16(kGeluQ[i]);
-    K.half = pack2_f16(0.5f);
-    return K;
-}
-
-__device__ __forceinline__ h2 as_h2(uint32_t u) { return __builtin_bit_cast(h2, u); }
-__device__ __forceinline__ h2 pk_fma(h2 a, h2 b, h2 c) { return __builtin_elementwise_fma(a, b, c); }
-// fused multiply-add with the instruction's output clamp to [0, 1]
-__device__ __forceinline__ h2 pk_fma_clamp01(h2 a, h2 b, h2 c)
-{
-    h2 d;
-    asm("v_pk_fma_f16 %0, %1, %2, %3 clamp" : "=v"(d) : "v"(a), "v"(b), "v"(c));
-    return d;
-}
-
-// 16 accumulators of one 32x32 tile -> 8 packed fp16 pairs of kappa * GELU(z); pair i holds the
-// accumulator registers 2i and 2i+1, i.e. contraction slots of GEMM2 in register order.
-__device__ __forceinline__ void activation_tile(const f32x16 &acc, h2 p2, const h2 (&bias)[8], const EpiConst &K, uint4 (&out)[2])
-{
-    uint32_t o[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const h2 A = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(acc[2 * i], acc[2 * i + 1]));
-        const h2 s = pk_fma(A, p2, bias[i]);
-        const h2 v = pk_fma(s, s, as_h2(K.neg_w0));
-        h2 Q = pk_fma(v, as_h2(K.q[kGeluM]), as_h2(K.q[kGeluM - 1]));
-#pragma unroll
-        for (int c = kGeluM - 2; c >= 0; --c) Q = pk_fma(Q, v, as_h2(K.q[c]));
-        const h2 F = pk_fma_clamp01(s, Q, as_h2(K.half));
-        o[i] = __builtin_bit_cast(uint32_t, s * F);
-    }
-    out[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    out[1] = make_uint4(o[4], o[5], o[6], o[7]);
-}
 
 template <int DS, int NSUB> struct RowUnit {
     bf16x8 xb[NSUB][SliceTiles<DS>::KS];
     h2 p2[NSUB];   // (p, p), zero for a lane without a row
     int row[NSUB]; // -1: no row
 };
-
-// The 16 fp16 biases (already scaled by kappa) of hidden tile ht for lane group g, in accumulator order.
-__device__ __forceinline__ void load_bias_tile(const uint4 *__restrict__ b1s, int ht, int g, h2 (&bias)[8])
-{
-    const uint4 b0 = b1s[(ht * 2 + g) * 2 + 0], b1 = b1s[(ht * 2 + g) * 2 + 1];
-    bias[0] = as_h2(b0.x); bias[1] = as_h2(b0.y); bias[2] = as_h2(b0.z); bias[3] = as_h2(b0.w);
-    bias[4] = as_h2(b1.x); bias[5] = as_h2(b1.y); bias[6] = as_h2(b1.z); bias[7] = as_h2(b1.w);
-}
 
 // AHEAD: the weight fragment of the next K-step is requested from LDS before this step's matrix instructions, so
 // that they do not each wait for an LDS round trip (for kernels with few wavefronts per SIMD to cover it).
@@ -178,11 +113,6 @@ __device__ __forceinline__ void gemm2_tile(const uint4 (&hb)[NSUB][2], const uin
                     yacc[sub][ot] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2, __builtin_bit_cast(f16x8, hb[sub][s]), yacc[sub][ot], 0, 0, 0);
             }
     }
-}
-
-__device__ __forceinline__ uint32_t pack_half2(float a, float b)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
 }
 
 // y rows as fp16.  Per output tile a lane holds features 8q + 4g + (0..3) of its own row, i.e. half
@@ -1368,6 +1298,10 @@ static bool streamed_saves_a_round(const slicemoe_config &c)
     return (tall < 0.99 && low > 1.01) || (tall < 1.99 && low > 2.01 && low <= 2.25 && c.He >= 256 && c.E <= 48);
 }
 
+// Whether the sums of a row start from the second-layer bias, in the kernels of every batch size.
+static bool bias_first(const PackedLayout &L) { return plan_ffn(L).resident && L.ds == 64; }
+bool ffn_bias_first(const slicemoe_config &c) { return bias_first(packed_layout(c)); }
+
 hipError_t launch_ffn_mfma(const slicemoe_config &c, const void *h, const float *p,
                            const int32_t *offsets, const int32_t *perm, const void *packed,
                            void *y, hipStream_t s)
@@ -1378,7 +1312,7 @@ hipError_t launch_ffn_mfma(const slicemoe_config &c, const void *h, const float 
     const FfnPlan pl = plan_ffn(L);
     const char *experts = (const char *)packed + L.experts;
     if (ffn_is_small(L.ds, L.E, Na)) {
-        const bool b2_first = pl.resident && L.ds == 64;   // the start of the sums in the kernel that larger batches take
+        const bool b2_first = bias_first(L);   // the start of the sums in the kernel that larger batches take
         if (L.ds == 24) return run_split<24>(c, L, h, p, offsets, perm, experts, b2_first, y, s);
         if (L.ds == 48) return run_split<48>(c, L, h, p, offsets, perm, experts, b2_first, y, s);
         if (L.ds == 64) return run_split<64>(c, L, h, p, offsets, perm, experts, b2_first, y, s);
