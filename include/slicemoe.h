@@ -511,13 +511,14 @@ slicemoe_status slicemoe_mx_dequantize(const slicemoe_mx_config *cfg, const void
  * up.  With 4-bit rows every product counts whole.)
  *   x_mx  T rows of K columns, in cfg->bits;  w_mx  N rows of K columns, in 4 bits
  *   addend [T, N] in, storage dtype, may be NULL (zero);  y [T, N] out, one rounding; may be addend
- *   workspace >= slicemoe_mx_product_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; may be NULL where that is 0
+ *   workspace >= slicemoe_mx_product_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; may be NULL where that is 0; its
+ *             size never falls as T grows
  * A row's result does not depend on the other rows, but the order of its sums depends on T.
  */
 typedef struct {
     int32_t T;     /* rows, 0 <= T <= 2^24                              */
     int32_t K;     /* contracted width, 1 <= K <= 2^20                  */
-    int32_t N;     /* outputs, 1 <= N <= 2^20; T * max(K, N) <= 2^40    */
+    int32_t N;     /* outputs, 1 <= N <= 2^20; T * max(K, N) <= 2^36    */
     int32_t bits;  /* of the rows: 4 or 8                               */
     int32_t dtype; /* slicemoe_dtype of addend and y                    */
 } slicemoe_mx_product_config;
@@ -528,11 +529,11 @@ slicemoe_status slicemoe_mx_product(const slicemoe_mx_product_config *cfg, const
 /*
  * The gated network on microscaled operands: y = addend + (silu(x Wg) * (x Wu)) Wd with x_mx and the hidden rows in `bits` (the hidden
  * rows are taken in fp32, rounded once), the weights in 4 bits.
- *   cfg   dtype must be SLICEMOE_BF16, T <= 2^24 (UNSUPPORTED otherwise)
+ *   cfg   dtype must be SLICEMOE_BF16, T <= 2^24, T * max(d, H) <= 2^36 (UNSUPPORTED otherwise)
  *   x_mx  T rows of d columns, in `bits`
  *   w     Wg, Wu: H rows of d columns; Wd: d rows of H columns, all in 4 bits (from the [in, out] matrices with transposed = 1)
  *   addend [T, d] in, may be NULL;  y [T, d] out, may be addend
- *   workspace >= slicemoe_gated_ffn_mx_workspace_bytes(cfg, bits) (0 on invalid arguments), 256-byte aligned
+ *   workspace >= slicemoe_gated_ffn_mx_workspace_bytes(cfg, bits) (0 on invalid arguments), 256-byte aligned; its size never falls as T grows
  */
 typedef struct {
     const void *Wg, *Wu, *Wd;

@@ -55,18 +55,19 @@ static slicemoe_status validate(const slicemoe_mx_config *c)
     if (c->transposed != 0 && c->transposed != 1) return SLICEMOE_ERR_INVALID_ARG;
     return c->cols > 1 << 20 || (long long)c->rows * c->cols > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
+constexpr long long kMxMost = 1ll << 36;   // (a launch ends below 2^32 threads: 2^24 blocks of 128 x 64 results)
 static slicemoe_status validate(const slicemoe_mx_product_config *c)
 {
     if (!c || c->T < 0 || c->K < 1 || c->N < 1 || !bits_ok(c->bits) || !storage_ok(c->dtype)) return SLICEMOE_ERR_INVALID_ARG;
-    if (c->T > 1 << 24 || c->K > 1 << 20 || c->N > 1 << 20) return SLICEMOE_ERR_UNSUPPORTED;   // (tiles are counted in 31 bits)
-    return (long long)c->T * std::max(c->K, c->N) > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+    if (c->T > 1 << 24 || c->K > 1 << 20 || c->N > 1 << 20) return SLICEMOE_ERR_UNSUPPORTED;
+    return (long long)c->T * std::max(c->K, c->N) > kMxMost ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
 static slicemoe_status validate_mx(const slicemoe_gated_config *c, int bits)
 {
     const slicemoe_status st = validate(c);
     if (st != SLICEMOE_OK) return st;
     if (!bits_ok(bits)) return SLICEMOE_ERR_INVALID_ARG;
-    return c->dtype != SLICEMOE_BF16 || c->T > 1 << 24 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+    return c->dtype != SLICEMOE_BF16 || c->T > 1 << 24 || (long long)c->T * std::max(c->d, c->H) > kMxMost ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
 // A workspace of at least `need` bytes on the alignment every workspace has.
 static slicemoe_status check_workspace(const void *ws, size_t bytes, size_t need)

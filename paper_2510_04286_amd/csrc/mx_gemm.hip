@@ -31,10 +31,10 @@ static MxMatrix mx_matrix(const void *p, int rows, int cols, int bits)
 struct MxArgs {
     MxMatrix x, w, w2;   // w2: the up projection of a pair
     int T, N, Kt;        // rows, features (of one image), tiles of 256 along the contraction
-    int tiles_r, tiles_f;   // blocks along the rows, along the features
+    int tiles_r, tiles_f, splits;   // blocks along the rows, along the features, shares of the contraction
     // product
     const void *addend;
-    void *y;
+    void *y;             // shares: the sums of each, [splits][T][N] float
     // pair: the hidden rows
     uint8_t *h, *hs;
     int hKt;             // their tiles of 256 columns
@@ -110,21 +110,23 @@ template <int BITS_, bool DUAL_, int TR_, int TF_> struct MxTile {
     static constexpr int RT = 2 * TR, FB = 2 * TF;                     // tiles of 32 per block: rows, features (of all images)
     static constexpr int BR = 32 * RT, BF = 32 * FB / IMAGES;          // rows, features of one image per block
     static constexpr int KS = BITS == 4 ? 4 : 2;                       // instructions along a step
-    static constexpr int F_TILE = KS * 1024;                           // bytes of a feature tile in a step; a row tile: 4096
-    static constexpr int R_BYTES = RT * 4096, F_BYTES = FB * F_TILE, S_BYTES = (RT + FB) * 256;
+    static constexpr int F_TILE = KS * 1024, R_TILE = F_TILE * BITS / 4;   // bytes of a tile in a step: features, rows
+    static constexpr int R_KB = R_TILE / 1024;
+    static constexpr int R_BYTES = RT * R_TILE, F_BYTES = FB * F_TILE, S_BYTES = (RT + FB) * 256;
     static constexpr int SLOT = R_BYTES + F_BYTES + S_BYTES;
-    static constexpr int SLOTS = BITS == 4 ? 2 : 3;
+    static constexpr int SLOTS = BITS == 4 || TR + TF == 4 ? 2 : 3;
     static constexpr int LDS = SLOTS * SLOT;
     static constexpr int R_TILES = RT / 4, F_TILES = FB / 4;           // tiles that a wavefront requests
-    static constexpr int LOADS = 4 * R_TILES + KS * F_TILES + 1;       // instructions per wavefront and step
-    static_assert(RT % 4 == 0 && FB % 4 == 0 && (RT + FB == 16 || RT + FB == 8), "scales: a kilobyte per wavefront, or per pair of them");
+    static constexpr int LOADS = R_KB * R_TILES + KS * F_TILES + 1;       // instructions per wavefront and step
+    static_assert(RT % 4 == 0 && FB % 4 == 0 && RT + FB <= 16, "scales: a kilobyte per wavefront at most");
+    static constexpr int PER_CU = 160 * 1024 / LDS, PER_SIMD = PER_CU < 1 ? 1 : PER_CU > 3 ? 3 : PER_CU;   // blocks, wavefronts
     static_assert(LDS <= 160 * 1024, "");
 };
 
-template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::TF][S::TR], const MxArgs &A, int r0, int f0, char *lds)
+template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::TF][S::TR], const MxArgs &A, int r0, int f0, int k0, int k1, char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave >> 1, wf = wave & 1;
-    const int steps = A.Kt * (4 / S::KS);
+    const int steps = (k1 - k0) * (4 / S::KS);   // tiles [k0, k1) of 256 columns
     const uint32_t lds0 = (uint32_t)(uintptr_t)as_lds(lds);
     // tile i of the block's features: image 0's, then image 1's
     const auto feature_tile = [&](int i) {
@@ -135,14 +137,14 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
 #pragma unroll
     for (int i = 0; i < S::R_TILES; ++i) {
         const int t = r0 + wave * S::R_TILES + i;
-        rp[i] = A.x.v + (size_t)(t < A.x.tiles ? t : A.x.tiles - 1) * A.Kt * (1024 * S::BITS);
+        rp[i] = A.x.v + ((size_t)(t < A.x.tiles ? t : A.x.tiles - 1) * A.Kt + k0) * (1024 * S::BITS);
     }
 #pragma unroll
     for (int i = 0; i < S::F_TILES; ++i) {
         const int t = wave * S::F_TILES + i;
-        fp[i] = (S::DUAL && t >= S::FB / 2 ? A.w2.v : A.w.v) + (size_t)feature_tile(t) * A.Kt * 4096;
+        fp[i] = (S::DUAL && t >= S::FB / 2 ? A.w2.v : A.w.v) + ((size_t)feature_tile(t) * A.Kt + k0) * 4096;
     }
-    // Scales: a kilobyte is four tiles; the block's RT row tiles, then its FB feature tiles.  (128 x 128 tiles: two kilobytes, each twice.)
+    // Scales: a kilobyte is four tiles; the block's RT row tiles, then its FB feature tiles.  (Fewer than four kilobytes: some twice.)
     constexpr int S_KB = S::S_BYTES / 1024;
     const int sk = wave % S_KB;
     const uint8_t *sp;
@@ -150,7 +152,7 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
         const int st = 4 * sk + (lane >> 4), t = r0 + st, f = st - S::RT;
         const bool rows = st < S::RT;
         const size_t tile = rows ? (t < A.x.tiles ? t : A.x.tiles - 1) : feature_tile(f);
-        sp = (rows ? A.x.s : S::DUAL && f >= S::FB / 2 ? A.w2.s : A.w.s) + tile * A.Kt * 256 + 16 * (lane & 15);
+        sp = (rows ? A.x.s : S::DUAL && f >= S::FB / 2 ? A.w2.s : A.w.s) + (tile * A.Kt + k0) * 256 + 16 * (lane & 15);
     }
     const uint32_t lane16 = 16 * lane;
     int at = 0, slot = 0;   // of the next request
@@ -161,9 +163,9 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
             constexpr int i = I / S::KS, q = I % S::KS;
             if constexpr (q == 0) set_lds_target(to + S::R_BYTES + (wave * S::F_TILES + i) * S::F_TILE);
             load_lds_1k<1024 * q>((const char *)fp[i], lane16);
-        } else if constexpr (I < S::F_TILES * S::KS + 4 * S::R_TILES) {
-            constexpr int i = (I - S::F_TILES * S::KS) / 4, q = (I - S::F_TILES * S::KS) % 4;
-            if constexpr (q == 0) set_lds_target(to + (wave * S::R_TILES + i) * 4096);
+        } else if constexpr (I < S::F_TILES * S::KS + S::R_KB * S::R_TILES) {
+            constexpr int i = (I - S::F_TILES * S::KS) / S::R_KB, q = (I - S::F_TILES * S::KS) % S::R_KB;
+            if constexpr (q == 0) set_lds_target(to + (wave * S::R_TILES + i) * S::R_TILE);
             load_lds_1k<1024 * q>((const char *)rp[i], lane16);
         } else {
             set_lds_target(to + S::R_BYTES + S::F_BYTES + 1024 * sk);
@@ -174,7 +176,7 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
         ++at;
         slot = slot + 1 == S::SLOTS ? 0 : slot + 1;
 #pragma unroll
-        for (int i = 0; i < S::R_TILES; ++i) rp[i] += 4096;
+        for (int i = 0; i < S::R_TILES; ++i) rp[i] += S::R_TILE;
 #pragma unroll
         for (int i = 0; i < S::F_TILES; ++i) fp[i] += S::F_TILE;
     };
@@ -187,7 +189,7 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
     const auto read = [&](int set, int ks, int i) {   // fragment i of instruction ks: the first features', all rows', the other features'
         const char *image = lds + cur * S::SLOT;
         if (i >= 1 && i <= S::TR) {
-            const char *p = image + (wr * S::TR + i - 1) * 4096 + lane16;
+            const char *p = image + (wr * S::TR + i - 1) * S::R_TILE + lane16;
             if constexpr (S::BITS == 4) rf[set][i - 1] = *(const u32x4 *)(p + 1024 * ks);
             else rf[set][i - 1] = frag8(*(const u32x4 *)(p + 2048 * ks), *(const u32x4 *)(p + 2048 * ks + 1024));
         } else {
@@ -271,17 +273,94 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
     take_scales();
 #pragma unroll
     for (int i = 0; i < NF; ++i) read(0, 0, i);
-    int left = steps - S::SLOTS;
-    for (; left > 0; --left) step(Yes(), Yes(), Yes());
-    if (left == 0) step(Yes(), No(), Yes());
-    if (S::SLOTS == 3 && steps >= 2) step(No(), No(), Yes());
+    int left = steps;
+    for (; left > S::SLOTS; --left) step(Yes(), Yes(), Yes());
+    if (left == S::SLOTS) {
+        step(Yes(), No(), Yes());
+        --left;
+    }
+    for (; left > 1; --left) step(No(), No(), Yes());
     step(No(), No(), No());
 }
 
-template <typename S, typename T> __global__ __launch_bounds__(256, 1) void mx_tile_kernel(MxArgs A)
+// Lanes j and j + 32 trade halves of 16 features: each has eight consecutive ones of its row, 16 q + 8 g of the tile.
+__device__ __forceinline__ void eight_features(const f32x16 &acc, int q, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * q + i]), __float_as_uint(acc[8 * q + 4 + i]), false, false);
+        v[i] = __uint_as_float(sw[0]);
+        v[4 + i] = __uint_as_float(sw[1]);
+    }
+}
+
+// A tile of the product.  Rows of whole pieces of eight features: the addend's pieces of 32 rows are requested together, those of the next
+// 32 in front of the stores of these (one by one they were a trip to memory each: 16384 x 1024 x 2816 took 80 us instead of 70).
+template <typename S, typename T> __device__ __forceinline__ void store_tile(const f32x16 (&acc)[S::TF][S::TR], const MxArgs &A, int rt0, int ft0, int j, int g)
+{
+    typedef RowPiece<T> P;
+    constexpr int W = 8 / P::V;   // 16-byte accesses of eight features
+    const T *addend = (const T *)A.addend;
+    T *y = (T *)A.y;
+    if (A.N % 8 != 0) {
+#pragma unroll
+        for (int u = 0; u < S::TR; ++u)
+#pragma unroll
+            for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int row = 32 * (rt0 + u) + j, f = 32 * (ft0 + t) + 16 * q + 8 * g;
+                    float v[8];
+                    eight_features(acc[t][u], q, v);
+                    if (row < A.T) store_features<T>(addend, y, row, f, A.N, v);
+                }
+        return;
+    }
+    u32x4 a[2][S::FT][2][W];
+    const auto request = [&](int u) {
+        const int row = 32 * (rt0 + u) + j;
+        const T *r = addend + (size_t)(row < A.T ? row : A.T - 1) * A.N;
+#pragma unroll
+        for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int f = 32 * (ft0 + t) + 16 * q + 8 * g;
+#pragma unroll
+                for (int w = 0; w < W; ++w) a[u & 1][t][q][w] = *(const u32x4 *)(r + (f < A.N ? f : 0) + w * P::V);
+            }
+    };
+    const auto tile = [&](auto with) {
+        constexpr bool ADD = decltype(with)::value;
+        if constexpr (ADD) request(0);
+#pragma unroll
+        for (int u = 0; u < S::TR; ++u) {
+            const int row = 32 * (rt0 + u) + j;
+            if constexpr (ADD)
+                if (u + 1 < S::TR) request(u + 1);
+#pragma unroll
+            for (int t = 0; t < S::FT; ++t)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int f = 32 * (ft0 + t) + 16 * q + 8 * g;
+                    float v[8];
+                    eight_features(acc[t][u], q, v);
+                    if constexpr (ADD)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] += P::get(a[u & 1][t][q][i / P::V], i % P::V);
+                    if (row < A.T && f < A.N)
+#pragma unroll
+                        for (int w = 0; w < W; ++w) *(u32x4 *)(y + (size_t)row * A.N + f + w * P::V) = P::make(v + w * P::V);
+                }
+        }
+    };
+    if (addend) tile(std::true_type());
+    else tile(std::false_type());
+}
+
+template <typename S, typename T> __global__ __launch_bounds__(256, S::PER_SIMD) void mx_tile_kernel(MxArgs A)
 {
     extern __shared__ __align__(1024) char lds[];
-    const TilePlace place = tile_of(blockIdx.x, A.tiles_r, A.tiles_f, 1);
+    const TilePlace place = tile_of(blockIdx.x, A.tiles_r, A.tiles_f, A.splits);
     const int r0 = place.r * S::RT, f0 = place.f * (S::FB / S::IMAGES);   // tiles of 32
     f32x16 acc[S::TF][S::TR];
 #pragma unroll
@@ -290,17 +369,16 @@ template <typename S, typename T> __global__ __launch_bounds__(256, 1) void mx_t
         for (int u = 0; u < S::TR; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[t][u][i] = 0.f;
-    mx_steps<S>(acc, A, r0, f0, lds);
+    mx_steps<S>(acc, A, r0, f0, (int)((long long)A.Kt * place.split / A.splits), (int)((long long)A.Kt * (place.split + 1) / A.splits), lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave >> 1, wf = wave & 1, j = lane & 31, g = lane >> 5;
+    const int rt0 = r0 + wr * S::TR, ft0 = f0 + wf * S::FT;
+    if constexpr (S::DUAL) {
 #pragma unroll
-    for (int u = 0; u < S::TR; ++u) {
-        const int rt = r0 + wr * S::TR + u;
-        if (rt >= A.x.tiles) continue;
-        const int row = 32 * rt + j;
+        for (int u = 0; u < S::TR; ++u) {
+            if (rt0 + u >= A.x.tiles) continue;
 #pragma unroll
-        for (int t = 0; t < S::FT; ++t) {
-            const int ft = f0 + wf * S::FT + t;
-            if constexpr (S::DUAL) {
+            for (int t = 0; t < S::FT; ++t) {
+                const int ft = ft0 + t;
                 if (ft >= 8 * A.hKt) continue;
                 float a[16];
 #pragma unroll
@@ -308,43 +386,264 @@ template <typename S, typename T> __global__ __launch_bounds__(256, 1) void mx_t
                     const float v = gated(acc[t][u][i], acc[S::FT + t][u][i]);
                     a[i] = 32 * ft + acc_feature(i, g) < A.N ? v : 0.f;   // (what is past the last row of the weights is anything)
                 }
-                store_hidden<S::BITS>(A, row, ft, g, a);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {   // lanes j and j + 32 trade halves: each has eight consecutive features of its row
-                    float v[8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[t][u][8 * q + i]), __float_as_uint(acc[t][u][8 * q + 4 + i]), false, false);
-                        v[i] = __uint_as_float(sw[0]);
-                        v[4 + i] = __uint_as_float(sw[1]);
-                    }
-                    const int f = 32 * ft + 16 * q + 8 * g;
-                    if (row < A.T) store_features<T>((const T *)A.addend, (T *)A.y, row, f, A.N, v);
-                }
+                store_hidden<S::BITS>(A, 32 * (rt0 + u) + j, ft, g, a);
             }
+        }
+    } else {
+        if (A.splits > 1) A.y = (float *)A.y + (size_t)place.split * A.T * A.N;
+        store_tile<S, T>(acc, A, rt0, ft0, j, g);
+    }
+}
+
+// y = addend + the shares' sums, in their order; four elements a thread.
+template <typename T> __global__ __launch_bounds__(256) void mx_sum_kernel(const float *__restrict__ part, int splits, long long n, const T *addend, T *y)
+{
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= n) return;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (at + 4 <= n && n % 4 == 0) {
+        for (int s = 0; s < splits; ++s) {
+            const f32x4 p = *(const f32x4 *)(part + s * n + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += p[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += addend ? Storage<T>::load(addend + at + i) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Storage<T>::store(y + at + i, v[i]);
+        return;
+    }
+    for (int i = 0; i < 4 && at + i < n; ++i) {
+        float t = 0.f;
+        for (int s = 0; s < splits; ++s) t += part[s * n + at + i];
+        Storage<T>::store(y + at + i, t + (addend ? Storage<T>::load(addend + at + i) : 0.f));
+    }
+}
+
+// shares: [splits][T][N] float of workspace (splits > 1)
+template <typename S, typename T> static hipError_t run_tiles(MxArgs A, int f_tiles, int splits, float *shares, hipStream_t s)
+{
+    A.tiles_r = (A.x.tiles + S::RT - 1) / S::RT;
+    A.tiles_f = (f_tiles + S::FB / S::IMAGES - 1) / (S::FB / S::IMAGES);
+    A.splits = splits;
+    const void *addend = A.addend;
+    void *y = A.y;
+    const auto launch = [&](auto kern) {
+        const hipError_t e = grant_dynamic_lds((const void *)kern, S::LDS);
+        if (e != hipSuccess) return e;
+        kern<<<(unsigned)(A.tiles_r * A.tiles_f * splits), 256, S::LDS, s>>>(A);
+        return hipGetLastError();
+    };
+    if (splits == 1) return launch(mx_tile_kernel<S, T>);
+    if constexpr (!S::DUAL) {
+        A.addend = nullptr;
+        A.y = shares;
+        const hipError_t e = launch(mx_tile_kernel<S, float>);
+        if (e != hipSuccess) return e;
+        const long long n = (long long)A.T * A.N;
+        mx_sum_kernel<T><<<(unsigned)((n + 1023) / 1024), 256, 0, s>>>(shares, splits, n, (const T *)addend, (T *)y);
+    }
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------ few rows
+// Up to 32 TR rows: bound by the weights, which cross memory once.  A block has 32 features (of one or two images), its KW wavefronts the
+// tiles of 256 columns in turn, whose fragments go straight from memory to registers (nobody else in the block needs them).  Their sums
+// meet in the LDS, added in the wavefronts' order; behind it a row's 32 features are in 16 neighbouring lanes.
+template <int BITS, bool DUAL, int TR> struct MxFewStep {
+    static constexpr int IMAGES = DUAL ? 2 : 1, RP = BITS == 4 ? 4 : 8;
+    u32x4 f[IMAGES][4], r[TR][RP];
+    int fs[IMAGES], rs[TR];
+    __device__ __forceinline__ void load(const MxArgs &A, int ft, int kt, int lane)
+    {
+#pragma unroll
+        for (int m = 0; m < IMAGES; ++m) {
+            const MxMatrix &w = m ? A.w2 : A.w;
+            const size_t t = (size_t)ft * A.Kt + kt;
+            const u32x4 *p = (const u32x4 *)(w.v + t * 4096) + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[m][i] = __builtin_nontemporal_load(p + 64 * i);
+            fs[m] = *((const int *)(w.s + t * 256) + lane);
+        }
+#pragma unroll
+        for (int u = 0; u < TR; ++u) {
+            const size_t t = (size_t)(u < A.x.tiles ? u : 0) * A.Kt + kt;
+            const u32x4 *p = (const u32x4 *)(A.x.v + t * (1024 * BITS)) + lane;
+            const bool there = 32 * u + (lane & 31) < A.T;   // (the others are not fetched)
+#pragma unroll
+            for (int i = 0; i < RP; ++i) r[u][i] = u32x4{0, 0, 0, 0};
+            rs[u] = 0;
+            if (there) {
+#pragma unroll
+                for (int i = 0; i < RP; ++i) r[u][i] = p[64 * i];
+                rs[u] = *((const int *)(A.x.s + t * 256) + lane);
+            }
+        }
+    }
+    __device__ __forceinline__ void multiply(f32x16 (&acc)[IMAGES][TR]) const
+    {
+        for_range<0, 4>([&](auto k) {
+            constexpr int K = decltype(k)::value;
+#pragma unroll
+            for (int u = 0; u < TR; ++u) {
+                i32x8 b;
+                if constexpr (BITS == 4) b = frag4(r[u][K]);
+                else b = frag8(r[u][2 * K], r[u][2 * K + 1]);
+#pragma unroll
+                for (int m = 0; m < IMAGES; ++m) acc[m][u] = mx_mfma<BITS, K>(frag4(f[m][K]), b, acc[m][u], fs[m], rs[u]);
+            }
+        });
+    }
+};
+
+template <int BITS, bool DUAL, int TR, int KW, typename T> __global__ __launch_bounds__(64 * KW, TR == 1 ? 4 : 2) void mx_few_kernel(MxArgs A)
+{
+    typedef MxFewStep<BITS, DUAL, TR> Step;
+    constexpr int IMAGES = Step::IMAGES;
+    extern __shared__ __align__(16) float sums[];   // [KW][IMAGES][64 lanes][16], pieces of four swizzled over the 64 banks
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ft = blockIdx.x;
+    f32x16 acc[IMAGES][TR];
+#pragma unroll
+    for (int m = 0; m < IMAGES; ++m)
+#pragma unroll
+        for (int u = 0; u < TR; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[m][u][i] = 0.f;
+    if (ft < A.w.tiles)
+#pragma unroll 1
+        for (int kt = wave; kt < A.Kt; kt += KW) {
+            Step a;
+            a.load(A, ft, kt, lane);
+            a.multiply(acc);
+        }
+    // thread -> row, and positions p, p + 1 of its block: p = 16 g + 4 q + c is feature 8 q + 4 g + c
+    const int row = tid >> 4 & 31, p = 2 * (tid & 15), g = p >> 4, from = row + 32 * g;
+    const int at = from * 16 + 4 * ((p >> 2 & 3) ^ (from >> 2 & 3)) + (p & 3), f = 32 * ft + 8 * (p >> 2 & 3) + 4 * g + (p & 3);
+#pragma unroll
+    for (int u = 0; u < TR; ++u) {
+        if (u > 0) __syncthreads();
+#pragma unroll
+        for (int m = 0; m < IMAGES; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(f32x4 *)(sums + ((wave * IMAGES + m) * 64 + lane) * 16 + 4 * (q ^ (lane >> 2 & 3))) =
+                    f32x4{acc[m][u][4 * q], acc[m][u][4 * q + 1], acc[m][u][4 * q + 2], acc[m][u][4 * q + 3]};
+        __syncthreads();
+        const int R = 32 * u + row;
+        if (tid >= 512 || R >= A.T) continue;   // (a row's lanes together)
+        float v[IMAGES][2];
+#pragma unroll
+        for (int m = 0; m < IMAGES; ++m) {
+            v[m][0] = v[m][1] = 0.f;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) {
+                const float2 t = *(const float2 *)(sums + (w * IMAGES + m) * 1024 + at);
+                v[m][0] += t.x;
+                v[m][1] += t.y;
+            }
+        }
+        if constexpr (DUAL) {
+            float a[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float h = gated(v[0][i], v[IMAGES - 1][i]);
+                a[i] = f + i < A.N ? h : 0.f;   // (what is past the last row of the weights is anything)
+            }
+            uint32_t most = __float_as_uint(a[0]) & 0x7fffffffu, other = __float_as_uint(a[1]) & 0x7fffffffu;
+            most = other > most ? other : most;
+            const auto larger = [&](int o) { most = (uint32_t)o > most ? (uint32_t)o : most; };
+            larger(lane_move<0xB1>((int)most));
+            larger(lane_move<0x4E>((int)most));
+            larger(lane_move<0x141>((int)most));
+            larger(lane_move<0x140>((int)most));
+            const uint32_t byte = mx_scale_byte<BITS>(most);
+            const float inv = mx_inverse(byte);
+            const uint32_t q = mx_pack4<BITS>(a[0] * inv, a[1] * inv, 0.f, 0.f);
+            uint8_t *o = A.h + mx_quad_offset<BITS>(R, ft, 2 * (p >> 2 & 3) + g, A.hKt) + (p & 3) * BITS / 8;
+            if constexpr (BITS == 4) *o = (uint8_t)q;
+            else *(uint16_t *)o = (uint16_t)q;
+            if (p == 0) A.hs[mx_scale_offset(R, ft, A.hKt)] = (uint8_t)byte;
+        } else {
+            const size_t y = (size_t)R * A.N + f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (f + i < A.N) Storage<T>::store((T *)A.y + y + i, v[0][i] + (A.addend ? Storage<T>::load((const T *)A.addend + y + i) : 0.f));
         }
     }
 }
 
-template <typename S, typename T> static hipError_t run_tiles(MxArgs A, int f_tiles, hipStream_t s)
+template <int BITS, bool DUAL, int TR, int KW, typename T> static hipError_t run_few(const MxArgs &A, int f_tiles, hipStream_t s)
 {
-    A.tiles_r = (A.x.tiles + S::RT - 1) / S::RT;
-    A.tiles_f = (f_tiles + S::FB / S::IMAGES - 1) / (S::FB / S::IMAGES);
-    const auto kern = mx_tile_kernel<S, T>;
-    const hipError_t e = grant_dynamic_lds((const void *)kern, S::LDS);
+    const auto kern = mx_few_kernel<BITS, DUAL, TR, KW, T>;
+    constexpr size_t lds = (size_t)KW * (DUAL ? 2 : 1) * 4096;
+    const hipError_t e = grant_dynamic_lds((const void *)kern, lds);
     if (e != hipSuccess) return e;
-    kern<<<(unsigned)(A.tiles_r * A.tiles_f), 256, S::LDS, s>>>(A);
+    kern<<<(unsigned)f_tiles, 64 * KW, lds, s>>>(A);
     return hipGetLastError();
 }
 
-template <int BITS, bool DUAL, typename T> static hipError_t run_product(const MxArgs &A, hipStream_t s)
+// Which kernel a product takes: few rows, tiles of 128 x 128 (several blocks a CU), or of 256 x 256 (one).
+constexpr int kFewRows = 64;
+constexpr int kMostSplits = 8, kSplitBlocks = 512;   // shares of the contraction at most, and blocks of all shares together
+struct MxChoice {
+    bool large;
+    int splits;
+};
+// us of a step of 256 columns, fitted to products of 64 to 16384 rows at K 1024 to 11008 (T, K, N: 128 tiles / 256 tiles, us):
+//   4 bits   16384 1024 2816: 53.9 / 56.8   2048 11008 4096: 47.9 / 56.6   4096 11008 4096: 92.4 / 84.3   1024 2816 1024: 9.0 / 21.8
+//   8 bits   16384 2816 1024: 50.6 / 42.6   2048 11008 4096: 72.0 / 94.3   4096 11008 4096: 153 / 124     1024 2816 1024: 12.6 / 31.4
+// and in shares, 128 tiles, 1 / 2 / 4 / 8 of them: 4 bits 128 11008 4096 27.4 / 20.6 / 17.0 / 17.8, 512 11008 4096 32.1 / 27.8 / 28.2 / 37.3; 8 bits
+// 128 11008 4096 51.1 / 31.3 / 22.2 / 19.8, 1024 11008 4096 55.5 / 52.6 / 60.3 / 77.0.
+struct MxCosts {
+    double one, each, start;   // 128 tiles: a block alone on its CU, every further one, beginning and end of a block
+    int per_cu;
+    double large, large_start;
+};
+static constexpr MxCosts kMxCosts4 = {0.77, 0.32, 2.7, 2, 1.96, 9.0}, kMxCosts8 = {1.25, 0.5, 3.0, 3, 2.85, 9.0};
+static MxChoice choose(long long T, int f_tiles, int Kt, int N, int bits, bool dual)
 {
-    const int f_tiles = DUAL ? 8 * A.hKt : A.w.tiles;
-    return run_tiles<MxTile<BITS, DUAL, 4, 4>, T>(A, f_tiles, s);
+    const MxCosts &c = bits == 4 ? kMxCosts4 : kMxCosts8;
+    const long long cus = num_compute_units(), per = dual ? 2 : 4;
+    const auto blocks = [&](int rows, int tiles) { return ((T + rows - 1) / rows) * ((f_tiles + tiles - 1) / tiles); };
+    const long long small = blocks(128, per), large = blocks(256, 2 * per);
+    MxChoice best = {true, 1};
+    const long long left = large % cus;   // a partial round's steps are shorter: 1.3 of 2 with half of the chip
+    double least = Kt * c.large * (large / cus + (left ? 0.6 + 0.4 * left / cus : 0)) + c.large_start * ((large + cus - 1) / cus);
+    for (int s = 1; s <= kMostSplits && s <= Kt; s *= 2) {
+        const long long n = small * s, round = cus * c.per_cu, rest = n % round;
+        if (s > 1 && (dual || n > kSplitBlocks)) break;
+        const auto depth = [&](long long b) { return b == 0 ? 0 : c.one + c.each * ((double)b / cus > 1 ? (double)b / cus - 1 : 0); };
+        double t = (double)Kt / s * (n / round * depth(round) + depth(rest)) + c.start * ((n + round - 1) / round);
+        if (s > 1) t += 3 + (double)s * T * N * 8 / 5e6;   // the shares' addition: a launch, and their sums through the caches
+        if (t < least) {
+            least = t;
+            best = {false, s};
+        }
+    }
+    return best;
+}
+// Bytes of the shares' sums, for this and every smaller batch: as many of them as the rule above can choose.
+static size_t shares_bytes(long long T, int N, int Kt)
+{
+    if (T <= kFewRows || Kt < 2) return 0;
+    const long long tiles_f = (N + 127) / 128, rows = kSplitBlocks / tiles_f * 128;
+    return (size_t)(kMostSplits * T < rows ? kMostSplits * T : rows) * N * 4;
 }
 
-size_t mx_product_workspace(const slicemoe_mx_product_config &c) { return 0; }
+template <int BITS, bool DUAL, typename T> static hipError_t run_product(const MxArgs &A, float *shares, hipStream_t s)
+{
+    const int f_tiles = DUAL ? 8 * A.hKt : A.w.tiles;
+    if (A.T <= kFewRows) {
+        if (A.T > 32) return run_few<BITS, DUAL, 2, 8, T>(A, f_tiles, s);
+        return f_tiles <= 160 ? run_few<BITS, DUAL, 1, 16, T>(A, f_tiles, s) : run_few<BITS, DUAL, 1, 8, T>(A, f_tiles, s);
+    }
+    const MxChoice c = choose(A.T, f_tiles, A.Kt, A.N, BITS, DUAL);
+    if (c.large) return run_tiles<MxTile<BITS, DUAL, 4, 4>, T>(A, f_tiles, 1, nullptr, s);
+    return run_tiles<MxTile<BITS, DUAL, 2, 2>, T>(A, f_tiles, c.splits, shares, s);
+}
+
+size_t mx_product_workspace(const slicemoe_mx_product_config &c) { return align_up(shares_bytes(c.T, c.N, mx_tiles_k(c.K)), 256); }
 
 hipError_t launch_mx_product(const slicemoe_mx_product_config &c, const uint8_t *x, const uint8_t *w, const void *addend, void *y, char *ws, hipStream_t s)
 {
@@ -357,14 +656,15 @@ hipError_t launch_mx_product(const slicemoe_mx_product_config &c, const uint8_t 
     A.Kt = mx_tiles_k(c.K);
     A.addend = addend;
     A.y = y;
-    if (c.bits == 4) return c.dtype == SLICEMOE_BF16 ? run_product<4, false, bf16_t>(A, s) : run_product<4, false, float>(A, s);
-    return c.dtype == SLICEMOE_BF16 ? run_product<8, false, bf16_t>(A, s) : run_product<8, false, float>(A, s);
+    float *f = (float *)ws;
+    if (c.bits == 4) return c.dtype == SLICEMOE_BF16 ? run_product<4, false, bf16_t>(A, f, s) : run_product<4, false, float>(A, f, s);
+    return c.dtype == SLICEMOE_BF16 ? run_product<8, false, bf16_t>(A, f, s) : run_product<8, false, float>(A, f, s);
 }
 
-size_t gated_mx_workspace(const slicemoe_gated_config &c, int bits)
-{
-    return align_up(mx_total_bytes(c.T, c.H, bits), 256) + 256;   // (never 0)
-}
+// The hidden rows, and behind them the second product's workspace.
+static size_t hidden_bytes(const slicemoe_gated_config &c, int bits) { return align_up(mx_total_bytes(c.T, c.H, bits), 256) + 256; }   // (never 0)
+static slicemoe_mx_product_config second_product(const slicemoe_gated_config &c, int bits) { return {c.T, c.H, c.d, bits, SLICEMOE_BF16}; }
+size_t gated_mx_workspace(const slicemoe_gated_config &c, int bits) { return hidden_bytes(c, bits) + mx_product_workspace(second_product(c, bits)); }
 
 hipError_t launch_gated_mx(const slicemoe_gated_config &c, int bits, const uint8_t *x, const slicemoe_gated_weights_mx &w, const void *addend, void *y,
                            char *ws, hipStream_t s)
@@ -380,10 +680,9 @@ hipError_t launch_gated_mx(const slicemoe_gated_config &c, int bits, const uint8
     A.h = (uint8_t *)ws;
     A.hs = A.h + mx_tiles(c.T, c.H) * mx_tile_bytes(bits);
     A.hKt = mx_tiles_k(c.H);
-    const hipError_t e = bits == 4 ? run_product<4, true, bf16_t>(A, s) : run_product<8, true, bf16_t>(A, s);
+    const hipError_t e = bits == 4 ? run_product<4, true, bf16_t>(A, nullptr, s) : run_product<8, true, bf16_t>(A, nullptr, s);
     if (e != hipSuccess) return e;
-    const slicemoe_mx_product_config p = {c.T, c.H, c.d, bits, SLICEMOE_BF16};
-    return launch_mx_product(p, A.h, (const uint8_t *)w.Wd, addend, y, ws, s);
+    return launch_mx_product(second_product(c, bits), A.h, (const uint8_t *)w.Wd, addend, y, ws + hidden_bytes(c, bits), s);
 }
 
 }  // namespace slicemoe

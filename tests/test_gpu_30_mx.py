@@ -109,7 +109,7 @@ def test_ends_of_the_range(B, bits):
 
 
 SHAPES = [(1, 1, 1), (1, 33, 7), (2, 256, 64), (16, 300, 129), (31, 1000, 96), (33, 257, 100), (64, 512, 256), (65, 513, 255), (100, 2000, 333), (128, 64, 40),
-          (200, 768, 1000), (257, 511, 257), (300, 1025, 513), (513, 1300, 130)]
+          (200, 768, 1000), (257, 511, 257), (300, 1025, 513), (513, 1300, 130), (130, 5000, 264), (257, 2816, 500), (1025, 4096, 130), (4100, 2048, 2050)]
 
 
 @pytest.mark.parametrize("bits", [4, 8])

@@ -109,15 +109,19 @@ def test_mx_refusals_and_sizes(B):
     pc, size = B.make_mx_product_config, B.slicemoe_mx_product_workspace_bytes
     f = L.slicemoe_mx_product
     for c, want in [(pc(-1, 64, 64), inv), (pc(4, 0, 64), inv), (pc(4, 64, 0), inv), (pc(4, 64, 64, 3), inv), (B.slicemoe_mx_product_config(4, 64, 64, 4, 2), inv),
-                    (pc((1 << 24) + 1, 64, 64), uns), (pc(4, (1 << 20) + 1, 64), uns), (pc(4, 64, (1 << 20) + 1), uns), (pc(1 << 24, 1 << 17, 64), uns)]:
+                    (pc((1 << 24) + 1, 64, 64), uns), (pc(4, (1 << 20) + 1, 64), uns), (pc(4, 64, (1 << 20) + 1), uns), (pc(1 << 24, 1 << 13, 64), uns), (pc(1 << 24, 64, (1 << 12) + 1), uns)]:
         assert f(by(c), P, P, P, Q, P, BIG, NULL) == want and size(c) == 0
+    for bits in (4, 8):     # a workspace of the largest batch serves the smaller ones
+        for K, N in ((64, 64), (11008, 4096), (4096, 11008), (512, 100), (3000, 70000)):
+            sizes = [size(pc(T, K, N, bits)) for T in (0, 1, 64, 65, 128, 200, 512, 1000, 4096, 100000)]
+            assert sizes == sorted(sizes)
     ok = pc(4, 64, 64)
     for args in [(NULL, P, P, Q), (P, NULL, P, Q), (P, P, P, NULL), (ODD, P, P, Q), (P, ODD, P, Q), (P, P, ODD, Q), (P, P, P, ODD)]:
         assert f(by(ok), *args, P, BIG, NULL) == inv, args
     gc, w = B.make_gated_config(4, 64, 32), B.slicemoe_gated_weights_mx(4096, 4096, 4096)
     h, gs = L.slicemoe_gated_ffn_mx, B.slicemoe_gated_ffn_mx_workspace_bytes
     for c, bits, want in [(B.make_gated_config(-1, 64, 32), 4, inv), (B.make_gated_config(4, 0, 32), 4, inv), (gc, 2, inv), (gc, 16, inv),
-                          (B.make_gated_config(4, 64, 32, "f32"), 4, uns), (B.make_gated_config((1 << 24) + 1, 64, 32), 8, uns)]:
+                          (B.make_gated_config(4, 64, 32, "f32"), 4, uns), (B.make_gated_config((1 << 24) + 1, 64, 32), 8, uns), (B.make_gated_config(1 << 24, 64, 4097), 8, uns)]:
         assert h(by(c), bits, P, by(w), P, Q, P, BIG, NULL) == want and gs(c, bits) == 0
     for args in [(NULL, by(w), P, Q), (P, NULL, P, Q), (P, by(B.slicemoe_gated_weights_mx(4096, 0, 4096)), P, Q), (P, by(w), P, NULL), (ODD, by(w), P, Q),
                  (P, by(B.slicemoe_gated_weights_mx(4096, 4112, 4096)), P, Q), (P, by(w), ODD, Q), (P, by(w), P, ODD)]:
