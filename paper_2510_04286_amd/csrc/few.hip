@@ -14,7 +14,8 @@
 
 namespace slicemoe {
 
-constexpr int kFewWaves = 8, kFewThreads = kFewWaves * 64, kFewGroup = 8;   // kFewGroup: hidden tiles whose second-layer fragments a wavefront holds
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * 64;
+constexpr int kFewGroup = 4;   // hidden tiles whose second-layer fragments a wavefront holds, twice: these and the next ones
 
 struct FewArgs {
     const bf16_t *x;
@@ -28,18 +29,23 @@ struct FewArgs {
     float *p;
 };
 
-// LDS: terms of the router's hidden layer, activations [k][HT][2][2] pieces, outputs [k][DS] fp16, selection.
+// LDS: terms of the router's hidden layer, its second layer, activations [k][HT][2][2] pieces, outputs [k][ds] fp16.
 constexpr int kFewTerms = 8 * 2 * 2 * 2 * 16;
-__host__ __device__ constexpr size_t few_lds(int k, int HT, int ds) { return kFewTerms + (size_t)k * HT * 64 + (size_t)k * ds * 2 + 64; }
+__host__ __device__ constexpr size_t few_router2(int E) { return (size_t)((E + 31) / 32) * 8 * 2 * 64 * 16; }
+__host__ __device__ constexpr size_t few_lds(int E, int k, int HT, int ds) { return kFewTerms + few_router2(E) + (size_t)k * HT * 64 + (size_t)k * ds * 2 + 64; }
 
+// (Two blocks a CU where the registers allow it: 512 slices of width 64 are one round then.)
 template <int DS, int ET>
-__global__ __launch_bounds__(kFewThreads) void few_mfma_kernel(FewArgs A)
+__global__ __launch_bounds__(kFewThreads, DS <= 64 ? 4 : 2) void few_mfma_kernel(FewArgs A)
 {
     constexpr int KS = SliceTiles<DS>::KS, OT = SliceTiles<DS>::OT, HTr = 8;
+    constexpr bool AHEAD = KS <= 8;   // the next hidden tile's fragments are requested before this one's are used
     extern __shared__ __align__(16) char lds[];
     uint4 *us = (uint4 *)lds;                                    // [HTr][2 K-steps][2 terms][2 lane groups]
-    uint4 *hs = (uint4 *)(lds + kFewTerms);                      // [k][HT][2][2]
-    half_t *ys = (half_t *)(lds + kFewTerms + (size_t)A.k * A.HT * 64);   // [k][DS]
+    uint4 *w2s = (uint4 *)(lds + kFewTerms);                     // [ET][HTr][2][64]
+    char *rest = lds + kFewTerms + ET * HTr * 2 * 64 * 16;
+    uint4 *hs = (uint4 *)rest;                                   // [k][HT][2][2]
+    half_t *ys = (half_t *)(rest + (size_t)A.k * A.HT * 64);     // [k][DS]
     __shared__ int sel_idx[8];
     __shared__ float sel_p[8];
     const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -52,21 +58,24 @@ __global__ __launch_bounds__(kFewThreads) void few_mfma_kernel(FewArgs A)
     for (int ks = 0; ks < KS; ++ks) xb[ks] = load_row_piece<DS>(xr, ks, g);
     {
         const uint4 *w1 = (const uint4 *)(A.packed + A.L.r_w1) + wave * KS * 64 + lane;
-        uint4 w1r[KS];
+        uint4 w1r[KS], w2r[ET][2];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) w1r[ks] = w1[ks * 64];
         const uint4 *w2 = (const uint4 *)(A.packed + A.L.r_w2) + lane;   // [ET][HTr][2][64]
-        uint4 w2r[ET * HTr * 2];
-        f32x16 gacc[ET];
-        if (wave == 0) {
 #pragma unroll
-            for (int i = 0; i < ET * HTr * 2; ++i) w2r[i] = w2[i * 64];
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) w2r[et][s] = w2[((et * HTr + wave) * 2 + s) * 64];
+        f32x16 acc = load_bias_tile((const float *)(A.packed + A.L.r_b1), wave, g), gacc[ET];
+        if (wave == 0)
 #pragma unroll
             for (int et = 0; et < ET; ++et) gacc[et] = load_bias_tile((const float *)(A.packed + A.L.r_b2), et, g);
-        }
-        f32x16 acc = load_bias_tile((const float *)(A.packed + A.L.r_b1), wave, g);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) acc = mfma_bf16(__builtin_bit_cast(bf16x8, w1r[ks]), xb[ks], acc);
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) w2s[((et * HTr + wave) * 2 + s) * 64 + lane] = w2r[et][s];
         uint32_t t0[8], t1[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) relu_split_pair(acc[2 * i], acc[2 * i + 1], t0[i], t1[i]);
@@ -86,7 +95,7 @@ __global__ __launch_bounds__(kFewThreads) void few_mfma_kernel(FewArgs A)
                     const f16x8 u1 = __builtin_bit_cast(f16x8, us[((h * 2 + s) * 2 + 1) * 2 + g]);
 #pragma unroll
                     for (int et = 0; et < ET; ++et) {   // small term first
-                        const f16x8 a2 = __builtin_bit_cast(f16x8, w2r[(et * HTr + h) * 2 + s]);
+                        const f16x8 a2 = __builtin_bit_cast(f16x8, w2s[((et * HTr + h) * 2 + s) * 64 + lane]);
                         gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2, u1, gacc[et], 0, 0, 0);
                         gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2, u0, gacc[et], 0, 0, 0);
                     }
@@ -98,62 +107,91 @@ __global__ __launch_bounds__(kFewThreads) void few_mfma_kernel(FewArgs A)
                 for (int r = 0; r < 16; ++r) v[et * 16 + r] = gacc[et][r];
             select_experts<ET, kRouteInference>(v, 0, j == 0, g, A.L.E, k, nullptr, 0.f, 1.4426950408889634f, nullptr, 0.f, sel_idx, sel_p, false, nullptr);
         }
-        __syncthreads();
+        lds_barrier();
     }
     if (tid < k) {   // (the selection is in range whatever the logits are: see select_experts)
         if (A.idx) A.idx[n * k + tid] = sel_idx[tid];
         if (A.p) A.p[n * k + tid] = sel_p[tid];
     }
+    const auto expert = [&](int jj) { return A.packed + A.L.experts + (size_t)__builtin_amdgcn_readfirstlane(sel_idx[jj]) * A.L.e_stride; };
 
+    // Second layer: the k OT output tiles, each the sum over all hidden tiles in their order, kFewGroup of them at a time.
+    const int jobs2 = k * OT;
+    uint4 w2[2][kFewGroup][2];
+    const auto load_w2 = [&](int set, int job, int ht0) {   // [HT][2][OT][64]
+        const uint4 *p = (const uint4 *)(expert(job / OT) + A.L.e_w2) + (size_t)(job % OT) * 64 + lane;
+#pragma unroll
+        for (int i = 0; i < kFewGroup; ++i)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) w2[set][i][s] = p[(size_t)(min(ht0 + i, HT - 1) * 2 + s) * OT * 64];
+    };
     // First layer: the k HT hidden tiles in turn over the wavefronts.
-    for (int job = wave; job < k * HT; job += kFewWaves) {
-        const int jj = job / HT, ht = job - jj * HT;
-        const int e = __builtin_amdgcn_readfirstlane(sel_idx[jj]);
-        const char *ew = A.packed + A.L.experts + (size_t)e * A.L.e_stride;
-        const uint4 *w1 = (const uint4 *)(ew + A.L.e_w1) + (size_t)ht * KS * 64 + lane;
-        uint4 w[KS];
+    {
+        const int jobs = k * HT;
+        uint4 w1[AHEAD ? 2 : 1][KS];
+        const auto load_w1 = [&](int set, int job) {
+            const uint4 *p = (const uint4 *)(expert(job / HT) + A.L.e_w1) + (size_t)(job % HT) * KS * 64 + lane;
 #pragma unroll
-        for (int i = 0; i < KS; ++i) w[i] = w1[i * 64];
-        h2 bias[8];
-        load_bias_tile((const uint4 *)(ew + A.L.e_b1), ht, g, bias);
-        const float pv = sel_p[jj];
-        const h2 p2 = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(pv, pv));
-        f32x16 acc;
+            for (int i = 0; i < KS; ++i) w1[set][i] = p[i * 64];
+        };
+        const auto tile = [&](int set, int job) {
+            const int jj = job / HT, ht = job - jj * HT;
+            h2 bias[8];
+            load_bias_tile((const uint4 *)(expert(jj) + A.L.e_b1), ht, g, bias);
+            const float pv = sel_p[jj];
+            const h2 p2 = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(pv, pv));
+            f32x16 acc;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+            for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) acc = mfma_bf16(__builtin_bit_cast(bf16x8, w[ks]), xb[ks], acc);
-        uint4 hb[2];
-        activation_tile(acc, p2, bias, A.K, hb);
-        if (j == 0)
+            for (int ks = 0; ks < KS; ++ks) acc = mfma_bf16(__builtin_bit_cast(bf16x8, w1[set][ks]), xb[ks], acc);
+            uint4 hb[2];
+            activation_tile(acc, p2, bias, A.K, hb);
+            if (j == 0)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) hs[(job * 2 + s) * 2 + g] = hb[s];
+                for (int s = 0; s < 2; ++s) hs[(job * 2 + s) * 2 + g] = hb[s];
+        };
+        load_w1(0, min(wave, jobs - 1));
+        if (wave < jobs2) load_w2(0, wave, 0);
+#pragma unroll 1
+        for (int job = wave; job < jobs; job += AHEAD ? 2 * kFewWaves : kFewWaves) {
+            if constexpr (AHEAD) {   // (past the end: the last one again)
+                load_w1(1, min(job + kFewWaves, jobs - 1));
+                tile(0, job);
+                load_w1(0, min(job + 2 * kFewWaves, jobs - 1));
+                if (job + kFewWaves < jobs) tile(1, job + kFewWaves);
+            } else {
+                tile(0, job);
+                load_w1(0, min(job + kFewWaves, jobs - 1));
+            }
+        }
     }
+    if (wave < jobs2 && HT > kFewGroup) load_w2(1, wave, kFewGroup);
     lds_barrier();
-    // Second layer: the k OT output tiles, each the sum over all hidden tiles in their order.
-    for (int job = wave; job < k * OT; job += kFewWaves) {
+    for (int job = wave; job < jobs2; job += kFewWaves) {
         const int jj = job / OT, ot = job - jj * OT;
-        const int e = __builtin_amdgcn_readfirstlane(sel_idx[jj]);
-        const char *ew = A.packed + A.L.experts + (size_t)e * A.L.e_stride;
-        const uint4 *w2 = (const uint4 *)(ew + A.L.e_w2) + (size_t)ot * 64 + lane;   // [HT][2][OT][64]
-        const f32x16 bias = load_bias_tile((const float *)(ew + A.L.e_b2), ot, g);   // padded with zeros by the packer
+        const f32x16 bias = load_bias_tile((const float *)(expert(jj) + A.L.e_b2), ot, g);   // padded with zeros by the packer
         f32x16 acc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] = A.b2_first ? bias[r] : 0.f;
-        for (int ht0 = 0; ht0 < HT; ht0 += kFewGroup) {
-            uint4 w[kFewGroup][2];
-#pragma unroll
-            for (int i = 0; i < kFewGroup; ++i)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) w[i][s] = w2[(size_t)(min(ht0 + i, HT - 1) * 2 + s) * OT * 64];
+        if (job != wave) {
+            load_w2(0, job, 0);
+            if (HT > kFewGroup) load_w2(1, job, kFewGroup);
+        }
+        const auto group = [&](int set, int ht0) {
 #pragma unroll
             for (int i = 0; i < kFewGroup; ++i) {
                 if (ht0 + i >= HT) break;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
-                    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w[i][s]),
+                    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w2[set][i][s]),
                                                                  __builtin_bit_cast(f16x8, hs[((jj * HT + ht0 + i) * 2 + s) * 2 + g]), acc, 0, 0, 0);
             }
+            if (ht0 + 2 * kFewGroup < HT) load_w2(set, job, ht0 + 2 * kFewGroup);
+        };
+        for (int ht0 = 0; ht0 < HT; ht0 += 2 * kFewGroup) {
+            group(0, ht0);
+            if (ht0 + kFewGroup < HT) group(1, ht0 + kFewGroup);
         }
         if (j == 0)
 #pragma unroll
@@ -289,7 +327,7 @@ template <typename T> __global__ __launch_bounds__(kFewGenericThreads) void few_
 size_t few_lds_bytes(const slicemoe_config &c, bool mfma)
 {
     const int ds = c.d / c.S;
-    return mfma ? few_lds(c.k, c.He / 32, ds) : few_generic_lds(ds, c.Hr, c.He);
+    return mfma ? few_lds(c.E, c.k, c.He / 32, ds) : few_generic_lds(ds, c.Hr, c.He);
 }
 
 template <int DS> static hipError_t run_few(const slicemoe_config &c, const FewArgs &A, size_t lds, hipStream_t s)

@@ -103,18 +103,18 @@ template <int BITS> __device__ __forceinline__ void store_hidden(const MxArgs &A
 // LDS as linear kilobytes and are read as they lie.  A ring of SLOTS images; one barrier per step, a fragment before its end: behind it
 // the next step's images have landed for every wavefront, and the present ones, whose last fragments are in registers, are free for the
 // step SLOTS ahead.
-template <int BITS_, bool DUAL_, int TR_, int TF_> struct MxTile {
+template <int BITS_, bool DUAL_, int TR_, int TF_, int KS_, int SLOTS_> struct MxTile {
     static constexpr int BITS = BITS_, TR = TR_, TF = TF_;
     static constexpr bool DUAL = DUAL_;
     static constexpr int IMAGES = DUAL ? 2 : 1, FT = TF / IMAGES;      // feature tiles of one image per wavefront
     static constexpr int RT = 2 * TR, FB = 2 * TF;                     // tiles of 32 per block: rows, features (of all images)
     static constexpr int BR = 32 * RT, BF = 32 * FB / IMAGES;          // rows, features of one image per block
-    static constexpr int KS = BITS == 4 ? 4 : 2;                       // instructions along a step
+    static constexpr int KS = KS_;                                     // instructions along a step
     static constexpr int F_TILE = KS * 1024, R_TILE = F_TILE * BITS / 4;   // bytes of a tile in a step: features, rows
     static constexpr int R_KB = R_TILE / 1024;
     static constexpr int R_BYTES = RT * R_TILE, F_BYTES = FB * F_TILE, S_BYTES = (RT + FB) * 256;
     static constexpr int SLOT = R_BYTES + F_BYTES + S_BYTES;
-    static constexpr int SLOTS = BITS == 4 || TR + TF == 4 ? 2 : 3;
+    static constexpr int SLOTS = SLOTS_;
     static constexpr int LDS = SLOTS * SLOT;
     static constexpr int R_TILES = RT / 4, F_TILES = FB / 4;           // tiles that a wavefront requests
     static constexpr int LOADS = R_KB * R_TILES + KS * F_TILES + 1;       // instructions per wavefront and step
@@ -207,7 +207,7 @@ template <typename S> __device__ __forceinline__ void mx_steps(f32x16 (&acc)[S::
             fn[t] = *(const int *)(p + (S::RT + (t < S::FT ? wf * S::FT + t : S::FB / 2 + wf * S::FT + t - S::FT)) * 256);
     };
     const auto take_scales = [&]() {   // (the instruction's byte is a constant: the second half's two are moved down)
-        const int shift = S::BITS == 8 ? 16 * odd : 0;
+        const int shift = S::KS == 2 ? 16 * odd : 0;
 #pragma unroll
         for (int u = 0; u < S::TR; ++u) rs[u] = (int)((uint32_t)rn[u] >> shift);
 #pragma unroll
@@ -294,14 +294,16 @@ __device__ __forceinline__ void eight_features(const f32x16 &acc, int q, float (
     }
 }
 
-// A tile of the product.  Rows of whole pieces of eight features: the addend's pieces of 32 rows are requested together, those of the next
-// 32 in front of the stores of these (one by one they were a trip to memory each: 16384 x 1024 x 2816 took 80 us instead of 70).
-template <typename S, typename T> __device__ __forceinline__ void store_tile(const f32x16 (&acc)[S::TF][S::TR], const MxArgs &A, int rt0, int ft0, int j, int g)
+// A tile of the product.  Rows of whole pieces of eight features go through the LDS, 32 rows of a wavefront at a time, so that memory sees
+// whole lines (as they lie in the accumulators an access is 32 bytes of each of 32 rows); the addend's pieces of 32 rows are requested
+// together, those of the next 32 in front of the stores of these.
+template <typename S, typename T>
+__device__ __forceinline__ void store_tile(const f32x16 (&acc)[S::TF][S::TR], const MxArgs &A, int rt0, int ft0, int lane, int wave, char *lds)
 {
     typedef RowPiece<T> P;
-    constexpr int W = 8 / P::V;   // 16-byte accesses of eight features
     const T *addend = (const T *)A.addend;
     T *y = (T *)A.y;
+    const int j = lane & 31, g = lane >> 5;
     if (A.N % 8 != 0) {
 #pragma unroll
         for (int u = 0; u < S::TR; ++u)
@@ -316,43 +318,59 @@ template <typename S, typename T> __device__ __forceinline__ void store_tile(con
                 }
         return;
     }
-    u32x4 a[2][S::FT][2][W];
+    constexpr int W = 8 / P::V;                                   // 16-byte accesses of eight features
+    constexpr int COLS = 32 * S::FT, STRIDE = COLS + 4;           // floats of a row in the LDS
+    constexpr int LANES = COLS / 8, ROWS = 64 / LANES, N = 32 / ROWS;   // lanes per row, rows per access, accesses of 32 rows
+    static_assert(4 * 32 * STRIDE * 4 <= S::LDS, "a part of the LDS for every wavefront");
+    float *mine = (float *)lds + wave * (32 * STRIDE);
+    const int r = lane / LANES, c = 8 * (lane % LANES), f = 32 * ft0 + c;
+    constexpr int SETS = S::TR == 4 && W == 2 ? 1 : 2;            // (beside 256 accumulators two sets of fp32 pieces do not fit)
+    u32x4 a[SETS][N][W];
     const auto request = [&](int u) {
-        const int row = 32 * (rt0 + u) + j;
-        const T *r = addend + (size_t)(row < A.T ? row : A.T - 1) * A.N;
 #pragma unroll
-        for (int t = 0; t < S::FT; ++t)
+        for (int i = 0; i < N; ++i) {
+            const int row = 32 * (rt0 + u) + ROWS * i + r;
+            const T *p = addend + (size_t)(row < A.T ? row : A.T - 1) * A.N + (f < A.N ? f : 0);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int f = 32 * (ft0 + t) + 16 * q + 8 * g;
-#pragma unroll
-                for (int w = 0; w < W; ++w) a[u & 1][t][q][w] = *(const u32x4 *)(r + (f < A.N ? f : 0) + w * P::V);
-            }
+            for (int w = 0; w < W; ++w) a[u % SETS][i][w] = *(const u32x4 *)(p + w * P::V);
+        }
     };
     const auto tile = [&](auto with) {
         constexpr bool ADD = decltype(with)::value;
-        if constexpr (ADD) request(0);
+        if constexpr (ADD && SETS == 2) request(0);
 #pragma unroll
         for (int u = 0; u < S::TR; ++u) {
-            const int row = 32 * (rt0 + u) + j;
             if constexpr (ADD)
-                if (u + 1 < S::TR) request(u + 1);
+                if (u + SETS - 1 < S::TR) request(u + SETS - 1);
+            wave_lds_sync();   // the last 32 rows have been read
 #pragma unroll
             for (int t = 0; t < S::FT; ++t)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int f = 32 * (ft0 + t) + 16 * q + 8 * g;
-                    float v[8];
-                    eight_features(acc[t][u], q, v);
-                    if constexpr (ADD)
+                for (int q = 0; q < 4; ++q)
+                    *(f32x4 *)(mine + j * STRIDE + 32 * t + 8 * q + 4 * g) =
+                        f32x4{acc[t][u][4 * q], acc[t][u][4 * q + 1], acc[t][u][4 * q + 2], acc[t][u][4 * q + 3]};
+            wave_lds_sync();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] += P::get(a[u & 1][t][q][i / P::V], i % P::V);
-                    if (row < A.T && f < A.N)
+            for (int i = 0; i < N; ++i) {
+                const int row = 32 * (rt0 + u) + ROWS * i + r;
+                const float *m = mine + (ROWS * i + r) * STRIDE + c;
+                const f32x4 lo = *(const f32x4 *)m, hi = *(const f32x4 *)(m + 4);
+                float v[8];
 #pragma unroll
-                        for (int w = 0; w < W; ++w) *(u32x4 *)(y + (size_t)row * A.N + f + w * P::V) = P::make(v + w * P::V);
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = lo[e];
+                    v[4 + e] = hi[e];
                 }
+                if constexpr (ADD)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += P::get(a[u % SETS][i][e / P::V], e % P::V);
+                if (row < A.T && f < A.N)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) *(u32x4 *)(y + (size_t)row * A.N + f + w * P::V) = P::make(v + w * P::V);
+            }
         }
     };
+    lds_barrier();   // every wavefront is past its last fragment
     if (addend) tile(std::true_type());
     else tile(std::false_type());
 }
@@ -391,7 +409,7 @@ template <typename S, typename T> __global__ __launch_bounds__(256, S::PER_SIMD)
         }
     } else {
         if (A.splits > 1) A.y = (float *)A.y + (size_t)place.split * A.T * A.N;
-        store_tile<S, T>(acc, A, rt0, ft0, j, g);
+        store_tile<S, T>(acc, A, rt0, ft0, lane, wave, lds);
     }
 }
 
@@ -615,7 +633,7 @@ static MxChoice choose(long long T, int f_tiles, int Kt, int N, int bits, bool d
         if (s > 1 && (dual || n > kSplitBlocks)) break;
         const auto depth = [&](long long b) { return b == 0 ? 0 : c.one + c.each * ((double)b / cus > 1 ? (double)b / cus - 1 : 0); };
         double t = (double)Kt / s * (n / round * depth(round) + depth(rest)) + c.start * ((n + round - 1) / round);
-        if (s > 1) t += 3 + (double)s * T * N * 8 / 5e6;   // the shares' addition: a launch, and their sums through the caches
+        if (s > 1) t += 5 + (double)s * T * N * 8 / 4e6;   // the shares' addition: a launch, and their sums through the caches
         if (t < least) {
             least = t;
             best = {false, s};
@@ -639,8 +657,8 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
         return f_tiles <= 160 ? run_few<BITS, DUAL, 1, 16, T>(A, f_tiles, s) : run_few<BITS, DUAL, 1, 8, T>(A, f_tiles, s);
     }
     const MxChoice c = choose(A.T, f_tiles, A.Kt, A.N, BITS, DUAL);
-    if (c.large) return run_tiles<MxTile<BITS, DUAL, 4, 4>, T>(A, f_tiles, 1, nullptr, s);
-    return run_tiles<MxTile<BITS, DUAL, 2, 2>, T>(A, f_tiles, c.splits, shares, s);
+    if (c.large) return run_tiles<MxTile<BITS, DUAL, 4, 4, BITS == 4 ? 4 : 2, BITS == 4 ? 2 : 3>, T>(A, f_tiles, 1, nullptr, s);
+    return run_tiles<MxTile<BITS, DUAL, 2, 2, BITS == 4 ? 4 : 2, 2>, T>(A, f_tiles, c.splits, shares, s);
 }
 
 size_t mx_product_workspace(const slicemoe_mx_product_config &c) { return align_up(shares_bytes(c.T, c.N, mx_tiles_k(c.K)), 256); }
