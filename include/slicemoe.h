@@ -268,7 +268,7 @@ slicemoe_status slicemoe_forward(const slicemoe_config *cfg, const void *h, cons
  * UNSUPPORTED for more than SLICEMOE_FEW_ASSIGNMENTS assignments (T*S*k), for a capacity limit, and where the k He hidden units of a slice do not fit
  * the LDS (k * He > 61 thousand): these are slicemoe_forward's.
  */
-#define SLICEMOE_FEW_ASSIGNMENTS 4096
+#define SLICEMOE_FEW_ASSIGNMENTS 1024
 slicemoe_status slicemoe_forward_few(const slicemoe_config *cfg, const void *h, const slicemoe_weights *w, void *h_out,
                                      int32_t *topk_idx, float *topk_p, slicemoe_stream_t stream);
 

@@ -27,7 +27,7 @@ SLICEMOE_BF16 = 1
 SLICEMOE_GATE_NONE = 0
 SLICEMOE_GATE_CHANNEL = 1
 SLICEMOE_GATE_TOKEN = 2
-SLICEMOE_FEW_ASSIGNMENTS = 4096
+SLICEMOE_FEW_ASSIGNMENTS = 1024
 SLICEMOE_FLAG_FORCE_GENERIC = 1
 SLICEMOE_FLAG_REQUIRE_MFMA = 2
 SLICEMOE_FLAG_SINGLE_STREAM = 4

@@ -42,6 +42,18 @@ __device__ __forceinline__ h2 pk_fma_clamp01(h2 a, h2 b, h2 c)
     return d;
 }
 
+// Two accumulators -> a packed fp16 pair of kappa * GELU(z): what activation_tile does eight times.
+__device__ __forceinline__ uint32_t activation_pair(float a0, float a1, h2 p2, h2 bias, const EpiConst &K)
+{
+    const h2 s = pk_fma(__builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(a0, a1)), p2, bias);
+    const h2 v = pk_fma(s, s, as_h2(K.neg_w0));
+    h2 Q = pk_fma(v, as_h2(K.q[kGeluM]), as_h2(K.q[kGeluM - 1]));
+#pragma unroll
+    for (int c = kGeluM - 2; c >= 0; --c) Q = pk_fma(Q, v, as_h2(K.q[c]));
+    const h2 F = pk_fma_clamp01(s, Q, as_h2(K.half));
+    return __builtin_bit_cast(uint32_t, s * F);
+}
+
 // 16 accumulators of one 32x32 tile -> 8 packed fp16 pairs of kappa * GELU(z); pair i holds the
 // accumulator registers 2i and 2i+1, i.e. contraction slots of GEMM2 in register order.
 __device__ __forceinline__ void activation_tile(const f32x16 &acc, h2 p2, const h2 (&bias)[8], const EpiConst &K, uint4 (&out)[2])

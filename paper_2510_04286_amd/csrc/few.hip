@@ -9,6 +9,7 @@
 //
 // Every sum has the order it has in the four launches (route_mfma.hip, ffn_mfma.hip, combine.hip), so the outputs are their bits.
 #include "expert_activation.h"
+#include "gemm_tile.h"
 #include "route_select.h"
 #include "wavefront.h"
 
@@ -22,6 +23,8 @@ struct FewArgs {
     const char *packed;
     PackedLayout L;
     int k, HT;
+    uint32_t ht_magic;   // ceil(2^31 / HT): see `job_of`
+    int parts_log2, run; // wavefronts that share an output tile, and hidden tiles of each
     bool b2_first;
     EpiConst K;
     bf16_t *out;
@@ -29,25 +32,42 @@ struct FewArgs {
     float *p;
 };
 
-// LDS: terms of the router's hidden layer, its second layer, activations [k][HT][2][2] pieces, outputs [k][ds] fp16.
+// LDS: terms of the router's hidden layer, its second layer, first-layer sums [k][HT][2][16], activations [k][HT][2][2] pieces, outputs [k][ds] fp16.
 constexpr int kFewTerms = 8 * 2 * 2 * 2 * 16;
 __host__ __device__ constexpr size_t few_router2(int E) { return (size_t)((E + 31) / 32) * 8 * 2 * 64 * 16; }
-__host__ __device__ constexpr size_t few_lds(int E, int k, int HT, int ds) { return kFewTerms + few_router2(E) + (size_t)k * HT * 64 + (size_t)k * ds * 2 + 64; }
+__host__ __device__ constexpr size_t few_lds(int E, int k, int HT, int ds) { return kFewTerms + few_router2(E) + (size_t)k * HT * 192 + (size_t)k * ds * 2; }
+
+// Largest value over the wavefront.
+__device__ __forceinline__ float wavefront_max(float v)
+{
+    v = fmaxf(v, __int_as_float(lane_move<0xB1>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(lane_move<0x4E>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(lane_move<0x141>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(lane_move<0x140>(__float_as_int(v))));
+    const int b = __float_as_int(v);
+    return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 0)), __int_as_float(__builtin_amdgcn_readlane(b, 16))),
+                 fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 32)), __int_as_float(__builtin_amdgcn_readlane(b, 48))));
+}
 
 // (Two blocks a CU where the registers allow it: 512 slices of width 64 are one round then.)
 template <int DS, int ET>
-__global__ __launch_bounds__(kFewThreads, DS <= 64 ? 4 : 2) void few_mfma_kernel(FewArgs A)
+__global__ __launch_bounds__(kFewThreads, DS <= 96 ? 4 : 2) void few_mfma_kernel(FewArgs A)
 {
     constexpr int KS = SliceTiles<DS>::KS, OT = SliceTiles<DS>::OT, HTr = 8;
-    constexpr bool AHEAD = KS <= 8;   // the next hidden tile's fragments are requested before this one's are used
+    // First-layer fragments in registers, two sets of them: of two hidden tiles, or of the two halves of one
+    constexpr int HALVES = KS == 6 || KS == 24 ? 2 : 1, CH = KS / HALVES;
+    constexpr int SETS = DS <= 96 || DS == 384 ? 1 : 2;   // of second-layer fragments: one where two blocks a CU, or wide rows, leave no more registers
+    constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(16) char lds[];
-    uint4 *us = (uint4 *)lds;                                    // [HTr][2 K-steps][2 terms][2 lane groups]
-    uint4 *w2s = (uint4 *)(lds + kFewTerms);                     // [ET][HTr][2][64]
-    char *rest = lds + kFewTerms + ET * HTr * 2 * 64 * 16;
-    uint4 *hs = (uint4 *)rest;                                   // [k][HT][2][2]
-    half_t *ys = (half_t *)(rest + (size_t)A.k * A.HT * 64);     // [k][DS]
+    u32x4 *us = (u32x4 *)lds;                                    // [HTr][2 K-steps][2 terms][2 lane groups]
+    u32x4 *w2s = (u32x4 *)(lds + kFewTerms);                     // [ET][HTr][2][64]
+    float *zs = (float *)(lds + kFewTerms + ET * HTr * 2 * 64 * 16);   // [k][HT][2 lane groups][16]
+    uint32_t *hs = (uint32_t *)(zs + (size_t)A.k * A.HT * 32);   // [k][HT][2 K-steps][2 lane groups][4]
+    half_t *ys = (half_t *)(hs + (size_t)A.k * A.HT * 16);       // [k][DS]
+    __shared__ __align__(16) float logits[64];                   // then their exponentials
     __shared__ int sel_idx[8];
     __shared__ float sel_p[8];
+    __shared__ f32x4 sums[kFewWaves / 2][4][2];                  // of output tiles that wavefronts share
     const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const long long n = blockIdx.x;
     const int k = A.k, HT = A.HT;
@@ -56,153 +76,258 @@ __global__ __launch_bounds__(kFewThreads, DS <= 64 ? 4 : 2) void few_mfma_kernel
     bf16x8 xb[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) xb[ks] = load_row_piece<DS>(xr, ks, g);
+    float v = -INFINITY;   // wavefront 0: the logit of expert `lane`
     {
-        const uint4 *w1 = (const uint4 *)(A.packed + A.L.r_w1) + wave * KS * 64 + lane;
-        uint4 w1r[KS], w2r[ET][2];
+        const u32x4 *w1 = (const u32x4 *)(A.packed + A.L.r_w1) + wave * KS * 64 + lane;
+        u32x4 w1r[KS], w2r[ET][2];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) w1r[ks] = w1[ks * 64];
-        const uint4 *w2 = (const uint4 *)(A.packed + A.L.r_w2) + lane;   // [ET][HTr][2][64]
+        f32x16 acc = load_bias_tile((const float *)(A.packed + A.L.r_b1), wave, g), gacc[ET];
+        const u32x4 *w2 = (const u32x4 *)(A.packed + A.L.r_w2) + lane;   // [ET][HTr][2][64]
 #pragma unroll
         for (int et = 0; et < ET; ++et)
 #pragma unroll
             for (int s = 0; s < 2; ++s) w2r[et][s] = w2[((et * HTr + wave) * 2 + s) * 64];
-        f32x16 acc = load_bias_tile((const float *)(A.packed + A.L.r_b1), wave, g), gacc[ET];
         if (wave == 0)
 #pragma unroll
             for (int et = 0; et < ET; ++et) gacc[et] = load_bias_tile((const float *)(A.packed + A.L.r_b2), et, g);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) acc = mfma_bf16(__builtin_bit_cast(bf16x8, w1r[ks]), xb[ks], acc);
-#pragma unroll
-        for (int et = 0; et < ET; ++et)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) w2s[((et * HTr + wave) * 2 + s) * 64 + lane] = w2r[et][s];
         uint32_t t0[8], t1[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) relu_split_pair(acc[2 * i], acc[2 * i + 1], t0[i], t1[i]);
         if (j == 0)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                us[((wave * 2 + s) * 2 + 0) * 2 + g] = make_uint4(t0[4 * s], t0[4 * s + 1], t0[4 * s + 2], t0[4 * s + 3]);
-                us[((wave * 2 + s) * 2 + 1) * 2 + g] = make_uint4(t1[4 * s], t1[4 * s + 1], t1[4 * s + 2], t1[4 * s + 3]);
+                us[((wave * 2 + s) * 2 + 0) * 2 + g] = u32x4{t0[4 * s], t0[4 * s + 1], t0[4 * s + 2], t0[4 * s + 3]};
+                us[((wave * 2 + s) * 2 + 1) * 2 + g] = u32x4{t1[4 * s], t1[4 * s + 1], t1[4 * s + 2], t1[4 * s + 3]};
             }
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) w2s[((et * HTr + wave) * 2 + s) * 64 + lane] = w2r[et][s];
         lds_barrier();
         if (wave == 0) {
+            // (the operands are read three K-steps ahead: a chain that waits for each read takes twice as long)
+            constexpr int RING = 4, N = 2 * HTr;
+            f16x8 u0[RING], u1[RING], a2[RING][ET];
+            const auto fetch = [&](auto index) {
+                constexpr int I = decltype(index)::value;
+                u0[I % RING] = __builtin_bit_cast(f16x8, us[(I * 2 + 0) * 2 + g]);
+                u1[I % RING] = __builtin_bit_cast(f16x8, us[(I * 2 + 1) * 2 + g]);
 #pragma unroll
-            for (int h = 0; h < HTr; ++h)
+                for (int et = 0; et < ET; ++et) a2[I % RING][et] = __builtin_bit_cast(f16x8, w2s[(et * N + I) * 64 + lane]);
+            };
+            for_range<0, RING - 1>(fetch);
+            for_range<0, N>([&](auto index) {
+                constexpr int I = decltype(index)::value;
+                if constexpr (I + RING - 1 < N) fetch(Int<I + RING - 1>());
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const f16x8 u0 = __builtin_bit_cast(f16x8, us[((h * 2 + s) * 2 + 0) * 2 + g]);
-                    const f16x8 u1 = __builtin_bit_cast(f16x8, us[((h * 2 + s) * 2 + 1) * 2 + g]);
+                for (int et = 0; et < ET; ++et)   // small term first
+                    gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2[I % RING][et], u1[I % RING], gacc[et], 0, 0, 0);
 #pragma unroll
-                    for (int et = 0; et < ET; ++et) {   // small term first
-                        const f16x8 a2 = __builtin_bit_cast(f16x8, w2s[((et * HTr + h) * 2 + s) * 64 + lane]);
-                        gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2, u1, gacc[et], 0, 0, 0);
-                        gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2, u0, gacc[et], 0, 0, 0);
-                    }
-                }
-            float v[ET * 16];
+                for (int et = 0; et < ET; ++et) gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2[I % RING][et], u0[I % RING], gacc[et], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            // an expert per lane; equal logits go to the lower one (logits that are not numbers: to a lane that is free)
+            if (j == 0)
 #pragma unroll
-            for (int et = 0; et < ET; ++et)
+                for (int et = 0; et < ET; ++et)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) v[et * 16 + r] = gacc[et][r];
-            select_experts<ET, kRouteInference>(v, 0, j == 0, g, A.L.E, k, nullptr, 0.f, 1.4426950408889634f, nullptr, 0.f, sel_idx, sel_p, false, nullptr);
+                    for (int q = 0; q < 4; ++q)
+                        *(f32x4 *)(logits + et * 32 + 8 * q + 4 * g) = f32x4{gacc[et][4 * q], gacc[et][4 * q + 1], gacc[et][4 * q + 2], gacc[et][4 * q + 3]};
+            wave_lds_sync();
+            if (lane < A.L.E) v = logits[lane];
+            unsigned long long open = __ballot(lane < A.L.E);
+            for (int jj = 0; jj < k; ++jj) {
+                const bool mine = open >> lane & 1;
+                const float most = wavefront_max(mine ? v : -INFINITY);
+                const unsigned long long at = __ballot(mine && v == most), from = at ? at : open;
+                const int e = __builtin_ctzll(from);
+                open &= ~(1ull << e);
+                if (lane == 0) sel_idx[jj] = e;
+            }
         }
         lds_barrier();
     }
-    if (tid < k) {   // (the selection is in range whatever the logits are: see select_experts)
-        if (A.idx) A.idx[n * k + tid] = sel_idx[tid];
-        if (A.p) A.p[n * k + tid] = sel_p[tid];
-    }
-    const auto expert = [&](int jj) { return A.packed + A.L.experts + (size_t)__builtin_amdgcn_readfirstlane(sel_idx[jj]) * A.L.e_stride; };
+    const int chosen = sel_idx[lane & 7];   // lane jj: the expert of selection jj
+    const auto expert = [&](int jj) { return A.packed + A.L.experts + (size_t)__builtin_amdgcn_readlane(chosen, jj) * A.L.e_stride; };
+    const uint32_t lane16 = 16 * lane;      // (addresses are a uniform base and this)
 
-    // Second layer: the k OT output tiles, each the sum over all hidden tiles in their order, kFewGroup of them at a time.
-    const int jobs2 = k * OT;
-    uint4 w2[2][kFewGroup][2];
+    // Second layer: the k OT output tiles, each the sum over all hidden tiles in their order.  With fewer tiles than wavefronts `parts` of these
+    // share one: each has a run of the hidden tiles, whose fragments it requests as soon as the experts are known, and passes the sums on.
+    const int jobs2 = k * OT, parts = 1 << A.parts_log2, part = wave & (parts - 1), job2 = wave >> A.parts_log2;
+    const int first = part * A.run, last = min(HT, first + A.run);   // (the last runs may be empty)
+    // job / HT without a division (2^31 / HT rounded up is off by less than HT / 2^31, and jobs are a few thousand)
+    const auto job_of = [&](int job) { return (int)__umulhi(2u * (uint32_t)job, A.ht_magic); };
+    u32x4 w2[SETS][kFewGroup][2];
     const auto load_w2 = [&](int set, int job, int ht0) {   // [HT][2][OT][64]
-        const uint4 *p = (const uint4 *)(expert(job / OT) + A.L.e_w2) + (size_t)(job % OT) * 64 + lane;
+        const char *p = expert(job / OT) + A.L.e_w2 + (size_t)(job % OT) * 1024;
 #pragma unroll
-        for (int i = 0; i < kFewGroup; ++i)
+        for (int i = 0; i < kFewGroup; ++i) {
+            const char *t = p + (size_t)min(ht0 + i, HT - 1) * (2 * OT * 1024);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) w2[set][i][s] = p[(size_t)(min(ht0 + i, HT - 1) * 2 + s) * OT * 64];
+            for (int s = 0; s < 2; ++s) w2[set][i][s] = *(const u32x4 *)(t + s * OT * 1024 + lane16);
+        }
     };
+    const auto bias2 = [&](int job) { return load_bias_tile((const float *)(expert(job / OT) + A.L.e_b2), job % OT, g); };   // padded with zeros by the packer
+    // Activations: a pair of hidden units per thread and round (in the accumulators all 32 columns would be the same one).  b1: [HT][2 lane groups][8 pairs]
+    const int pairs = k * HT * 16;
+    const auto bias1 = [&](int q) {
+        const int jj = job_of(q >> 4);
+        return ((const uint32_t *)(A.packed + A.L.experts + (size_t)sel_idx[jj] * A.L.e_stride + A.L.e_b1))[q - jj * HT * 16];
+    };
+    uint32_t b1 = 0;
+    f32x16 acc2;
     // First layer: the k HT hidden tiles in turn over the wavefronts.
     {
         const int jobs = k * HT;
-        uint4 w1[AHEAD ? 2 : 1][KS];
-        const auto load_w1 = [&](int set, int job) {
-            const uint4 *p = (const uint4 *)(expert(job / HT) + A.L.e_w1) + (size_t)(job % HT) * KS * 64 + lane;
+        u32x4 w1[2][CH];
+        f32x16 acc;
+        const auto load_w1 = [&](int set, int job, int half) {
+            const int jj = job_of(job);
+            const char *p = expert(jj) + A.L.e_w1 + (size_t)(job - jj * HT) * (KS * 1024) + half * (CH * 1024);
 #pragma unroll
-            for (int i = 0; i < KS; ++i) w1[set][i] = p[i * 64];
+            for (int i = 0; i < CH; ++i) w1[set][i] = *(const u32x4 *)(p + i * 1024 + lane16);
         };
-        const auto tile = [&](int set, int job) {
-            const int jj = job / HT, ht = job - jj * HT;
-            h2 bias[8];
-            load_bias_tile((const uint4 *)(expert(jj) + A.L.e_b1), ht, g, bias);
-            const float pv = sel_p[jj];
-            const h2 p2 = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(pv, pv));
-            f32x16 acc;
+        const auto multiply = [&](int set, auto which) {
+            constexpr int HALF = decltype(which)::value;
+            if constexpr (HALF == 0)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+                for (int r = 0; r < 16; ++r) acc[r] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) acc = mfma_bf16(__builtin_bit_cast(bf16x8, w1[set][ks]), xb[ks], acc);
-            uint4 hb[2];
-            activation_tile(acc, p2, bias, A.K, hb);
+            for (int i = 0; i < CH; ++i) acc = mfma_bf16(__builtin_bit_cast(bf16x8, w1[set][i]), xb[HALF * CH + i], acc);
+        };
+        const auto leave = [&](int job) {
             if (j == 0)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) hs[(job * 2 + s) * 2 + g] = hb[s];
+                for (int q = 0; q < 4; ++q) *(f32x4 *)(zs + (job * 2 + g) * 16 + 4 * q) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
         };
-        load_w1(0, min(wave, jobs - 1));
-        if (wave < jobs2) load_w2(0, wave, 0);
-#pragma unroll 1
-        for (int job = wave; job < jobs; job += AHEAD ? 2 * kFewWaves : kFewWaves) {
-            if constexpr (AHEAD) {   // (past the end: the last one again)
-                load_w1(1, min(job + kFewWaves, jobs - 1));
-                tile(0, job);
-                load_w1(0, min(job + 2 * kFewWaves, jobs - 1));
-                if (job + kFewWaves < jobs) tile(1, job + kFewWaves);
+        load_w1(0, min(wave, jobs - 1), 0);
+        if constexpr (HALVES == 2) load_w1(1, min(wave, jobs - 1), 1);
+        else load_w1(1, min(wave + kFewWaves, jobs - 1), 0);
+        if (job2 < jobs2) {
+            load_w2(0, job2, first);
+            acc2 = bias2(job2);
+        }
+        if (tid < pairs) b1 = bias1(tid);
+        if (wave == 0) {   // the probabilities, while the weights are on their way; their sum in the order of select_experts
+            const float nm = -wavefront_max(v) * kLog2e, ex = __builtin_amdgcn_exp2f(fmaf(v, kLog2e, nm));
+            wave_lds_sync();
+            logits[lane] = ex;
+            wave_lds_sync();
+            float den = 0.f;
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 t = *(const f32x4 *)(logits + et * 32 + 8 * q + 4 * g);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) den += t[c];
+                }
+            const auto sd = __builtin_amdgcn_permlane32_swap(__float_as_uint(den), __float_as_uint(den), false, false);
+            const float rden = __builtin_amdgcn_rcpf(__uint_as_float(sd[0]) + __uint_as_float(sd[1]));
+            if (lane < k) {
+                const int e = sel_idx[lane];
+                const float p = logits[e] * rden;
+                sel_p[lane] = p;
+                if (A.idx) A.idx[n * k + lane] = e;
+                if (A.p) A.p[n * k + lane] = p;
+            }
+        }
+        // one hidden tile (two of them) and the requests of the next; the first time outside of the loop: in front of it the second layer's
+        // fragments are on their way, and a loop would wait for them
+        const auto some = [&](int job) {
+            if constexpr (HALVES == 2) {
+                multiply(0, Int<0>());
+                if (job + kFewWaves < jobs) load_w1(0, job + kFewWaves, 0);
+                multiply(1, Int<1>());
+                if (job + kFewWaves < jobs) load_w1(1, job + kFewWaves, 1);
+                leave(job);
             } else {
-                tile(0, job);
-                load_w1(0, min(job + kFewWaves, jobs - 1));
+                multiply(0, Int<0>());
+                leave(job);
+                if (job + 2 * kFewWaves < jobs) load_w1(0, job + 2 * kFewWaves, 0);
+                if (job + kFewWaves < jobs) {
+                    multiply(1, Int<0>());
+                    leave(job + kFewWaves);
+                }
+                if (job + 3 * kFewWaves < jobs) load_w1(1, job + 3 * kFewWaves, 0);
             }
-        }
-    }
-    if (wave < jobs2 && HT > kFewGroup) load_w2(1, wave, kFewGroup);
-    lds_barrier();
-    for (int job = wave; job < jobs2; job += kFewWaves) {
-        const int jj = job / OT, ot = job - jj * OT;
-        const f32x16 bias = load_bias_tile((const float *)(expert(jj) + A.L.e_b2), ot, g);   // padded with zeros by the packer
-        f32x16 acc;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = A.b2_first ? bias[r] : 0.f;
-        if (job != wave) {
-            load_w2(0, job, 0);
-            if (HT > kFewGroup) load_w2(1, job, kFewGroup);
-        }
-        const auto group = [&](int set, int ht0) {
-#pragma unroll
-            for (int i = 0; i < kFewGroup; ++i) {
-                if (ht0 + i >= HT) break;
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-                    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w2[set][i][s]),
-                                                                 __builtin_bit_cast(f16x8, hs[((jj * HT + ht0 + i) * 2 + s) * 2 + g]), acc, 0, 0, 0);
-            }
-            if (ht0 + 2 * kFewGroup < HT) load_w2(set, job, ht0 + 2 * kFewGroup);
         };
-        for (int ht0 = 0; ht0 < HT; ht0 += 2 * kFewGroup) {
-            group(0, ht0);
-            if (ht0 + kFewGroup < HT) group(1, ht0 + kFewGroup);
-        }
-        if (j == 0)
+        constexpr int STEP = HALVES == 2 ? kFewWaves : 2 * kFewWaves;
+        if (wave < jobs) some(wave);
+#pragma unroll 1
+        for (int job = wave + STEP; job < jobs; job += STEP) some(job);
+    }
+    if (SETS == 2 && job2 < jobs2 && first + kFewGroup < last) load_w2(SETS - 1, job2, first + kFewGroup);
+    lds_barrier();
+    for (int q = tid; q < pairs; q += kFewThreads) {
+        const int job = q >> 4, i = q & 7;
+        const float pv = sel_p[job_of(job)];
+        const h2 p2 = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(pv, pv));
+        const float2 z = *(const float2 *)(zs + 2 * q);   // [job][g][pair]
+        const uint32_t b = q == tid ? b1 : bias1(q);
+        hs[((job * 2 + (i >> 2)) * 2 + (q >> 3 & 1)) * 4 + (i & 3)] = activation_pair(z.x, z.y, p2, as_h2(b), A.K);
+    }
+    lds_barrier();
+    for (int stage = 0; stage < parts; ++stage) {
+        if (part == stage)
+            for (int job = job2; job < jobs2; job += kFewWaves) {   // (with parts one job at most)
+                const int jj = job / OT, ot = job - jj * OT;
+                if (job != job2) {
+                    acc2 = bias2(job);
+                    load_w2(0, job, first);
+                    if (SETS == 2 && first + kFewGroup < last) load_w2(SETS - 1, job, first + kFewGroup);
+                }
+                const f32x16 bias = acc2;
+                if (!A.b2_first)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int f = ot * 32 + 8 * q + 4 * g;
-                if (f >= DS) continue;   // padding columns of the last tile
-                float v[4];
+                    for (int r = 0; r < 16; ++r) acc2[r] = 0.f;
+                if (stage > 0)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = A.b2_first ? acc[4 * q + c] : acc[4 * q + c] + bias[4 * q + c];
-                *(uint2 *)(ys + jj * DS + f) = make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]));
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 t = sums[job][q][g];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc2[4 * q + c] = t[c];
+                    }
+                const auto group = [&](int set, int ht0) {
+                    f16x8 h[kFewGroup][2];   // (read together; past the end: the last one again)
+#pragma unroll
+                    for (int i = 0; i < kFewGroup; ++i)
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            h[i][s] = __builtin_bit_cast(f16x8, *(const u32x4 *)(hs + (((jj * HT + min(ht0 + i, HT - 1)) * 2 + s) * 2 + g) * 4));
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < kFewGroup; ++i)
+                        if (ht0 + i < last)
+#pragma unroll
+                            for (int s = 0; s < 2; ++s)
+                                acc2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w2[set][i][s]), h[i][s], acc2, 0, 0, 0);
+                    if (ht0 + SETS * kFewGroup < last) load_w2(set, job, ht0 + SETS * kFewGroup);
+                };
+                for (int ht0 = first; ht0 < last; ht0 += SETS * kFewGroup) {
+                    group(0, ht0);
+                    if (SETS == 2 && ht0 + kFewGroup < last) group(SETS - 1, ht0 + kFewGroup);
+                }
+                if (stage + 1 < parts) {
+                    if (j == 0)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) sums[job][q][g] = f32x4{acc2[4 * q], acc2[4 * q + 1], acc2[4 * q + 2], acc2[4 * q + 3]};
+                } else if (j == 0)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int f = ot * 32 + 8 * q + 4 * g;
+                        if (f >= DS) continue;   // padding columns of the last tile
+                        float y[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) y[c] = A.b2_first ? acc2[4 * q + c] : acc2[4 * q + c] + bias[4 * q + c];
+                        *(uint2 *)(ys + jj * DS + f) = make_uint2(pack_half2(y[0], y[1]), pack_half2(y[2], y[3]));
+                    }
             }
+        if (stage + 1 < parts) lds_barrier();
     }
     lds_barrier();
     for (int f = tid; f < DS; f += kFewThreads) {
@@ -221,15 +346,15 @@ struct FewGenericArgs {
     int32_t *idx;
     float *p;
 };
-constexpr int kFewGenericThreads = 256;
+constexpr int kFewGenericThreads = 1024;   // (256: 15.4 us for the 64 slices of 16 tokens of the d = 256 fp32 layer instead of XX)
 static size_t few_generic_lds(int ds, int Hr, int He) { return (size_t)(ds + (Hr > He ? Hr : He) + kFewGenericThreads + ds) * 4; }
 
-// out[o] = sum over i < in of v[i] W[i * ld + o] for o < n, by `parts` threads each (a power of two that divides 256 into columns): f(o, sum).
+// out[o] = sum over i < in of v[i] W[i * ld + o] for o < n, by `parts` threads each (a power of two): f(o, sum).
 template <typename T, typename F>
 __device__ __forceinline__ void few_columns(const float *v, int in, const T *__restrict__ W, int ld, int n, float *part, const F &f)
 {
     int parts = 1;
-    while (parts < 16 && parts * 2 * n <= kFewGenericThreads) parts *= 2;
+    while (parts < 32 && parts * 2 * n <= kFewGenericThreads && parts * 8 < in) parts *= 2;
     const int per = kFewGenericThreads / parts, tid = threadIdx.x, q = tid / per, lo = tid % per;
     for (int o0 = 0; o0 < n; o0 += per) {
         const int o = o0 + lo;
@@ -353,7 +478,12 @@ hipError_t launch_forward_few(const slicemoe_config &c, const void *h, const sli
         kern<<<c.T * c.S, kFewGenericThreads, lds, s>>>(A);
         return hipGetLastError();
     }
-    const FewArgs A{(const bf16_t *)h, (const char *)w.packed, packed_layout(c), c.k, c.He / 32, ffn_bias_first(c), make_epi_const(), (bf16_t *)h_out, idx, p};
+    const int HT = c.He / 32, tiles = c.k * ((ds + 31) / 32);
+    int parts_log2 = 0;   // output tiles times parts: at most the wavefronts
+    while (tiles << (parts_log2 + 1) <= kFewWaves) ++parts_log2;
+    const int run = (HT + (1 << parts_log2) - 1) >> parts_log2;
+    const FewArgs A{(const bf16_t *)h, (const char *)w.packed, packed_layout(c), c.k, HT, (uint32_t)(((1ull << 31) + HT - 1) / HT), parts_log2, run,
+                    ffn_bias_first(c), make_epi_const(), (bf16_t *)h_out, idx, p};
     switch (ds) {
         case 24: return run_few<24>(c, A, lds, s);
         case 48: return run_few<48>(c, A, lds, s);
