@@ -49,6 +49,17 @@ __device__ __forceinline__ float wavefront_max(float v)
                  fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 32)), __int_as_float(__builtin_amdgcn_readlane(b, 48))));
 }
 
+// The lane with the largest v among the `open` ones, the lowest of equal ones (of values that are not numbers any open lane), which is then closed.
+__device__ __forceinline__ int largest_open(float v, int lane, unsigned long long &open)
+{
+    const bool mine = open >> lane & 1;
+    const float most = wavefront_max(mine ? v : -INFINITY);
+    const unsigned long long at = __ballot(mine && v == most);
+    const int e = __builtin_ctzll(at ? at : open);
+    open &= ~(1ull << e);
+    return e;
+}
+
 // (Two blocks a CU where the registers allow it: 512 slices of width 64 are one round then.)
 template <int DS, int ET>
 __global__ __launch_bounds__(kFewThreads, DS <= 96 ? 4 : 2) void few_mfma_kernel(FewArgs A)
@@ -130,7 +141,7 @@ __global__ __launch_bounds__(kFewThreads, DS <= 96 ? 4 : 2) void few_mfma_kernel
                 for (int et = 0; et < ET; ++et) gacc[et] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a2[I % RING][et], u0[I % RING], gacc[et], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             });
-            // an expert per lane; equal logits go to the lower one (logits that are not numbers: to a lane that is free)
+            // an expert per lane
             if (j == 0)
 #pragma unroll
                 for (int et = 0; et < ET; ++et)
@@ -141,11 +152,7 @@ __global__ __launch_bounds__(kFewThreads, DS <= 96 ? 4 : 2) void few_mfma_kernel
             if (lane < A.L.E) v = logits[lane];
             unsigned long long open = __ballot(lane < A.L.E);
             for (int jj = 0; jj < k; ++jj) {
-                const bool mine = open >> lane & 1;
-                const float most = wavefront_max(mine ? v : -INFINITY);
-                const unsigned long long at = __ballot(mine && v == most), from = at ? at : open;
-                const int e = __builtin_ctzll(from);
-                open &= ~(1ull << e);
+                const int e = largest_open(v, lane, open);
                 if (lane == 0) sel_idx[jj] = e;
             }
         }
@@ -346,28 +353,39 @@ struct FewGenericArgs {
     int32_t *idx;
     float *p;
 };
-constexpr int kFewGenericThreads = 1024;   // (256: 15.4 us for the 64 slices of 16 tokens of the d = 256 fp32 layer instead of XX)
-static size_t few_generic_lds(int ds, int Hr, int He) { return (size_t)(ds + (Hr > He ? Hr : He) + kFewGenericThreads + ds) * 4; }
+constexpr int kFewGenericThreads = 1024;
+static size_t few_generic_lds(int ds, int Hr, int He, int k) { return (size_t)(ds + (Hr > k * He ? Hr : k * He) + kFewGenericThreads + k * ds) * 4; }
 
-// out[o] = sum over i < in of v[i] W[i * ld + o] for o < n, by `parts` threads each (a power of two): f(o, sum).
-template <typename T, typename F>
-__device__ __forceinline__ void few_columns(const float *v, int in, const T *__restrict__ W, int ld, int n, float *part, const F &f)
+// f(o, sum over i < in of v(o)[i] col(o)[i * ld]) for the columns o < n, each by 2^p threads (neighbouring columns by neighbouring threads), sixteen
+// rows in flight.
+template <typename T, typename VEC, typename COL, typename F>
+__device__ __forceinline__ void few_columns(int in, int ld, int n, float *part, const VEC &vec, const COL &col, const F &f)
 {
-    int parts = 1;
-    while (parts < 32 && parts * 2 * n <= kFewGenericThreads && parts * 8 < in) parts *= 2;
-    const int per = kFewGenericThreads / parts, tid = threadIdx.x, q = tid / per, lo = tid % per;
+    int p = 0;
+    while (p < 5 && (n << (p + 1)) <= kFewGenericThreads && (8 << p) < in) ++p;
+    constexpr int kLog2Threads = 10;
+    static_assert(1 << kLog2Threads == kFewGenericThreads, "");
+    const int parts = 1 << p, log2per = kLog2Threads - p, per = 1 << log2per, tid = threadIdx.x, q = tid >> log2per, lo = tid & (per - 1);
     for (int o0 = 0; o0 < n; o0 += per) {
         const int o = o0 + lo;
         float s = 0.f;
         if (o < n) {
-            const T *w = W + o;
+            const T *w = col(o);
+            const float *v = vec(o);
             int i = q;
-            for (; i + 7 * parts < in; i += 8 * parts) {   // eight rows in flight
-                float t[8];
+            for (; i + 15 * parts < in; i += 16 * parts) {
+                float t[16];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) t[u] = Storage<T>::load(w + (size_t)(i + u * parts) * ld);
+                for (int u = 0; u < 16; ++u) t[u] = Storage<T>::load(w + (size_t)(i + u * parts) * ld);
 #pragma unroll
-                for (int u = 0; u < 8; ++u) s = fmaf(v[i + u * parts], t[u], s);
+                for (int u = 0; u < 16; ++u) s = fmaf(v[i + u * parts], t[u], s);
+            }
+            for (; i + 3 * parts < in; i += 4 * parts) {
+                float t[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) t[u] = Storage<T>::load(w + (size_t)(i + u * parts) * ld);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) s = fmaf(v[i + u * parts], t[u], s);
             }
             for (; i < in; i += parts) s = fmaf(v[i], Storage<T>::load(w + (size_t)i * ld), s);
         }
@@ -379,80 +397,78 @@ __device__ __forceinline__ void few_columns(const float *v, int in, const T *__r
                 for (int u = 0; u < parts; ++u) s += part[u * per + lo];
         }
         if (q == 0 && o < n) f(o, s);
-        if (parts > 1) __syncthreads();
+        if (parts > 1 && o0 + per < n) __syncthreads();
     }
 }
 
 template <typename T> __global__ __launch_bounds__(kFewGenericThreads) void few_generic_kernel(FewGenericArgs A)
 {
     extern __shared__ __align__(16) char lds[];
-    float *xs = (float *)lds, *hid = xs + A.ds, *part = hid + (A.Hr > A.He ? A.Hr : A.He), *ys = part + kFewGenericThreads;
+    float *xs = (float *)lds, *part = xs + A.ds, *ys = part + kFewGenericThreads, *hid = ys + A.k * A.ds;   // ys: [k][ds], hid: [k][He]
     __shared__ float logit[64], sel_p[8];
     __shared__ int sel_idx[8];
     const int tid = threadIdx.x, ds = A.ds, E = A.E, k = A.k;
     const long long n = blockIdx.x;
-    for (int i = tid; i < ds; i += kFewGenericThreads) {
-        xs[i] = Storage<T>::load((const T *)A.x + n * ds + i);
-        ys[i] = 0.f;
-    }
+    for (int i = tid; i < ds; i += kFewGenericThreads) xs[i] = Storage<T>::load((const T *)A.x + n * ds + i);
     __syncthreads();
-    few_columns<T>(xs, ds, (const T *)A.w.Wr1, A.Hr, A.Hr, part, [&](int o, float s) { hid[o] = fmaxf(s + Storage<T>::load((const T *)A.w.br1 + o), 0.f); });
+    const auto of_x = [&](int) { return xs; };
+    const auto of_hidden = [&](int) { return hid; };
+    few_columns<T>(ds, A.Hr, A.Hr, part, of_x, [&](int o) { return (const T *)A.w.Wr1 + o; },
+                   [&](int o, float s) { hid[o] = fmaxf(s + Storage<T>::load((const T *)A.w.br1 + o), 0.f); });
     __syncthreads();
-    few_columns<T>(hid, A.Hr, (const T *)A.w.Wr2, E, E, part, [&](int o, float s) { logit[o] = s + Storage<T>::load((const T *)A.w.br2 + o); });
+    few_columns<T>(A.Hr, E, E, part, of_hidden, [&](int o) { return (const T *)A.w.Wr2 + o; },
+                   [&](int o, float s) { logit[o] = s + Storage<T>::load((const T *)A.w.br2 + o); });
     __syncthreads();
-    if (tid < 64) {   // lane e has expert e; equal logits go to the lower one
-        float v = tid < E ? logit[tid] : -INFINITY;
-        float m = v;
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
-        const float ex = tid < E ? expf(v - m) : 0.f;
+    if (tid < 64) {   // lane e has expert e
+        const float v = tid < E ? logit[tid] : -INFINITY, ex = tid < E ? expf(v - wavefront_max(v)) : 0.f;
         const float den = wavefront_sum_f32(ex);
-        bool free_ = tid < E;
+        unsigned long long open = __ballot(tid < E);
         for (int jj = 0; jj < k; ++jj) {
-            float bv = free_ ? v : -INFINITY;
-            int be = free_ ? tid : 64 + tid;
-#pragma unroll
-            for (int i = 32; i > 0; i >>= 1) {
-                const float ov = __shfl_xor(bv, i);
-                const int oe = __shfl_xor(be, i);
-                if (ov > bv || (!(bv > ov) && oe < be)) {
-                    bv = ov;
-                    be = oe;
-                }
-            }
-            be = __builtin_amdgcn_readfirstlane(be);   // (the lanes agree but where logits are not numbers; nor does the bound matter elsewhere)
-            be = be < E ? be : E - 1;
-            if (tid == be) {
-                free_ = false;
-                sel_idx[jj] = be;
-                sel_p[jj] = ex / den;
+            const int e = largest_open(v, tid, open);
+            if (tid == e) {
+                const float p = ex / den;
+                sel_idx[jj] = e;
+                sel_p[jj] = p;
+                if (A.idx) A.idx[n * k + jj] = e;
+                if (A.p) A.p[n * k + jj] = p;
             }
         }
     }
     __syncthreads();
-    if (tid < k) {
-        if (A.idx) A.idx[n * k + tid] = sel_idx[tid];
-        if (A.p) A.p[n * k + tid] = sel_p[tid];
+    // the k experts together: column o = jj He + hidden unit, then jj ds + output
+    const int He = A.He;
+    few_columns<T>(ds, He, k * He, part, of_x,
+                   [&](int o) {
+                       const int jj = o / He;
+                       return (const T *)A.w.W1 + (size_t)sel_idx[jj] * ds * He + (o - jj * He);
+                   },
+                   [&](int o, float s) {
+                       const int jj = o / He;
+                       const float z = fmaf(sel_p[jj], s, Storage<T>::load((const T *)A.w.b1 + (size_t)sel_idx[jj] * He + (o - jj * He)));
+                       hid[o] = 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+                   });
+    __syncthreads();
+    few_columns<T>(He, ds, k * ds, part, [&](int o) { return hid + o / ds * He; },
+                   [&](int o) {
+                       const int jj = o / ds;
+                       return (const T *)A.w.W2 + (size_t)sel_idx[jj] * He * ds + (o - jj * ds);
+                   },
+                   [&](int o, float s) {
+                       const int jj = o / ds;
+                       ys[o] = s + Storage<T>::load((const T *)A.w.b2 + (size_t)sel_idx[jj] * ds + (o - jj * ds));
+                   });
+    __syncthreads();
+    for (int i = tid; i < ds; i += kFewGenericThreads) {
+        float s = 0.f;
+        for (int jj = 0; jj < k; ++jj) s += ys[jj * ds + i];
+        Storage<T>::store((T *)A.out + n * ds + i, s);
     }
-    for (int jj = 0; jj < k; ++jj) {
-        const int e = sel_idx[jj];
-        const float p = sel_p[jj];
-        const T *b1 = (const T *)A.w.b1 + (size_t)e * A.He, *b2 = (const T *)A.w.b2 + (size_t)e * ds;
-        few_columns<T>(xs, ds, (const T *)A.w.W1 + (size_t)e * ds * A.He, A.He, A.He, part, [&](int o, float s) {
-            const float z = fmaf(p, s, Storage<T>::load(b1 + o));
-            hid[o] = 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        });
-        __syncthreads();
-        few_columns<T>(hid, A.He, (const T *)A.w.W2 + (size_t)e * A.He * ds, ds, ds, part, [&](int o, float s) { ys[o] += s + Storage<T>::load(b2 + o); });
-        __syncthreads();
-    }
-    for (int i = tid; i < ds; i += kFewGenericThreads) Storage<T>::store((T *)A.out + n * ds + i, ys[i]);
 }
 
 size_t few_lds_bytes(const slicemoe_config &c, bool mfma)
 {
     const int ds = c.d / c.S;
-    return mfma ? few_lds(c.E, c.k, c.He / 32, ds) : few_generic_lds(ds, c.Hr, c.He);
+    return mfma ? few_lds(c.E, c.k, c.He / 32, ds) : few_generic_lds(ds, c.Hr, c.He, c.k);
 }
 
 template <int DS> static hipError_t run_few(const slicemoe_config &c, const FewArgs &A, size_t lds, hipStream_t s)
