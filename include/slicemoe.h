@@ -492,7 +492,7 @@ slicemoe_status slicemoe_clip_grads(const slicemoe_grad *grads, int32_t count, f
  * and behind the last tile's values follow 256 bytes of scales per tile: byte 4 (i + 32 h) + ks holds e + 127, or 255 for NaN.
  */
 typedef struct {
-    int32_t rows;       /* 0 <= rows                                                             */
+    int32_t rows;       /* 0 <= rows <= 2^30                                                     */
     int32_t cols;       /* the contracted width, 1 <= cols <= 2^20; rows * cols <= 2^40          */
     int32_t bits;       /* 4 or 8                                                                */
     int32_t dtype;      /* slicemoe_dtype of the plain matrix                                    */

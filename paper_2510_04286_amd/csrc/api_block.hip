@@ -53,7 +53,7 @@ static slicemoe_status validate(const slicemoe_mx_config *c)
 {
     if (!c || c->rows < 0 || c->cols < 1 || !bits_ok(c->bits) || !storage_ok(c->dtype)) return SLICEMOE_ERR_INVALID_ARG;
     if (c->transposed != 0 && c->transposed != 1) return SLICEMOE_ERR_INVALID_ARG;
-    return c->cols > 1 << 20 || (long long)c->rows * c->cols > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+    return c->cols > 1 << 20 || c->rows > 1 << 30 || (long long)c->rows * c->cols > 1ll << 40 ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
 }
 constexpr long long kMxMost = 1ll << 36;   // (a launch ends below 2^32 threads: 2^24 blocks of 128 x 64 results)
 static slicemoe_status validate(const slicemoe_mx_product_config *c)

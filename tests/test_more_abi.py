@@ -96,7 +96,7 @@ def test_mx_refusals_and_sizes(B):
     L, inv, uns, wsp = B.lib(), B.SLICEMOE_ERR_INVALID_ARG, B.SLICEMOE_ERR_UNSUPPORTED, B.SLICEMOE_ERR_WORKSPACE
     mc = B.make_mx_config
     for c, want in [(mc(-1, 64), inv), (mc(4, 0), inv), (mc(4, 64, 5), inv), (B.slicemoe_mx_config(4, 64, 4, 2, 0), inv), (B.slicemoe_mx_config(4, 64, 4, 1, 2), inv),
-                    (mc(4, (1 << 20) + 1), uns), (mc((1 << 31) - 1, 1024), uns)]:
+                    (mc(4, (1 << 20) + 1), uns), (mc(1 << 30, 1025), uns), (mc((1 << 30) + 1, 1), uns), (mc((1 << 31) - 1, 1), uns)]:
         assert L.slicemoe_mx_quantize(by(c), P, Q, NULL) == want and L.slicemoe_mx_dequantize(by(c), Q, P, NULL) == want and B.slicemoe_mx_bytes(c) == 0
     ok = mc(4, 64)
     for args in [(NULL, Q), (P, NULL), (ODD, Q), (P, ctypes.c_void_p(4096 + 128))]:
