@@ -11,6 +11,10 @@
 // a power of two for the row.
 // With one gate for all rows both d_post and d_gate are a column's sum of ds n1 times that column's gate and weight, so there are two column
 // sums in either case; persistent blocks, a row of partial sums per block, added in block order (bit-reproducible).
+//
+// Bound by memory: 65536 x 4096 in bf16 with one gate row takes 440 us forward and 614 backward (its 2.1 and 3.2 GB: 418 and 627 us at the 5.14
+// TB/s of a large copy), 12289 x 768 with a gate per token 20 and 32 (18.4 and 29.4); below some thousand rows by the launches, one forward and two
+// backward (32 x 1024: 4 us in the kernel; 3001 x 513 in fp32 backward: 15 us of 9.6), and by a row's two sums one behind the other.
 #include "block_norm.h"
 #include "mx.h"
 #include "norm.h"
@@ -18,14 +22,57 @@
 
 namespace slicemoe {
 
+// How a row's pieces lie: whole and aligned; or each at any element, the last one the V elements in front of the row's end, of which the first
+// `cut` are another lane's too (they count once in the sums, both lanes store them alike): no branch between the requests (12289 x 767 in bf16
+// backward: 36.7 us, 81 with a branch for the last piece); or by element, for rows below a piece and where a lane's columns
+// have to be its own (microscaled rows).
+enum { kAligned, kOverlapped, kByElement };
+template <typename T, int MODE> struct Place {
+    static constexpr int V = RowPiece<T>::V;
+    int from, cut;
+    bool mine;
+    __device__ __forceinline__ Place(int at, int d) : from(MODE == kOverlapped && at + V > d ? d - V : at), cut(at - from), mine(at < d) {}
+    __device__ __forceinline__ uint32_t bytes() const { return (uint32_t)from * (uint32_t)sizeof(T); }   // (32 bits on a row's uniform start)
+    __device__ __forceinline__ u32x4 load(const T *row, int d) const
+    {
+        if constexpr (MODE == kByElement) return load_piece<T, false>(row, from, d);
+        else if constexpr (MODE == kOverlapped) return *(const loose *)((const char *)row + bytes());
+        else {   // (zeros past the row's end)
+            u32x4 p = *(const u32x4 *)((const char *)row + (mine ? bytes() : 0u));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = mine ? p[i] : 0;
+            return p;
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int d, const float *v) const
+    {
+        if (!mine) return;
+        if constexpr (MODE == kByElement) store_piece<T, false>(row, from, d, v);
+        else if constexpr (MODE == kOverlapped) *(loose *)((char *)row + bytes()) = RowPiece<T>::make(v);
+        else *(u32x4 *)((char *)row + bytes()) = RowPiece<T>::make(v);
+    }
+    // sum + f(0) + .. + f(V - 1), of the elements that are this lane's.
+    template <typename F> __device__ __forceinline__ float add(float sum, const F &f) const
+    {
+        float t = sum;
+#pragma unroll
+        for (int i = 0; i < V; ++i) t += f(i);
+        if constexpr (MODE == kOverlapped)
+            if (cut > 0) {
+                t = sum;
+#pragma unroll
+                for (int i = 0; i < V; ++i) t += i >= cut ? f(i) : 0.f;
+            }
+        return t;
+    }
+};
+
 // mean(v^2) + eps of a row in registers as r = 1 / sqrt of it and the power of two k that v was multiplied with: v / rms = (v k) r.
-template <int W, int NP, int V> __device__ __forceinline__ float row_rsqrt(const float (&v)[NP][V], int d, float eps, float &k, float *lds)
+template <int W, int NP, int V, typename P> __device__ __forceinline__ float row_rsqrt(const float (&v)[NP][V], const P &place, int d, float eps, float &k, float *lds)
 {
     float ss = 0.f;
 #pragma unroll
-    for (int c = 0; c < NP; ++c)
-#pragma unroll
-        for (int i = 0; i < V; ++i) ss += v[c][i] * v[c][i];
+    for (int c = 0; c < NP; ++c) ss = place(c).add(ss, [&](int i) { return v[c][i] * v[c][i]; });
     float mean = row_sum<W>(ss, lds) / d + eps;
     k = 1.f;
     if (!in_range(mean)) {
@@ -34,15 +81,13 @@ template <int W, int NP, int V> __device__ __forceinline__ float row_rsqrt(const
         for (int c = 0; c < NP; ++c)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const uint32_t a = __float_as_uint(v[c][i]) & 0x7fffffffu;
+                const uint32_t a = __float_as_uint(v[c][i]) & 0x7fffffffu;   // (elements of the row in any case)
                 top = a > top ? a : top;
             }
         k = range_factor(row_max<W>(top, lds), eps);
         ss = 0.f;
 #pragma unroll
-        for (int c = 0; c < NP; ++c)
-#pragma unroll
-            for (int i = 0; i < V; ++i) ss += v[c][i] * k * (v[c][i] * k);
+        for (int c = 0; c < NP; ++c) ss = place(c).add(ss, [&](int i) { return v[c][i] * k * (v[c][i] * k); });
         mean = row_sum<W>(ss, lds) / d + eps * k * k;
     }
     return 1.f / sqrtf(mean);
@@ -83,9 +128,17 @@ __device__ __forceinline__ void store_mx(const float (&y)[NP][V], uint8_t *mx, u
     }
 }
 
+// With 16384 fp32 columns the registers hold a row and not the weights too (LEAN): those are read again for each row, from the caches, and the
+// compiler must not take them out of the loop.
+template <bool LEAN, typename T> __device__ __forceinline__ const T *per_row(const T *p)
+{
+    if constexpr (LEAN) asm volatile("" : "+s"(p));
+    return p;
+}
+
 // A block takes the rows b, b + gridDim.x, .. (W = 1: each of its wavefronts one of four).  gate_ld: 0 for a gate of one row.  sum and y may
 // be x or residual: a row's owners have all of it in registers before the first of them stores.
-template <typename T, bool ALIGNED, int W, int NP, bool MX>
+template <typename T, int MODE, int W, int NP, bool MX>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const T *x, const T *__restrict__ post, const T *__restrict__ gate, long long gate_ld,
                                                                         const T *residual, float a, const T *__restrict__ pre, T *sum, T *y,
                                                                         uint8_t *__restrict__ mx, uint8_t *__restrict__ mx_scales, int bits,
@@ -94,33 +147,43 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const 
     constexpr int V = RowPiece<T>::V, LANES = 64 * W, ROWS = W == 1 ? 4 : 1;
     __shared__ float lds[W];
     const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const auto place = [&](int c) { return Place<T, MODE>((lane + c * LANES) * V, d); };
+    constexpr bool LEAN = W * NP == 64;
+    const auto this_row = [](const T *p) { return per_row<LEAN>(p); };
     for (long long row = (long long)blockIdx.x * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < rows; row += (long long)gridDim.x * ROWS) {
         const size_t at0 = (size_t)row * d;
         u32x4 px[NP], pr[NP], pg[NP], po[NP], pw[NP];
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
-            px[c] = load_piece<T, ALIGNED>(x + at0, at, d);
-            pr[c] = load_piece<T, ALIGNED>(residual + at0, at, d);
+            px[c] = place(c).load(x + at0, d);
+            pr[c] = place(c).load(residual + at0, d);
         }
-        if (gate)
+        const auto factors = [&] {
+            if (gate)
 #pragma unroll
-            for (int c = 0; c < NP; ++c) pg[c] = load_piece<T, ALIGNED>(gate + (size_t)row * gate_ld, (lane + c * LANES) * V, d);
-        if (post)
+                for (int c = 0; c < NP; ++c) pg[c] = place(c).load(this_row(gate) + (size_t)row * gate_ld, d);
+            if (post)
 #pragma unroll
-            for (int c = 0; c < NP; ++c) po[c] = load_piece<T, ALIGNED>(post, (lane + c * LANES) * V, d);
-        if (pre)
+                for (int c = 0; c < NP; ++c) po[c] = place(c).load(this_row(post), d);
+        };
+        const auto weights = [&] {
+            if (pre)
 #pragma unroll
-            for (int c = 0; c < NP; ++c) pw[c] = load_piece<T, ALIGNED>(pre, (lane + c * LANES) * V, d);
+                for (int c = 0; c < NP; ++c) pw[c] = place(c).load(this_row(pre), d);
+        };
+        if (!LEAN) {
+            factors();
+            weights();
+        }
         float s[NP][V], k1 = 1.f, r1 = 1.f;
 #pragma unroll
         for (int c = 0; c < NP; ++c)
 #pragma unroll
             for (int i = 0; i < V; ++i) s[c][i] = RowPiece<T>::get(px[c], i);
-        if (post) r1 = row_rsqrt<W, NP, V>(s, d, eps, k1, lds);
+        if (post) r1 = row_rsqrt<W, NP, V>(s, place, d, eps, k1, lds);
+        if (LEAN) factors();
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 float n = s[c][i] * k1 * r1;
@@ -128,17 +191,17 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const 
                 if (gate) n *= RowPiece<T>::get(pg[c], i);
                 s[c][i] = fmaf(a, RowPiece<T>::get(pr[c], i), n);
             }
-            if (at < d) store_piece<T, ALIGNED>(sum + at0, at, d, s[c]);
+            place(c).store(sum + at0, d, s[c]);
         }
-        float k2, r2 = row_rsqrt<W, NP, V>(s, d, eps, k2, lds);
+        float k2, r2 = row_rsqrt<W, NP, V>(s, place, d, eps, k2, lds);
         if (stats && lane == 0) *(float2 *)(stats + 2 * row) = make_float2(k1 * r1, k2 * r2);
         if (!pre) continue;
+        if (LEAN) weights();
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) s[c][i] = s[c][i] * k2 * r2 * RowPiece<T>::get(pw[c], i);
-            if (at < d && y) store_piece<T, ALIGNED>(y + at0, at, d, s[c]);
+            if (y) place(c).store(y + at0, d, s[c]);
         }
         if constexpr (MX) {
             if (bits == 4) store_mx<4, T, W, NP, V>(s, mx, mx_scales, (int)row, d, lane);
@@ -162,8 +225,8 @@ template <int W> __device__ __forceinline__ float row_sum_once(float v, float *l
 }
 
 // part: [2][gridDim.x][d] column sums of dy n2 and of ds n1 (TOKEN: times the gate).  d_x may be d_y, d_residual may be d_sum (or d_y).
-template <typename T, bool ALIGNED, int W, int NP, bool TOKEN>
-__global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kernel(const T *__restrict__ x, const T *__restrict__ post, const T *__restrict__ gate,
+template <typename T, int MODE, int W, int NP, bool TOKEN>
+__global__ __launch_bounds__(W == 16 ? 1024 : 256, W == 16 ? 4 : 2) void block_norm_backward_kernel(const T *__restrict__ x, const T *__restrict__ post, const T *__restrict__ gate,
                                                                                  const T *__restrict__ sum, const T *__restrict__ pre,
                                                                                  const float *__restrict__ stats, const T *dy, const T *dsum, float a, T *dx,
                                                                                  T *dres, T *dgate, float *__restrict__ part, int rows, int d)
@@ -172,34 +235,50 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kern
     __shared__ float lds[2][W];
     __shared__ float cols[W == 1 ? 3 : 1][W == 1 ? 64 * V : 1];
     const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, wave = threadIdx.x >> 6;
+    const auto place = [&](int c) { return Place<T, MODE>((lane + c * LANES) * V, d); };
+    constexpr bool LEAN = W * NP == 64, APART = W == 16 && NP > 1;   // APART: a piece's values are unpacked when it is their turn
     u32x4 pw[NP], po[NP], pc[NP], ps[NP], pg[NP], pd[NP], px[NP], pt[TOKEN ? NP : 1];
-    float acc[2][NP][V];
+    // Column sums; of two and more pieces by 1024 lanes in the LDS (a lane's own, 16 bytes at a time: 2 x 64 KB with 16384 columns), for which there
+    // are no registers: 1024 rows of 16384 in bf16 took 169 us with them spilled, 70 so.
+    constexpr bool IN_LDS = APART;
+    float acc[2][IN_LDS ? 1 : NP][V];
+    extern __shared__ f32x4 block_norm_columns[];
+    const auto slot = [&](int q, int c, int h) { return block_norm_columns + ((q * NP + c) * (V / 4) + h) * LANES + lane; };
     const auto request = [&](long long row) {
         const size_t at0 = (size_t)row * d;
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
-            ps[c] = load_piece<T, ALIGNED>(sum + at0, at, d);
-            pg[c] = load_piece<T, ALIGNED>(dy + at0, at, d);
-            px[c] = load_piece<T, ALIGNED>(x + at0, at, d);
-            if constexpr (TOKEN) pt[c] = load_piece<T, ALIGNED>(gate + at0, at, d);
+            ps[c] = place(c).load(sum + at0, d);
+            pg[c] = place(c).load(dy + at0, d);
+            px[c] = place(c).load(x + at0, d);
+            if constexpr (TOKEN) pt[c] = place(c).load(gate + at0, d);
         }
         if (dsum)
 #pragma unroll
-            for (int c = 0; c < NP; ++c) pd[c] = load_piece<T, ALIGNED>(dsum + at0, (lane + c * LANES) * V, d);
+            for (int c = 0; c < NP; ++c) pd[c] = place(c).load(dsum + at0, d);
     };
     float ones[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) ones[i] = 1.f;
+    const auto weight = [&](int c) {
+        pw[c] = place(c).load(per_row<LEAN>(pre), d);
+        po[c] = post ? place(c).load(per_row<LEAN>(post), d) : RowPiece<T>::make(ones);
+        if constexpr (!TOKEN) pc[c] = gate ? place(c).load(per_row<LEAN>(gate), d) : RowPiece<T>::make(ones);
+    };
+    const auto turn = [&] {
+        if (APART) __builtin_amdgcn_sched_barrier(0);
+    };
 #pragma unroll
     for (int c = 0; c < NP; ++c) {
-        const int at = (lane + c * LANES) * V;
-        pw[c] = load_piece<T, ALIGNED>(pre, at, d);
-        po[c] = post ? load_piece<T, ALIGNED>(post, at, d) : RowPiece<T>::make(ones);
-        if constexpr (!TOKEN) pc[c] = gate ? load_piece<T, ALIGNED>(gate, at, d) : RowPiece<T>::make(ones);
+        if (!LEAN) weight(c);
         pd[c] = u32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[0][c][i] = acc[1][c][i] = 0.f;
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if constexpr (!IN_LDS) acc[q][c][i] = 0.f;
+                else if (i % 4 == 0) *slot(q, c, i / 4) = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
     }
     const float inv_d = 1.f / d, normed = post ? inv_d : 0.f;   // without a norm behind the block d_x is m1
     const long long stride = (long long)gridDim.x * ROWS;
@@ -212,6 +291,13 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kern
     }
     for (; row < rows; row += stride) {
         const size_t at0 = (size_t)row * d;
+        if (W == 16 && !LEAN)
+#pragma unroll
+            for (int c = 0; c < NP; ++c) {   // (nothing of them is kept unpacked or multiplied)
+                keep_packed(pw[c]);
+                keep_packed(po[c]);
+                if constexpr (!TOKEN) keep_packed(pc[c]);
+            }
         if (!AHEAD) {
             request(row);
             r = *(const float2 *)(stats + 2 * row);
@@ -225,8 +311,13 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kern
             cd[c] = pd[c];
             cx[c] = px[c];
             if constexpr (TOKEN) ct[c] = pt[c];
-#pragma unroll
-            for (int i = 0; i < V; ++i) along += RowPiece<T>::get(cg[c], i) * RowPiece<T>::get(pw[c], i) * (RowPiece<T>::get(cs[c], i) * r.y);
+            if (LEAN) pw[c] = place(c).load(per_row<true>(pre), d);
+            along = place(c).add(along, [&](int i) { return RowPiece<T>::get(cg[c], i) * RowPiece<T>::get(pw[c], i) * (RowPiece<T>::get(cs[c], i) * r.y); });
+            if (APART) {
+                keep_packed(cs[c]);
+                keep_packed(cg[c]);
+            }
+            turn();
         }
         const float r1 = r.x, r2 = r.y;
         if (AHEAD && row + stride < rows) {
@@ -238,36 +329,50 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kern
         float ds[NP][V];
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
-            float v[V];
+            float v[V], u[V];
+            if (LEAN) weight(c);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float n2 = RowPiece<T>::get(cs[c], i) * r2, g = RowPiece<T>::get(cg[c], i), n1 = RowPiece<T>::get(cx[c], i) * r1;
                 ds[c][i] = RowPiece<T>::get(cd[c], i) + r2 * (g * RowPiece<T>::get(pw[c], i) - n2 * mn2);
                 const float gt = TOKEN ? RowPiece<T>::get(ct[TOKEN ? c : 0], i) : RowPiece<T>::get(pc[c], i), dn = ds[c][i] * n1;
-                acc[0][c][i] += g * n2;
-                acc[1][c][i] += TOKEN ? dn * gt : dn;
-                along += dn * gt * RowPiece<T>::get(po[c], i);
+                if constexpr (!IN_LDS) {
+                    acc[0][c][i] += g * n2;
+                    acc[1][c][i] += TOKEN ? dn * gt : dn;
+                } else {
+                    acc[0][0][i] = g * n2;
+                    acc[1][0][i] = TOKEN ? dn * gt : dn;
+                }
+                u[i] = dn * gt * RowPiece<T>::get(po[c], i);
                 v[i] = a * ds[c][i];
             }
-            if (at < d) store_piece<T, ALIGNED>(dres + at0, at, d, v);
+            along = place(c).add(along, [&](int i) { return u[i]; });
+            if constexpr (IN_LDS)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int h = 0; h < V / 4; ++h) *slot(q, c, h) += f32x4{acc[q][0][4 * h], acc[q][0][4 * h + 1], acc[q][0][4 * h + 2], acc[q][0][4 * h + 3]};
+            place(c).store(dres + at0, d, v);
             if constexpr (TOKEN) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[i] = ds[c][i] * (RowPiece<T>::get(cx[c], i) * r1) * RowPiece<T>::get(po[c], i);
-                if (at < d) store_piece<T, ALIGNED>(dgate + at0, at, d, v);
+                place(c).store(dgate + at0, d, v);
             }
+            if (APART) keep_packed(cx[c]);
+            turn();
         }
         const float mn1 = row_sum_once<W>(along, lds[1]) * normed;
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
             float v[V];
+            if (LEAN) weight(c);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float gt = TOKEN ? RowPiece<T>::get(ct[TOKEN ? c : 0], i) : RowPiece<T>::get(pc[c], i);
                 v[i] = r1 * (ds[c][i] * gt * RowPiece<T>::get(po[c], i) - RowPiece<T>::get(cx[c], i) * r1 * mn1);
             }
-            if (at < d) store_piece<T, ALIGNED>(dx + at0, at, d, v);
+            place(c).store(dx + at0, d, v);
+            turn();
         }
     }
     // the block's column sums; with a row per wavefront the four wavefronts' are added in their order
@@ -276,7 +381,7 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kern
         float *out = part + ((size_t)q * gridDim.x + blockIdx.x) * d;
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int at = (lane + c * LANES) * V;
+            const auto at = place(c);
             if constexpr (W == 1) {
                 __syncthreads();
                 if (wave > 0)
@@ -290,38 +395,41 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_backward_kern
             if (W > 1 || wave == 0)
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    if (at + i < d) out[at + i] = acc[q][c][i];
+                    if (at.mine && i >= at.cut && at.from + i < d) {
+                        if constexpr (IN_LDS) out[at.from + i] = (*slot(q, c, i / 4))[i % 4];
+                        else out[at.from + i] = acc[q][c][i];
+                    }
         }
     }
 }
 
-// The sums over the blocks, in their order: 64 columns per block, its 16 wavefronts take the partial rows b, b + 16, ..  blockIdx.y = 0: d_pre; 1:
-// d_post and, where the gate is one row, d_gate.
-template <typename T>
+// The sums over the blocks: COLS columns per block, its 1024 / COLS groups of lanes take the partial rows g, g + groups, .., and are added in
+// their order.  blockIdx.y = 0: d_pre; 1: d_post and, where the gate is one row, d_gate.
+template <typename T, int COLS>
 __global__ __launch_bounds__(1024) void block_norm_weight_sum_kernel(const float *__restrict__ part, const T *__restrict__ post, const T *__restrict__ gate /* one row, or null */,
                                                                      float *__restrict__ dpre, float *__restrict__ dpost, float *__restrict__ dgate, int blocks, int d)
 {
-    __shared__ float t[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    constexpr int GROUPS = 1024 / COLS, PER = 64 / COLS;   // and groups in a wavefront
+    __shared__ float t[16][COLS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane % COLS, col = blockIdx.x * COLS + c;
     const float *p = part + (size_t)blockIdx.y * blocks * d;
     float a = 0.f;
-    if (col < d) {
-        int b = wave;
-        for (; b + 15 * 16 < blocks; b += 256) {   // sixteen rows in flight
+    if (col < d)
+        for (int b = wave * PER + lane / COLS; b < blocks; b += 16 * GROUPS) {   // sixteen rows in flight
             float v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = p[(size_t)(b + 16 * i) * d + col];
+            for (int i = 0; i < 16; ++i) v[i] = b + GROUPS * i < blocks ? p[(size_t)(b + GROUPS * i) * d + col] : 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) a += v[i];
         }
-        for (; b < blocks; b += 16) a += p[(size_t)b * d + col];
-    }
-    t[wave][lane] = a;
+#pragma unroll
+    for (int m = COLS; m < 64; m *= 2) a += __shfl_xor(a, m);
+    if (lane < COLS) t[wave][c] = a;
     __syncthreads();
-    if (wave == 0 && col < d) {
+    if (threadIdx.x < COLS && col < d) {
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s += t[i][lane];
+        for (int i = 0; i < 16; ++i) s += t[i][c];
         if (blockIdx.y == 0) dpre[col] = s;
         else {
             if (dpost) dpost[col] = gate ? s * Storage<T>::load(gate + col) : s;
@@ -330,8 +438,37 @@ __global__ __launch_bounds__(1024) void block_norm_weight_sum_kernel(const float
     }
 }
 
-struct BlockNormForward {
-    static constexpr bool kWide = true;
+// Calls f.run<T, MODE, W, NP>() for a row of d elements: one wavefront to 128 pieces (the forward, which holds less, to 192: 3001 x 513 in fp32 6.8
+// us, 7.8 with four), four to 512, then sixteen: with four the rows of 16384 in bf16 spill (1024 of them: 41 us forward, 303 backward; 36 and 70 with
+// sixteen).  Backward, a row per wavefront of 513 to 768 fp32 values has one wavefront per SIMD (21.8 us against 15.1).
+template <typename T, bool OVERLAP, typename F> static hipError_t pick_block_row(int d, const F &f)
+{
+    constexpr int V = RowPiece<T>::V;
+    const int pieces = (d + V - 1) / V;
+    const auto go = [&](auto mode) {
+        constexpr int M = decltype(mode)::value;
+        if (pieces <= 64) return f.template run<T, M, 1, 1>();
+        if (pieces <= 128) return f.template run<T, M, 1, 2>();
+        if constexpr (F::kThree)
+            if (pieces <= 192) return f.template run<T, M, 1, 3>();
+        if (pieces <= 256) return f.template run<T, M, 4, 1>();
+        if (pieces <= 512) return f.template run<T, M, 4, 2>();
+        if (pieces <= 1024) return f.template run<T, M, 16, 1>();
+        if (V == 8 || pieces <= 2048) return f.template run<T, M, 16, 2>();
+        if constexpr (V == 4) return f.template run<T, M, 16, 4>();   // (bf16 rows end at 2048 pieces)
+        return hipErrorInvalidValue;
+    };
+    if (d % V == 0) return go(std::integral_constant<int, kAligned>());
+    if constexpr (OVERLAP) {
+        if (d < V) return f.template run<T, kByElement, 1, 1>();
+        return go(std::integral_constant<int, kOverlapped>());
+    } else {
+        return go(std::integral_constant<int, kByElement>());
+    }
+}
+
+template <bool MX> struct BlockNormForward {
+    static constexpr bool kThree = true;
     const slicemoe_block_norm_config &c;
     const void *x, *post, *gate, *residual, *pre;
     void *sum, *y;
@@ -339,13 +476,13 @@ struct BlockNormForward {
     int bits;
     float *stats;
     hipStream_t s;
-    template <typename T, bool A, int W, int NP> hipError_t run() const
+    template <typename T, int MODE, int W, int NP> hipError_t run() const
     {
         constexpr int threads = W == 16 ? 1024 : 256, per_block = W == 1 ? 4 : 1;
         const int need = c.T / per_block + (c.T % per_block != 0), most = num_compute_units() * 8;
         const unsigned blocks = need < most ? need : most;
         uint8_t *scales = mx ? mx + mx_tiles(c.T, c.d) * mx_tile_bytes(bits) : nullptr;
-        const auto kern = mx ? block_norm_kernel<T, A, W, NP, true> : block_norm_kernel<T, A, W, NP, false>;
+        const auto kern = block_norm_kernel<T, MODE, W, NP, MX>;
         kern<<<blocks, threads, 0, s>>>((const T *)x, (const T *)post, (const T *)gate, c.gate == SLICEMOE_GATE_TOKEN ? c.d : 0, (const T *)residual,
                                         c.residual_scale, (const T *)pre, (T *)sum, (T *)y, mx, scales, bits, stats, c.T, c.d, c.eps);
         return hipGetLastError();
@@ -353,7 +490,7 @@ struct BlockNormForward {
 };
 
 struct BlockNormBackward {
-    static constexpr bool kWide = true;
+    static constexpr bool kThree = false;
     const slicemoe_block_norm_config &c;
     const void *x, *post, *gate, *sum, *pre;
     const float *stats;
@@ -364,33 +501,48 @@ struct BlockNormBackward {
     float *dpre, *part;
     int blocks;
     hipStream_t s;
-    template <typename T, bool A, int W, int NP> hipError_t run() const
+    template <typename T, int MODE, int W, int NP> hipError_t run() const
     {
         constexpr int threads = W == 16 ? 1024 : 256;
         const bool token = c.gate == SLICEMOE_GATE_TOKEN;
-        const auto kern = token ? block_norm_backward_kernel<T, A, W, NP, true> : block_norm_backward_kernel<T, A, W, NP, false>;
-        kern<<<blocks, threads, 0, s>>>((const T *)x, (const T *)post, (const T *)gate, (const T *)sum, (const T *)pre, stats, (const T *)dy, (const T *)dsum,
+        const auto kern = token ? block_norm_backward_kernel<T, MODE, W, NP, true> : block_norm_backward_kernel<T, MODE, W, NP, false>;
+        constexpr size_t lds = W == 16 && NP > 1 ? 2 * sizeof(float) * 1024 * NP * RowPiece<T>::V : 0;
+        if (lds) {
+            const hipError_t e = grant_dynamic_lds((const void *)kern, lds);
+            if (e != hipSuccess) return e;
+        }
+        kern<<<blocks, threads, lds, s>>>((const T *)x, (const T *)post, (const T *)gate, (const T *)sum, (const T *)pre, stats, (const T *)dy, (const T *)dsum,
                                         c.residual_scale, (T *)dx, (T *)dres, (T *)dgate, part, c.T, c.d);   // (no rows: writes zeros to part)
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        block_norm_weight_sum_kernel<T><<<dim3((c.d + 63) / 64, 2), 1024, 0, s>>>(part, (const T *)post, token ? nullptr : (const T *)gate, dpre, dpost,
-                                                                                token || !gate ? nullptr : (float *)dgate, blocks, c.d);
+        const int cols = c.d < 2048 ? 16 : 64;   // (both directions of 3001 x 513: 15.1 us with 16, 16.4 with 64; 256 x 4096: 19.5, 16.2)
+        const auto add = cols == 16 ? block_norm_weight_sum_kernel<T, 16> : block_norm_weight_sum_kernel<T, 64>;
+        add<<<dim3((c.d + cols - 1) / cols, 2), 1024, 0, s>>>(part, (const T *)post, token ? nullptr : (const T *)gate, dpre, dpost,
+                                                              token || !gate ? nullptr : (float *)dgate, blocks, c.d);
         return hipGetLastError();
     }
 };
 
+// Two blocks of four wavefronts a CU, or one of sixteen: what is resident, so that partial sums are few.  (65536 x 4096 bf16: 613 us with 512 blocks, 690
+// with 256, 667 with 1024; 12289 x 768: 31.9, 34.1, 35.3.)
 int block_norm_backward_blocks(const slicemoe_block_norm_config &c)
 {
-    const slicemoe_norm_config n = {c.T, c.d, c.eps, c.dtype};
-    return norm_backward_blocks(n);
+    const int V = c.dtype == SLICEMOE_BF16 ? 8 : 4, pieces = (c.d + V - 1) / V, rows = pieces <= 128 ? 4 : 1;
+    const int need = c.T / rows + (c.T % rows != 0), most = num_compute_units() * (pieces > 512 ? 1 : 2);
+    return need < 1 ? 1 : need < most ? need : most;
 }
 
 hipError_t launch_block_norm(const slicemoe_block_norm_config &c, const void *x, const void *post, const void *gate, const void *residual,
                              const void *pre, void *sum, void *y, uint8_t *mx, int bits, float *stats, hipStream_t s)
 {
     if (c.T == 0) return hipSuccess;
-    const BlockNormForward f{c, x, post, gate, residual, pre, sum, y, mx, bits, stats, s};
-    return c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);
+    const bool bf16 = c.dtype == SLICEMOE_BF16;
+    if (mx) {
+        const BlockNormForward<true> f{c, x, post, gate, residual, pre, sum, y, mx, bits, stats, s};
+        return bf16 ? pick_block_row<bf16_t, false>(c.d, f) : pick_block_row<float, false>(c.d, f);
+    }
+    const BlockNormForward<false> f{c, x, post, gate, residual, pre, sum, y, mx, bits, stats, s};
+    return bf16 ? pick_block_row<bf16_t, true>(c.d, f) : pick_block_row<float, true>(c.d, f);
 }
 
 hipError_t launch_block_norm_backward(const slicemoe_block_norm_config &c, const void *x, const void *post, const void *gate, const void *sum,
@@ -398,7 +550,7 @@ hipError_t launch_block_norm_backward(const slicemoe_block_norm_config &c, const
                                       float *dpost, void *dgate, float *dpre, float *part, hipStream_t s)
 {
     const BlockNormBackward f{c, x, post, gate, sum, pre, stats, dy, dsum, dx, dres, dpost, dgate, dpre, part, block_norm_backward_blocks(c), s};
-    return c.dtype == SLICEMOE_BF16 ? pick_row<bf16_t>(c.d, f) : pick_row<float>(c.d, f);
+    return c.dtype == SLICEMOE_BF16 ? pick_block_row<bf16_t, true>(c.d, f) : pick_block_row<float, true>(c.d, f);
 }
 
 }  // namespace slicemoe
