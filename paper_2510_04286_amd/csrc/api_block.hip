@@ -1,4 +1,4 @@
-// C ABI of the operators around the layer (norm, gated feed-forward network, gradient clipping): argument checks.
+// C ABI of the operators around the layer (norms, gated feed-forward network, microscaled values and products, gradient clipping): argument checks.
 // Host code only.
 #include <math.h>
 

@@ -1,11 +1,18 @@
 // The whole layer for few tokens in one launch: a block takes a slice from its router to its sum.
 //
-// slicemoe_forward is four launches whose outputs are the next one's inputs, 18 to 26 us for any small batch, of which the work of 32 tokens
+// slicemoe_forward is four launches whose outputs are the next one's inputs, 16 to 26 us for any small batch, of which the work of 32 tokens
 // is a few: what bounds it is launches and round trips.  Grouping by expert, which they are for, saves weight traffic only where an expert
-// has several rows.  Here nothing crosses a block: the eight wavefronts share a slice's router (a hidden tile each), one of them adds up
-// the logits and selects, then they share the k experts' hidden tiles and, behind a barrier, their output tiles; the k outputs meet in the LDS.
+// has several rows.  Here nothing crosses a block.  The eight wavefronts share a slice's router (a hidden tile each) and one of them adds up
+// the logits and selects; then they share the k experts' hidden tiles, whose sums become activations a pair of hidden units per thread, and
+// the output tiles, several wavefronts to a tile where there are fewer tiles; the k outputs meet in the LDS.
 // A slice takes a whole column of the matrix instruction's 32, and all 32 columns hold it: the loads of the weights (48 KB for the router
-// and 64 KB per expert at width 64, from the L2) and not the instructions set the pace, and a fragment is read by one lane each.
+// and 64 KB per expert at width 64, from the L2) and not the instructions set the pace, and a fragment is read by one lane each.  What
+// remains is one chain of router, selection and two layers, each a trip to the L2 (requested ahead where the address is known) and, at width
+// 128, two experts of 256 KB through one CU's 44 bytes a cycle.
+//
+// us in a graph, here / slicemoe_forward: d 1024 in 16 slices of 64 (32 experts, He 256): 1 token 7.1 / 16.0, 32 tokens 9.8 / 18.1; d 4096 in 32 slices
+// of 128 (64 experts, He 512): 1 token 11.5 / 22, 8 tokens 16.3 / 24, 16 tokens 29.8 / 24.3 (two rounds of blocks: from 512 slices of 128 columns on
+// the four launches are faster); d 768 in 8 slices of 96: 64 tokens 13.1 / 19.6; fp32, d 256 in 4 slices: 64 tokens 13.6 / 26.
 //
 // Every sum has the order it has in the four launches (route_mfma.hip, ffn_mfma.hip, combine.hip), so the outputs are their bits.
 #include "expert_activation.h"
@@ -16,7 +23,7 @@
 namespace slicemoe {
 
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * 64;
-constexpr int kFewGroup = 4;   // hidden tiles whose second-layer fragments a wavefront holds, twice: these and the next ones
+constexpr int kFewGroup = 4;   // hidden tiles whose second-layer fragments are requested together
 
 struct FewArgs {
     const bf16_t *x;
@@ -344,7 +351,9 @@ __global__ __launch_bounds__(kFewThreads, DS <= 96 ? 4 : 2) void few_mfma_kernel
     }
 }
 
-// Any shape, either storage type, fp32 arithmetic on the logical tensors: a thread per hidden unit, then per output.
+// Any shape, either storage type, fp32 arithmetic on the logical tensors: the columns of a layer by neighbouring threads, the rows of one by several
+// where columns are few; the k experts together.  Bound by the L2's latency: sixteen rows in flight (16 tokens of d 256 in fp32: 12.7 us, 15.6 with
+// four and one expert after the other).
 struct FewGenericArgs {
     const void *x;
     slicemoe_weights w;

@@ -1,7 +1,9 @@
 // Microscaled values (layout and scales: mx.h): conversion of a matrix, and back.
 //
 // A thread has a block of 32 values: a tile's 32 rows x 8 blocks are the 256 threads of a block.  Bound by memory; a row's eight blocks are
-// read by neighbouring lanes, 512 bytes of it together.
+// read by neighbouring lanes, 512 bytes of it together: 16384 x 1024 in bf16 to 4 bits 8.1 us, to 8 bits 10.3 (8.3 and 9.9 at the rate of a copy),
+// 11008 x 4096 19.2 and 23.9.  Back, the same pieces are stored in four parts: 33 us, 22 at that rate.  A transposed matrix is read 64 bytes
+// of a row at a time, 128 us: a set of weights is converted once.
 #include "mx.h"
 #include "norm_row.h"
 

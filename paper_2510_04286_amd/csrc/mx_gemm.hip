@@ -7,7 +7,13 @@
 // accumulators are features of one row: 16 of the 32 of a block, the other 16 in lane ^ 32.  The hidden rows' block maximum is thus one exchange
 // away, and their values leave as whole pieces in the order the second product reads them.
 //
-// v_mfma_scale_f32_32x32x64 takes 32 cycles of a SIMD with both operands in 4 bits, 64 with either in 8.
+// v_mfma_scale_f32_32x32x64 takes 32 cycles of a SIMD with both operands in 4 bits, 64 with either in 8; with random values in the operands the
+// chip's power limit allows 6.1 and 3.7 PFLOP/s from registers alone (zeros: 8.8).
+//
+// Three kernels: up to 64 rows, bound by the weights, one pass over them straight to the registers (32 rows, 4096 x 11008: 10.5 us in 8 bits; the network
+// 12.6 + 8.8, 45 and 22.5 MB); tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits: the pair 200 us = 3.7 PFLOP/s, the
+// second product 88 = 4.2).  Wide results and short contractions are bound by the results: 16384 x 1024 x 2816 with an addend takes 53 us, its
+// 184 MB of addend and y 36 at the rate of a copy.
 #include <type_traits>
 
 #include "gemm_tile.h"
@@ -602,6 +608,8 @@ template <int BITS, bool DUAL, int TR, int KW, typename T> static hipError_t run
 }
 
 // Which kernel a product takes: few rows, tiles of 128 x 128 (several blocks a CU), or of 256 x 256 (one).
+// us, few rows / tiles: 8 bits 64 rows 4096 11008 10.0 / 17.3, 11008 4096 14.7 / 15.6, 1024 2816 3.9 / 6.3; 32 rows 8.5 / 14.8, 10.5 / 14.2, 3.2 / 5.9.  4 bits
+// 64 rows 8.1 / 9.8, 11.7 / 13.6, 3.6 / 5.1; in the network at 4096 11008 29.9 / 28.6, 10.6 / 13.7 at 1024 2816.
 constexpr int kFewRows = 64;
 constexpr int kMostSplits = 8, kSplitBlocks = 512;   // shares of the contraction at most, and blocks of all shares together
 struct MxChoice {
@@ -654,6 +662,7 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
     const int f_tiles = DUAL ? 8 * A.hKt : A.w.tiles;
     if (A.T <= kFewRows) {
         if (A.T > 32) return run_few<BITS, DUAL, 2, 8, T>(A, f_tiles, s);
+        // (16 wavefronts where blocks are few, 8 else: 8 bits 4096 2048 3.9 us / 4.6 with 8; 1024 11008 4.1 / 3.4)
         return f_tiles <= 160 ? run_few<BITS, DUAL, 1, 16, T>(A, f_tiles, s) : run_few<BITS, DUAL, 1, 8, T>(A, f_tiles, s);
     }
     const MxChoice c = choose(A.T, f_tiles, A.Kt, A.N, BITS, DUAL);
