@@ -271,6 +271,10 @@ slicemoe_status slicemoe_block_norm(const slicemoe_block_norm_config *cfg, const
     for (const void *p : {x, post_weight, gate, residual, pre_weight, (const void *)sum, (const void *)y})
         if (misaligned(p, 16)) return SLICEMOE_ERR_INVALID_ARG;
     if (misaligned(stats, 8) || (y && y == sum)) return SLICEMOE_ERR_INVALID_ARG;
+    for (const void *p : {post_weight, gate, pre_weight, (const void *)y_mx})   // what every row reads, and a third output
+        if (p && (p == sum || p == y)) return SLICEMOE_ERR_INVALID_ARG;
+    for (const void *p : {x, post_weight, gate, residual, pre_weight})
+        if (y_mx && p == y_mx) return SLICEMOE_ERR_INVALID_ARG;
     return status_of(launch_block_norm(*cfg, x, post_weight, gate, residual, pre_weight, sum, y, (uint8_t *)y_mx, y_bits, stats, (hipStream_t)stream));
 }
 

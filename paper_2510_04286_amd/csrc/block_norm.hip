@@ -137,7 +137,7 @@ template <bool LEAN, typename T> __device__ __forceinline__ const T *per_row(con
 }
 
 // A block takes the rows b, b + gridDim.x, .. (W = 1: each of its wavefronts one of four).  gate_ld: 0 for a gate of one row.  sum and y may
-// be x or residual: a row's owners have all of it in registers before the first of them stores.
+// be x or residual: a row's owners have requested all of it before the first of them stores.
 template <typename T, int MODE, int W, int NP, bool MX>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const T *x, const T *__restrict__ post, const T *__restrict__ gate, long long gate_ld,
                                                                         const T *residual, float a, const T *__restrict__ pre, T *sum, T *y,
@@ -181,6 +181,7 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const 
 #pragma unroll
             for (int i = 0; i < V; ++i) s[c][i] = RowPiece<T>::get(px[c], i);
         if (post) r1 = row_rsqrt<W, NP, V>(s, place, d, eps, k1, lds);
+        else if (MODE == kOverlapped && W > 1) __syncthreads();   // sum may be x or residual, and the last piece is another wavefront's too
         if (LEAN) factors();
 #pragma unroll
         for (int c = 0; c < NP; ++c) {

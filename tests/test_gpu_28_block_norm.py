@@ -196,6 +196,20 @@ def test_in_place(B, d, dt):
         assert all(torch.equal(o[n], want[n]) for n in want)
 
 
+@pytest.mark.parametrize("dt", [B16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [513, 1025, 1537, 2049, 4097, 5001, 8193, 16383])
+def test_in_place_without_a_norm_behind(B, d, dt):
+    """Rows whose last piece belongs to two wavefronts, with no sum over the row in front of the stores."""
+    T = 1031
+    t = inputs(T, d, dt, "channel", post=False)
+    cfg, s, y, stats, _ = forward(B, t, "channel", 0.5, 1e-5)
+    for target in ("x", "residual"):
+        u = dict(t, x=t["x"].clone(), residual=t["residual"].clone())
+        out = torch.empty_like(s)
+        B.slicemoe_block_norm(cfg, u["x"], None, u["gate"], u["residual"], u["pre"], u[target], out)
+        assert torch.equal(u[target], s) and torch.equal(out, y)
+
+
 def test_sum_alone_and_no_rows(B):
     t = inputs(5, 300, B16, "channel")
     _, s, *_ = forward(B, t, "channel", 0.5, 1e-5)
