@@ -10,8 +10,8 @@
 // v_mfma_scale_f32_32x32x64 takes 32 cycles of a SIMD with both operands in 4 bits, 64 with either in 8; with random values in the operands the
 // chip's power limit allows 6.1 and 3.7 PFLOP/s from registers alone (zeros: 8.8).
 //
-// Three kernels: up to 64 rows, bound by the weights, one pass over them straight to the registers (32 rows, 4096 x 11008: 10.5 us in 8 bits; the network
-// 12.6 + 8.8, 45 and 22.5 MB); tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits: the pair 200 us = 3.7 PFLOP/s, the
+// Up to 64 rows, bound by the weights, one pass over them straight to the registers (16 rows in 8 bits, the network with d 4096, H 11008: 12.4 + 7.5 us for 45
+// and 22.5 MB); else tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits: the pair 200 us = 3.7 PFLOP/s, the
 // second product 88 = 4.2).  Wide results and short contractions are bound by the results: 16384 x 1024 x 2816 with an addend takes 53 us, its
 // 184 MB of addend and y 36 at the rate of a copy.
 #include <type_traits>
@@ -471,9 +471,10 @@ template <typename S, typename T> static hipError_t run_tiles(MxArgs A, int f_ti
 }
 
 // ------------------------------------------------------------------------------ few rows
-// Up to 32 TR rows: bound by the weights, which cross memory once.  A block has 32 features (of one or two images), its KW wavefronts the
+// Up to 32 TR rows: bound by the weights, which cross memory once.  A block has 32 features (of one or two images), its eight wavefronts the
 // tiles of 256 columns in turn, whose fragments go straight from memory to registers (nobody else in the block needs them).  Their sums
 // meet in the LDS, added in the wavefronts' order; behind it a row's 32 features are in 16 neighbouring lanes.
+constexpr int kFewWaves = 8;   // (sixteen: equal or slower, d 4096, H 11008, 32 rows in 8 bits 25.8 us against 24.0)
 template <int BITS, bool DUAL, int TR> struct MxFewStep {
     static constexpr int IMAGES = DUAL ? 2 : 1, RP = BITS == 4 ? 4 : 8;
     u32x4 f[IMAGES][4], r[TR][RP];
@@ -520,10 +521,10 @@ template <int BITS, bool DUAL, int TR> struct MxFewStep {
     }
 };
 
-template <int BITS, bool DUAL, int TR, int KW, typename T> __global__ __launch_bounds__(64 * KW, TR == 1 ? 4 : 2) void mx_few_kernel(MxArgs A)
+template <int BITS, bool DUAL, int TR, typename T> __global__ __launch_bounds__(64 * kFewWaves, TR == 1 ? 4 : 2) void mx_few_kernel(MxArgs A)
 {
     typedef MxFewStep<BITS, DUAL, TR> Step;
-    constexpr int IMAGES = Step::IMAGES;
+    constexpr int IMAGES = Step::IMAGES, KW = kFewWaves;
     extern __shared__ __align__(16) float sums[];   // [KW][IMAGES][64 lanes][16], pieces of four swizzled over the 64 banks
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ft = blockIdx.x;
@@ -555,7 +556,7 @@ template <int BITS, bool DUAL, int TR, int KW, typename T> __global__ __launch_b
                     f32x4{acc[m][u][4 * q], acc[m][u][4 * q + 1], acc[m][u][4 * q + 2], acc[m][u][4 * q + 3]};
         __syncthreads();
         const int R = 32 * u + row;
-        if (tid >= 512 || R >= A.T) continue;   // (a row's lanes together)
+        if (R >= A.T) continue;   // (a row's lanes together)
         float v[IMAGES][2];
 #pragma unroll
         for (int m = 0; m < IMAGES; ++m) {
@@ -597,19 +598,87 @@ template <int BITS, bool DUAL, int TR, int KW, typename T> __global__ __launch_b
     }
 }
 
-template <int BITS, bool DUAL, int TR, int KW, typename T> static hipError_t run_few(const MxArgs &A, int f_tiles, hipStream_t s)
+// Up to 16 TR rows (groups of 16) and few features: 16 of them a block, so that twice as many CUs draw on the memory, on the instruction of 16 x 16
+// results and 128 columns (lane i + 16 g: row i and, in 4 bits, block g of four; in 8 bits 16 values each of block g / 2 and of block 2 + g / 2; the scale of
+// block b from lane i + 16 b; result r of lane i + 16 g: feature 4 g + r of row i).
+template <int BITS, int TR, typename T> __global__ __launch_bounds__(1024, 4) void mx_half_kernel(MxArgs A)
 {
-    const auto kern = mx_few_kernel<BITS, DUAL, TR, KW, T>;
-    constexpr size_t lds = (size_t)KW * (DUAL ? 2 : 1) * 4096;
+    constexpr int KW = 16, RP = BITS == 4 ? 1 : 2;
+    __shared__ __align__(16) float sums[KW][TR * 256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ft = blockIdx.x >> 1, i = lane & 15, g = lane >> 4;
+    const uint32_t piece = 1024 * (g >> 1) + 512 * (g & 1) + 16 * i, scale = 128 * (g & 1) + 4 * i;   // of row i of a tile
+    const uint32_t half = 16 * (blockIdx.x & 1);
+    // thread -> row and feature
+    const int row = tid >> 4, f = tid & 15, F = 32 * ft + half + f;
+    const bool out = tid < 256 * TR && row < A.T && F < A.N;
+    const size_t y = (size_t)row * A.N + F;
+    const float addend = out && A.addend ? Storage<T>::load((const T *)A.addend + y) : 0.f;
+    f32x4 acc[TR];
+#pragma unroll
+    for (int u = 0; u < TR; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int kt = wave; kt < A.Kt; kt += KW) {
+        const size_t t = (size_t)ft * A.Kt + kt;
+        u32x4 w[2], r[TR][2][RP];
+        int rs[TR];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) w[j] = __builtin_nontemporal_load((const u32x4 *)(A.w.v + t * 4096 + 2048 * j + piece + 16 * half));
+        const int ws = *(const int *)(A.w.s + t * 256 + scale + 4 * half) >> 8 * (g >> 1);
+#pragma unroll
+        for (int u = 0; u < TR; ++u) {
+            rs[u] = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < RP; ++q) r[u][j][q] = u32x4{0, 0, 0, 0};
+            if (16 * u + i < A.T) {   // (the others are not fetched)
+                const size_t xt = (size_t)(u >> 1) * A.Kt + kt;
+                const uint8_t *x = A.x.v + xt * (1024 * BITS) + piece + 256 * (u & 1);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int q = 0; q < RP; ++q) r[u][j][q] = *(const u32x4 *)(x + 2048 * (RP * j + q));
+                rs[u] = *(const int *)(A.x.s + xt * 256 + scale + 64 * (u & 1)) >> 8 * (g >> 1);
+            }
+        }
+        for_range<0, 2>([&](auto jj) {
+            constexpr int J = decltype(jj)::value;
+#pragma unroll
+            for (int u = 0; u < TR; ++u) {
+                i32x8 b;
+                if constexpr (BITS == 4) b = frag4(r[u][J][0]);
+                else b = frag8(r[u][J][0], r[u][J][RP - 1]);
+                acc[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag4(w[J]), b, acc[u], 4, BITS == 4 ? 4 : 0, 2 * J, ws, 2 * J, rs[u]);
+            }
+        });
+    }
+#pragma unroll
+    for (int u = 0; u < TR; ++u) *(f32x4 *)(sums[wave] + 256 * u + 4 * lane) = acc[u];
+    __syncthreads();
+    if (!out) return;
+    const int at = 256 * (row >> 4) + 64 * (f >> 2) + 4 * (row & 15) + (f & 3);
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) v += sums[k][at];
+    Storage<T>::store((T *)A.y + y, v + addend);
+}
+
+template <int BITS, bool DUAL, int TR, typename T> static hipError_t run_few(const MxArgs &A, int f_tiles, hipStream_t s)
+{
+    const auto kern = mx_few_kernel<BITS, DUAL, TR, T>;
+    constexpr size_t lds = (size_t)kFewWaves * (DUAL ? 2 : 1) * 4096;
     const hipError_t e = grant_dynamic_lds((const void *)kern, lds);
     if (e != hipSuccess) return e;
-    kern<<<(unsigned)f_tiles, 64 * KW, lds, s>>>(A);
+    kern<<<(unsigned)f_tiles, 64 * kFewWaves, lds, s>>>(A);
     return hipGetLastError();
 }
 
 // Which kernel a product takes: few rows, tiles of 128 x 128 (several blocks a CU), or of 256 x 256 (one).
-// us, few rows / tiles: 8 bits 64 rows 4096 11008 10.0 / 17.3, 11008 4096 14.7 / 15.6, 1024 2816 3.9 / 6.3; 32 rows 8.5 / 14.8, 10.5 / 14.2, 3.2 / 5.9.  4 bits
-// 64 rows 8.1 / 9.8, 11.7 / 13.6, 3.6 / 5.1; in the network at 4096 11008 29.9 / 28.6, 10.6 / 13.7 at 1024 2816.
+// us, few rows / tiles: 8 bits 64 rows 4096 11008 10.0 / 17.3, 11008 4096 12.5 / 15.6, 1024 2816 4.0 / 6.3; 32 rows 8.5 / 14.8, 9.7 / 14.2, 3.1 / 5.9.  4 bits
+// 64 rows 8.1 / 9.8, 9.0 / 13.6, 3.7 / 5.1; in the network with d 4096, H 11008 about equal (29.9 / 28.6 before the halves), 10.6 / 13.7 with 1024, 2816.
+// With few rows, 16 features a block while every block has a CU, 32 else; us, 16 / 32 of them: 16 rows in 8 bits 11008 4096 7.5 / 8.9, 4096 4096 4.2 / 5.0,
+// 2816 1024 2.8 / 3.5, 64 rows 12.5 / 15.0, 6.1 / 7.5, 4.7 / 5.2; beyond, 4096 5120 5.5 / 5.1, 11008 8192 13.4 / 11.2.
 constexpr int kFewRows = 64;
 constexpr int kMostSplits = 8, kSplitBlocks = 512;   // shares of the contraction at most, and blocks of all shares together
 struct MxChoice {
@@ -661,9 +730,13 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
 {
     const int f_tiles = DUAL ? 8 * A.hKt : A.w.tiles;
     if (A.T <= kFewRows) {
-        if (A.T > 32) return run_few<BITS, DUAL, 2, 8, T>(A, f_tiles, s);
-        // (16 wavefronts where blocks are few, 8 else: 8 bits 4096 2048 3.9 us / 4.6 with 8; 1024 11008 4.1 / 3.4)
-        return f_tiles <= 160 ? run_few<BITS, DUAL, 1, 16, T>(A, f_tiles, s) : run_few<BITS, DUAL, 1, 8, T>(A, f_tiles, s);
+        if constexpr (!DUAL)
+            if (2 * f_tiles <= num_compute_units()) {
+                const auto kern = A.T <= 16 ? mx_half_kernel<BITS, 1, T> : A.T <= 32 ? mx_half_kernel<BITS, 2, T> : mx_half_kernel<BITS, 4, T>;
+                kern<<<(unsigned)(2 * f_tiles), 1024, 0, s>>>(A);
+                return hipGetLastError();
+            }
+        return A.T > 32 ? run_few<BITS, DUAL, 2, T>(A, f_tiles, s) : run_few<BITS, DUAL, 1, T>(A, f_tiles, s);
     }
     const MxChoice c = choose(A.T, f_tiles, A.Kt, A.N, BITS, DUAL);
     if (c.large) return run_tiles<MxTile<BITS, DUAL, 4, 4, BITS == 4 ? 4 : 2, BITS == 4 ? 2 : 3>, T>(A, f_tiles, 1, nullptr, s);
