@@ -556,7 +556,8 @@ slicemoe_status slicemoe_gated_ffn_mx(const slicemoe_gated_config *cfg, int32_t 
  *   sum         [T, d] out, s in the storage dtype; may be x or residual
  *   y           [T, d] out, storage dtype; may be NULL; may be x or residual if sum is not that one
  *   y_mx        out, the same rows (y before its rounding) as microscaled values of y_bits bits: slicemoe_mx_bytes of T rows and d columns,
- *               256-byte aligned; may be NULL.  Rows past T are left as they were.  With pre_weight y or y_mx has to be there.
+ *               256-byte aligned; may be NULL (UNSUPPORTED where slicemoe_mx_bytes is 0: T > 2^30).  Rows past T are left as they were.  With
+ *               pre_weight y or y_mx has to be there.
  *   stats       [T, 2] out float, 8-byte aligned, for the backward pass: 1 / rms(x) (1 without post_weight) and 1 / rms(s); may be NULL.
  *               (Infinite for a row below 2^-126 with eps = 0; its gradients are then not finite.)
  */

@@ -268,6 +268,8 @@ slicemoe_status slicemoe_block_norm(const slicemoe_block_norm_config *cfg, const
     if (cfg->T > 0 && (!x || !residual || !sum)) return SLICEMOE_ERR_INVALID_ARG;
     if (pre_weight ? cfg->T > 0 && !y && !y_mx : y || y_mx) return SLICEMOE_ERR_INVALID_ARG;
     if (y_mx && (!bits_ok(y_bits) || misaligned(y_mx, 256))) return SLICEMOE_ERR_INVALID_ARG;
+    const slicemoe_mx_config rows = {cfg->T, cfg->d, y_bits, cfg->dtype, 0};
+    if (y_mx && validate(&rows) != SLICEMOE_OK) return SLICEMOE_ERR_UNSUPPORTED;
     for (const void *p : {x, post_weight, gate, residual, pre_weight, (const void *)sum, (const void *)y})
         if (misaligned(p, 16)) return SLICEMOE_ERR_INVALID_ARG;
     if (misaligned(stats, 8) || (y && y == sum)) return SLICEMOE_ERR_INVALID_ARG;

@@ -75,6 +75,7 @@ def test_block_norm_refusals(B):
     n = [P, R_, S_, Q, ctypes.c_void_p(1 << 23), ctypes.c_void_p(1 << 24), ctypes.c_void_p(1 << 25), ctypes.c_void_p(1 << 26)]
     for a, b in ((5, 1), (5, 2), (5, 4), (6, 1), (6, 2), (6, 4), (6, 5), (7, 0), (7, 1), (7, 2), (7, 3), (7, 4), (7, 5), (7, 6)):   # outputs in the place of what all rows read, or of each other
         assert f(by(token), *[n[b] if i == a else v for i, v in enumerate(n)], 4, NULL, NULL) == inv, (a, b)
+    assert f(by(cfg((1 << 30) + 1, 1, gate="token")), *n, 4, NULL, NULL) == uns        # more rows than microscaled values have
     assert f(by(none), P, P, P, P, P, Q, P, NULL, 0, NULL, NULL) == inv      # a gate that the configuration does not have
     # x, post, gate, sum, pre, stats, d_y, d_sum, d_x, d_residual, d_post, d_gate, d_pre
     good = [P, P, Q, P, P, P, P, P, R_, S_, P, Q, P]
