@@ -676,7 +676,7 @@ template <int BITS, bool DUAL, int TR, typename T> static hipError_t run_few(con
 
 // Which kernel a product takes: few rows, tiles of 128 x 128 (several blocks a CU), or of 256 x 256 (one).
 // us, few rows / tiles: 8 bits 64 rows 4096 11008 10.0 / 17.3, 11008 4096 12.5 / 15.6, 1024 2816 4.0 / 6.3; 32 rows 8.5 / 14.8, 9.7 / 14.2, 3.1 / 5.9.  4 bits
-// 64 rows 8.1 / 9.8, 9.0 / 13.6, 3.7 / 5.1; in the network with d 4096, H 11008 about equal (29.9 / 28.6 before the halves), 10.6 / 13.7 with 1024, 2816.
+// 64 rows 8.1 / 9.8, 9.0 / 13.6, 3.7 / 5.1; in the network with d 4096, H 11008 see `second_round`.
 // With few rows, 16 features a block while every block has a CU, 32 else; us, 16 / 32 of them: 16 rows in 8 bits 11008 4096 7.5 / 8.9, 4096 4096 4.2 / 5.0,
 // 2816 1024 2.8 / 3.5, 64 rows 12.5 / 15.0, 6.1 / 7.5, 4.7 / 5.2; beyond, 4096 5120 5.5 / 5.1, 11008 8192 13.4 / 11.2.
 constexpr int kFewRows = 64;
@@ -729,7 +729,11 @@ static size_t shares_bytes(long long T, int N, int Kt)
 template <int BITS, bool DUAL, typename T> static hipError_t run_product(const MxArgs &A, float *shares, hipStream_t s)
 {
     const int f_tiles = DUAL ? 8 * A.hKt : A.w.tiles;
-    if (A.T <= kFewRows) {
+    // A pair of more than 32 rows has one block of few rows a CU: a second round of them loses to the tiles, but for long rows in 8 bits.  The network, us, few
+    // rows / tiles for the pair: H 8192, 48 rows: 4 bits d 4096 17.6 / 22.6, d 1024 12.1 / 12.0, 8 bits 21.5 / 32.4, 14.5 / 15.6; H 11008: 4 bits 26.1 / 25.2,
+    // 16.6 / 13.3, 8 bits 32.5 / 34.7, 20.6 / 16.8.  (32 rows, H 11008: 4 bits 20.5 / 22.8, 11.9 / 11.0, 8 bits 23.8 / 31.6, 13.8 / 13.9.)
+    const bool second_round = DUAL && A.T > 32 && f_tiles > num_compute_units() && (BITS == 4 || A.Kt <= 8);
+    if (A.T <= kFewRows && !second_round) {
         if constexpr (!DUAL)
             if (2 * f_tiles <= num_compute_units()) {
                 const auto kern = A.T <= 16 ? mx_half_kernel<BITS, 1, T> : A.T <= 32 ? mx_half_kernel<BITS, 2, T> : mx_half_kernel<BITS, 4, T>;
