@@ -684,25 +684,26 @@ constexpr int kMostSplits = 8, kSplitBlocks = 512;   // shares of the contractio
 struct MxChoice {
     bool large;
     int splits;
+    bool alone;   // at most one block a CU
 };
-// us of a step of 256 columns, fitted to products of 64 to 16384 rows at K 1024 to 11008 (T, K, N: 128 tiles / 256 tiles, us):
-//   4 bits   16384 1024 2816: 53.9 / 56.8   2048 11008 4096: 47.9 / 56.6   4096 11008 4096: 92.4 / 84.3   1024 2816 1024: 9.0 / 21.8
-//   8 bits   16384 2816 1024: 50.6 / 42.6   2048 11008 4096: 72.0 / 94.3   4096 11008 4096: 153 / 124     1024 2816 1024: 12.6 / 31.4
-// and in shares, 128 tiles, 1 / 2 / 4 / 8 of them: 4 bits 128 11008 4096 27.4 / 20.6 / 17.0 / 17.8, 512 11008 4096 32.1 / 27.8 / 28.2 / 37.3; 8 bits
-// 128 11008 4096 51.1 / 31.3 / 22.2 / 19.8, 1024 11008 4096 55.5 / 52.6 / 60.3 / 77.0.
+// us of a step of 256 columns, fitted to products of 66 to 16384 rows at K 1024 to 11008 (T, K, N: 128 tiles / 256 tiles, us):
+//   4 bits   2048 4096 11008: 55.2 / 57.6   4096 4096 11008: 104.5 / 93.5   4096 11008 4096: 93.0 / 77.8   2048 11008 4096: 49.0 / 59.2   1024 2816 1024: 7.8 / 18.6
+//   8 bits   2048 4096 11008: 76.3 / 87.2   4096 4096 11008: 144 / 137   4096 11008 4096: 131 / 117   2048 11008 4096: 69.3 / 97.5   1024 2816 1024: 10.2 / 28.5
+// and in shares, 128 tiles, 1 / 2 / 4 / 8 of them: 4 bits 66 11008 4096 18.1 / 13.7 / 12.0 / 13.1, 200 11008 4096 19.1 / 16.1 / 17.4 / 20.3, 512 11008 4096 20.3 / 22.3 /
+// 27.8; 8 bits 66 11008 4096 27.0 / 18.0 / 13.9 / 14.1, 128 11008 4096 27.7 / 19.4 / 16.6 / 17.5, 512 11008 4096 30.4 / 27.9 / 31.9.
 struct MxCosts {
     double one, each, start;   // 128 tiles: a block alone on its CU, every further one, beginning and end of a block
     int per_cu;
     double large, large_start;
 };
-static constexpr MxCosts kMxCosts4 = {0.77, 0.32, 2.7, 2, 1.96, 9.0}, kMxCosts8 = {1.25, 0.5, 3.0, 3, 2.85, 9.0};
+static constexpr MxCosts kMxCosts4 = {0.48, 0.55, 2.7, 2, 1.55, 9.0}, kMxCosts8 = {0.73, 0.72, 3.0, 2, 2.45, 9.0};
 static MxChoice choose(long long T, int f_tiles, int Kt, int N, int bits, bool dual)
 {
     const MxCosts &c = bits == 4 ? kMxCosts4 : kMxCosts8;
     const long long cus = num_compute_units(), per = dual ? 2 : 4;
     const auto blocks = [&](int rows, int tiles) { return ((T + rows - 1) / rows) * ((f_tiles + tiles - 1) / tiles); };
     const long long small = blocks(128, per), large = blocks(256, 2 * per);
-    MxChoice best = {true, 1};
+    MxChoice best = {true, 1, false};
     const long long left = large % cus;   // a partial round's steps are shorter: 1.3 of 2 with half of the chip
     double least = Kt * c.large * (large / cus + (left ? 0.6 + 0.4 * left / cus : 0)) + c.large_start * ((large + cus - 1) / cus);
     for (int s = 1; s <= kMostSplits && s <= Kt; s *= 2) {
@@ -713,7 +714,7 @@ static MxChoice choose(long long T, int f_tiles, int Kt, int N, int bits, bool d
         if (s > 1) t += 5 + (double)s * T * N * 8 / 4e6;   // the shares' addition: a launch, and their sums through the caches
         if (t < least) {
             least = t;
-            best = {false, s};
+            best = {false, s, n <= cus};
         }
     }
     return best;
@@ -744,7 +745,13 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
     }
     const MxChoice c = choose(A.T, f_tiles, A.Kt, A.N, BITS, DUAL);
     if (c.large) return run_tiles<MxTile<BITS, DUAL, 4, 4, BITS == 4 ? 4 : 2, BITS == 4 ? 2 : 3>, T>(A, f_tiles, 1, nullptr, s);
-    return run_tiles<MxTile<BITS, DUAL, 2, 2, BITS == 4 ? 4 : 2, 2>, T>(A, f_tiles, c.splits, shares, s);
+    // Rings of 128 x 128 tiles.  8 bits: three images, two blocks a CU (us with two images and three blocks / three and two: 1024 11008 4096 55.4 / 37.1, the pair
+    // 1024 4096 11008 83 / 80, 16384 1024 2816 48.3 / 48.4).  4 bits: four images of half the step, two blocks a CU (with two whole ones / so: the network, 1024
+    // rows, 4096 11008 91.3 / 85.4, 256 rows, 1024 2816 16.0 / 14.8, 16384 1024 2816 110.7 / 110.6), where no CU has a second block three whole ones (700
+    // 11008 4096 29.9 / 25.7 / 21.6; with a second block 512 4096 11008 19.3 / 19.7 / 20.9).
+    if constexpr (BITS == 8) return run_tiles<MxTile<8, DUAL, 2, 2, 2, 3>, T>(A, f_tiles, c.splits, shares, s);
+    else if (c.alone) return run_tiles<MxTile<4, DUAL, 2, 2, 4, 3>, T>(A, f_tiles, c.splits, shares, s);
+    else return run_tiles<MxTile<4, DUAL, 2, 2, 2, 4>, T>(A, f_tiles, c.splits, shares, s);
 }
 
 size_t mx_product_workspace(const slicemoe_mx_product_config &c) { return align_up(shares_bytes(c.T, c.N, mx_tiles_k(c.K)), 256); }
