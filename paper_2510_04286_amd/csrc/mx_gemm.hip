@@ -11,8 +11,8 @@
 // chip's power limit allows 6.1 and 3.7 PFLOP/s from registers alone (zeros: 8.8).
 //
 // Up to 64 rows, bound by the weights, one pass over them straight to the registers (16 rows in 8 bits, the network with d 4096, H 11008: 12.4 + 7.5 us for 45
-// and 22.5 MB); else tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits: the pair 200 us = 3.7 PFLOP/s, the
-// second product 88 = 4.2).  Wide results and short contractions are bound by the results: 16384 x 1024 x 2816 with an addend takes 53 us, its
+// and 22.5 MB); else tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits: the pair 194 us = 3.8 PFLOP/s, the
+// second product 83 = 4.4).  Wide results and short contractions are bound by the results: 16384 x 1024 x 2816 with an addend takes 53 us, its
 // 184 MB of addend and y 36 at the rate of a copy.
 #include <type_traits>
 
