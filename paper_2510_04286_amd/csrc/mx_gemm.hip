@@ -105,7 +105,7 @@ template <int BITS> __device__ __forceinline__ void store_hidden(const MxArgs &A
 
 // ------------------------------------------------------------------------------ tiles
 // One block of four wavefronts, 2 x 2, each with TR x TF fragments of 32 rows and features.  DUAL: half of a wavefront's feature tiles
-// come from w, half from w2.  A step is 128 bytes of a row: 256 columns in 4 bits, 128 in 8; its images come straight from memory to the
+// come from w, half from w2.  A step is KS instructions of 64 columns (256 columns, or 128); its images come straight from memory to the
 // LDS as linear kilobytes and are read as they lie.  A ring of SLOTS images; one barrier per step, a fragment before its end: behind it
 // the next step's images have landed for every wavefront, and the present ones, whose last fragments are in registers, are free for the
 // step SLOTS ahead.
