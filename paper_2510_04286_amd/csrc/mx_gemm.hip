@@ -684,7 +684,7 @@ constexpr int kMostSplits = 8, kSplitBlocks = 512;   // shares of the contractio
 struct MxChoice {
     bool large;
     int splits;
-    bool alone;   // at most one block a CU
+    long long blocks;
 };
 // us of a step of 256 columns, fitted to products of 66 to 16384 rows at K 1024 to 11008 (T, K, N: 128 tiles / 256 tiles, us):
 //   4 bits   2048 4096 11008: 55.2 / 57.6   4096 4096 11008: 104.5 / 93.5   4096 11008 4096: 93.0 / 77.8   2048 11008 4096: 49.0 / 59.2   1024 2816 1024: 7.8 / 18.6
@@ -703,7 +703,7 @@ static MxChoice choose(long long T, int f_tiles, int Kt, int N, int bits, bool d
     const long long cus = num_compute_units(), per = dual ? 2 : 4;
     const auto blocks = [&](int rows, int tiles) { return ((T + rows - 1) / rows) * ((f_tiles + tiles - 1) / tiles); };
     const long long small = blocks(128, per), large = blocks(256, 2 * per);
-    MxChoice best = {true, 1, false};
+    MxChoice best = {true, 1, large};
     const long long left = large % cus;   // a partial round's steps are shorter: 1.3 of 2 with half of the chip
     double least = Kt * c.large * (large / cus + (left ? 0.6 + 0.4 * left / cus : 0)) + c.large_start * ((large + cus - 1) / cus);
     for (int s = 1; s <= kMostSplits && s <= Kt; s *= 2) {
@@ -714,7 +714,7 @@ static MxChoice choose(long long T, int f_tiles, int Kt, int N, int bits, bool d
         if (s > 1) t += 5 + (double)s * T * N * 8 / 4e6;   // the shares' addition: a launch, and their sums through the caches
         if (t < least) {
             least = t;
-            best = {false, s, n <= cus};
+            best = {false, s, n};
         }
     }
     return best;
@@ -749,8 +749,13 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
     // 1024 4096 11008 83 / 80, 16384 1024 2816 48.3 / 48.4).  4 bits: four images of half the step, two blocks a CU (with two whole ones / so: the network, 1024
     // rows, 4096 11008 91.3 / 85.4, 256 rows, 1024 2816 16.0 / 14.8, 16384 1024 2816 110.7 / 110.6), where no CU has a second block three whole ones (700
     // 11008 4096 29.9 / 25.7 / 21.6; with a second block 512 4096 11008 19.3 / 19.7 / 20.9).
-    if constexpr (BITS == 8) return run_tiles<MxTile<8, DUAL, 2, 2, 2, 3>, T>(A, f_tiles, c.splits, shares, s);
-    else if (c.alone) return run_tiles<MxTile<4, DUAL, 2, 2, 4, 3>, T>(A, f_tiles, c.splits, shares, s);
+    // Short contractions in 8 bits, where results count, take three blocks a CU: 4096 1024 2816 with an addend 17.8 / 18.8, 16384 256 768 11.9 / 13.7; of at most
+    // two blocks a CU 4096 512 1408 9.5 / 9.0.
+    const int cus = num_compute_units();
+    if constexpr (BITS == 8) {
+        if (A.Kt <= 4 && c.blocks > 2 * cus) return run_tiles<MxTile<8, DUAL, 2, 2, 2, 2>, T>(A, f_tiles, c.splits, shares, s);
+        return run_tiles<MxTile<8, DUAL, 2, 2, 2, 3>, T>(A, f_tiles, c.splits, shares, s);
+    } else if (c.blocks <= cus) return run_tiles<MxTile<4, DUAL, 2, 2, 4, 3>, T>(A, f_tiles, c.splits, shares, s);
     else return run_tiles<MxTile<4, DUAL, 2, 2, 2, 4>, T>(A, f_tiles, c.splits, shares, s);
 }
 

@@ -110,7 +110,7 @@ def test_ends_of_the_range(B, bits):
 
 SHAPES = [(1, 1, 1), (1, 33, 7), (2, 256, 64), (16, 300, 129), (31, 1000, 96), (33, 257, 100), (64, 512, 256), (65, 513, 255), (100, 2000, 333), (128, 64, 40),
           (200, 768, 1000), (257, 511, 257), (300, 1025, 513), (513, 1300, 130), (130, 5000, 264), (257, 2816, 500), (1025, 4096, 130), (4100, 2048, 2050),
-          (1, 1, 4097), (17, 300, 4200), (40, 513, 4096), (64, 257, 5003), (16, 4500, 4100)]
+          (1, 1, 4097), (17, 300, 4200), (40, 513, 4096), (64, 257, 5003), (16, 4500, 4100), (8200, 300, 1100)]
 
 
 @pytest.mark.parametrize("bits", [4, 8])
@@ -137,7 +137,7 @@ def test_product(B, T, K, N, dt, bits):
 
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("T,d,H", [(1, 1, 1), (1, 40, 33), (2, 256, 256), (16, 512, 1000), (31, 300, 257), (33, 257, 96), (64, 1024, 300), (65, 768, 513), (129, 200, 1100),
-                                   (256, 1000, 2047), (300, 513, 100), (520, 264, 800), (20, 300, 8300), (48, 300, 8300), (64, 2100, 8200)])
+                                   (256, 1000, 2047), (300, 513, 100), (520, 264, 800), (20, 300, 8300), (48, 300, 8300), (64, 2100, 8200), (4100, 300, 1100)])
 def test_gated_network(B, T, d, H, bits):
     x, add = rand((T, d), 1, B16), rand((T, d), 2, B16)
     w = {"Wg": rand((d, H), 3, B16, d ** -0.5), "Wu": rand((d, H), 4, B16, d ** -0.5), "Wd": rand((H, d), 5, B16, H ** -0.5)}
