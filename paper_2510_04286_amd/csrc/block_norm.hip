@@ -24,19 +24,24 @@ namespace slicemoe {
 
 // How a row's pieces lie: whole and aligned; or each at any element, the last one the V elements in front of the row's end, of which the first
 // `cut` are another lane's too (they count once in the sums, both lanes store them alike): no branch between the requests (12289 x 767 in bf16
-// backward: 36.7 us, 81 with a branch for the last piece); or by element, for rows below a piece and where a lane's columns
-// have to be its own (microscaled rows).
-enum { kAligned, kOverlapped, kByElement };
+// backward: 36.7 us, 81 with a branch for the last piece); kShared: the same, and these two lanes are in two wavefronts, so that in place the store of one may
+// meet the load of the other, for which a barrier alone does not wait (a mode of its own: with the wait in both, rows of 8191 in bf16 need 68 registers for
+// 62 and have one block a CU for two: 8192 of them 190 us for 161); or by element, for rows below a piece and where a lane's columns have to be its
+// own (microscaled rows).
+enum { kAligned, kOverlapped, kShared, kByElement };
+// What this wavefront has requested has arrived.
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 template <typename T, int MODE> struct Place {
+    static constexpr bool OVERLAPS = MODE == kOverlapped || MODE == kShared;
     static constexpr int V = RowPiece<T>::V;
     int from, cut;
     bool mine;
-    __device__ __forceinline__ Place(int at, int d) : from(MODE == kOverlapped && at + V > d ? d - V : at), cut(at - from), mine(at < d) {}
+    __device__ __forceinline__ Place(int at, int d) : from(OVERLAPS && at + V > d ? d - V : at), cut(at - from), mine(at < d) {}
     __device__ __forceinline__ uint32_t bytes() const { return (uint32_t)from * (uint32_t)sizeof(T); }   // (32 bits on a row's uniform start)
     __device__ __forceinline__ u32x4 load(const T *row, int d) const
     {
         if constexpr (MODE == kByElement) return load_piece<T, false>(row, from, d);
-        else if constexpr (MODE == kOverlapped) return *(const loose *)((const char *)row + bytes());
+        else if constexpr (OVERLAPS) return *(const loose *)((const char *)row + bytes());
         else {   // (zeros past the row's end)
             u32x4 p = *(const u32x4 *)((const char *)row + (mine ? bytes() : 0u));
 #pragma unroll
@@ -48,7 +53,7 @@ template <typename T, int MODE> struct Place {
     {
         if (!mine) return;
         if constexpr (MODE == kByElement) store_piece<T, false>(row, from, d, v);
-        else if constexpr (MODE == kOverlapped) *(loose *)((char *)row + bytes()) = RowPiece<T>::make(v);
+        else if constexpr (OVERLAPS) *(loose *)((char *)row + bytes()) = RowPiece<T>::make(v);
         else *(u32x4 *)((char *)row + bytes()) = RowPiece<T>::make(v);
     }
     // sum + f(0) + .. + f(V - 1), of the elements that are this lane's.
@@ -57,7 +62,7 @@ template <typename T, int MODE> struct Place {
         float t = sum;
 #pragma unroll
         for (int i = 0; i < V; ++i) t += f(i);
-        if constexpr (MODE == kOverlapped)
+        if constexpr (OVERLAPS)
             if (cut > 0) {
                 t = sum;
 #pragma unroll
@@ -81,8 +86,8 @@ template <int W, int NP, int V, typename P> __device__ __forceinline__ float row
         for (int c = 0; c < NP; ++c)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const uint32_t a = __float_as_uint(v[c][i]) & 0x7fffffffu;   // (elements of the row in any case)
-                top = a > top ? a : top;
+                const uint32_t a = __float_as_uint(v[c][i]) & 0x7fffffffu;
+                top = place(c).mine && a > top ? a : top;   // (a lane behind the row's end may have loaded what another wavefront has stored since)
             }
         k = range_factor(row_max<W>(top, lds), eps);
         ss = 0.f;
@@ -137,7 +142,7 @@ template <bool LEAN, typename T> __device__ __forceinline__ const T *per_row(con
 }
 
 // A block takes the rows b, b + gridDim.x, .. (W = 1: each of its wavefronts one of four).  gate_ld: 0 for a gate of one row.  sum and y may
-// be x or residual: a row's owners have requested all of it before the first of them stores.
+// be x or residual: a row's owners have all of it before the first of them stores.
 template <typename T, int MODE, int W, int NP, bool MX>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const T *x, const T *__restrict__ post, const T *__restrict__ gate, long long gate_ld,
                                                                         const T *residual, float a, const T *__restrict__ pre, T *sum, T *y,
@@ -180,8 +185,9 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256) void block_norm_kernel(const 
         for (int c = 0; c < NP; ++c)
 #pragma unroll
             for (int i = 0; i < V; ++i) s[c][i] = RowPiece<T>::get(px[c], i);
+        if (MODE == kShared) wait_for_loads();   // sum may be x or residual: in front of the row's barrier everybody has its pieces
         if (post) r1 = row_rsqrt<W, NP, V>(s, place, d, eps, k1, lds);
-        else if (MODE == kOverlapped && W > 1) __syncthreads();   // sum may be x or residual, and the last piece is another wavefront's too
+        else if (MODE == kShared) __syncthreads();
         if (LEAN) factors();
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
@@ -448,15 +454,21 @@ template <typename T, bool OVERLAP, typename F> static hipError_t pick_block_row
     const int pieces = (d + V - 1) / V;
     const auto go = [&](auto mode) {
         constexpr int M = decltype(mode)::value;
+        const auto wide = [&](auto w, auto np) {
+            constexpr int W = decltype(w)::value, NP = decltype(np)::value;
+            if constexpr (M == kOverlapped)
+                if (pieces % 64 == 1) return f.template run<T, kShared, W, NP>();
+            return f.template run<T, M, W, NP>();
+        };
         if (pieces <= 64) return f.template run<T, M, 1, 1>();
         if (pieces <= 128) return f.template run<T, M, 1, 2>();
         if constexpr (F::kThree)
             if (pieces <= 192) return f.template run<T, M, 1, 3>();
-        if (pieces <= 256) return f.template run<T, M, 4, 1>();
-        if (pieces <= 512) return f.template run<T, M, 4, 2>();
-        if (pieces <= 1024) return f.template run<T, M, 16, 1>();
-        if (V == 8 || pieces <= 2048) return f.template run<T, M, 16, 2>();
-        if constexpr (V == 4) return f.template run<T, M, 16, 4>();   // (bf16 rows end at 2048 pieces)
+        if (pieces <= 256) return wide(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+        if (pieces <= 512) return wide(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+        if (pieces <= 1024) return wide(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+        if (V == 8 || pieces <= 2048) return wide(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+        if constexpr (V == 4) return wide(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());   // (bf16 rows end at 2048 pieces)
         return hipErrorInvalidValue;
     };
     if (d % V == 0) return go(std::integral_constant<int, kAligned>());

@@ -238,3 +238,25 @@ def test_offsets_beyond_32_bits(B):
     st = torch.empty((T, 2), device="cuda")
     B.slicemoe_block_norm(bc, big["x"], t["post"], t["gate"], res, t["pre"], bs, by, stats=st)
     assert torch.equal(bs[-last:], s) and torch.equal(by[-last:], y) and torch.equal(st[-last:], stats)
+
+
+# rows whose last piece belongs to two wavefronts, four or sixteen of them a row
+SHARED_PIECE = [513, 1025, 1537, 2049, 4097, 5001, 8193, 16383]
+
+
+@pytest.mark.parametrize("dt", [B16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", SHARED_PIECE)
+def test_in_place_of_rows_with_a_shared_piece(B, d, dt):
+    """The sum, and y, in the place of the block's output and of the stream: no wavefront's rows are overwritten before it has them."""
+    T = 1031
+    for gate, post in (("channel", True), ("token", True), (None, False)):
+        t = inputs(T, d, dt, gate, post)
+        t["x"][::5], t["residual"][::3] = t["x"][::5] * 2.0 ** 70, t["residual"][::3] * 2.0 ** 70      # (some out of the squares' range)
+        cfg, s, y, stats, _ = forward(B, t, gate, 0.5, 1e-5)
+        for target, other in (("x", "residual"), ("residual", "x")):
+            for y_target in (other, None):
+                u = dict(t, x=t["x"].clone(), residual=t["residual"].clone())
+                out = u[y_target] if y_target else torch.empty_like(s)
+                st = torch.empty_like(stats)
+                B.slicemoe_block_norm(cfg, u["x"], u["post"], u["gate"], u["residual"], u["pre"], u[target], out, stats=st)
+                assert torch.equal(u[target], s) and torch.equal(out, y) and torch.equal(st, stats)
