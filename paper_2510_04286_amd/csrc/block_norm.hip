@@ -231,7 +231,8 @@ template <int W> __device__ __forceinline__ float row_sum_once(float v, float *l
     return v;
 }
 
-// part: [2][gridDim.x][d] column sums of dy n2 and of ds n1 (TOKEN: times the gate).  d_x may be d_y, d_residual may be d_sum (or d_y).
+// part: [2][gridDim.x][d] column sums of dy n2 and of ds n1 (TOKEN: times the gate).  d_x and d_residual may be d_y and d_sum: a row's owners have all
+// of it in front of its first barrier, and store behind that.
 template <typename T, int MODE, int W, int NP, bool TOKEN>
 __global__ __launch_bounds__(W == 16 ? 1024 : 256, W == 16 ? 4 : 2) void block_norm_backward_kernel(const T *__restrict__ x, const T *__restrict__ post, const T *__restrict__ gate,
                                                                                  const T *__restrict__ sum, const T *__restrict__ pre,
@@ -326,6 +327,7 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256, W == 16 ? 4 : 2) void block_n
             }
             turn();
         }
+        if (MODE == kShared) wait_for_loads();   // d_residual may be d_sum, which nobody has used yet
         const float r1 = r.x, r2 = r.y;
         if (AHEAD && row + stride < rows) {
             request(row + stride);

@@ -260,3 +260,23 @@ def test_in_place_of_rows_with_a_shared_piece(B, d, dt):
                 st = torch.empty_like(stats)
                 B.slicemoe_block_norm(cfg, u["x"], u["post"], u["gate"], u["residual"], u["pre"], u[target], out, stats=st)
                 assert torch.equal(u[target], s) and torch.equal(out, y) and torch.equal(st, stats)
+
+
+@pytest.mark.parametrize("dt", [B16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", SHARED_PIECE)
+def test_backward_in_place_of_rows_with_a_shared_piece(B, d, dt):
+    """The gradients in the place of those that arrive, either way round and each alone."""
+    T = 1031
+    for gate, post in (("channel", True), ("token", True), (None, False)):
+        t = inputs(T, d, dt, gate, post)
+        cfg, s, y, stats, _ = forward(B, t, gate, 0.5, 1e-5)
+        dy, dsum = rows(T, d, dt, 8, 0.1), rows(T, d, dt, 9, 0.1)
+        want = backward(B, cfg, t, s, stats, dy, dsum)
+        ws = torch.empty(B.slicemoe_block_norm_backward_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        for dx_at, dr_at in (("dy", "dsum"), ("dsum", "dy"), (None, "dsum"), ("dsum", None), (None, "dy"), ("dy", None)):
+            g = {"dy": dy.clone(), "dsum": dsum.clone()}
+            o = {n: torch.empty_like(v) for n, v in want.items()}
+            o["d_x"], o["d_residual"] = g.get(dx_at, o["d_x"]), g.get(dr_at, o["d_residual"])
+            B.slicemoe_block_norm_backward(cfg, t["x"], t["post"], t["gate"], s, t["pre"], stats, g["dy"], o["d_x"], o["d_residual"], o.get("d_post"),
+                                           o.get("d_gate"), o["d_pre"], ws, d_sum=g["dsum"])
+            assert all(torch.equal(o[n], want[n]) for n in want), (gate, dx_at, dr_at)
