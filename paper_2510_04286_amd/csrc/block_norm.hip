@@ -288,7 +288,7 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256, W == 16 ? 4 : 2) void block_n
                 else if (i % 4 == 0) *slot(q, c, i / 4) = f32x4{0.f, 0.f, 0.f, 0.f};
             }
     }
-    const float inv_d = 1.f / d, normed = post ? inv_d : 0.f;   // without a norm behind the block d_x is m1
+    const float inv_d = 1.f / d;
     const long long stride = (long long)gridDim.x * ROWS;
     long long row = (long long)blockIdx.x * ROWS + (W == 1 ? wave : 0);
     constexpr bool AHEAD = W < 16 && NP < 4;   // (where the registers hold two rows)
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(W == 16 ? 1024 : 256, W == 16 ? 4 : 2) void block_n
             if (APART) keep_packed(cx[c]);
             turn();
         }
-        const float mn1 = row_sum_once<W>(along, lds[1]) * normed;
+        const float dot = row_sum_once<W>(along, lds[1]), mn1 = post ? dot * inv_d : 0.f;   // without a norm behind the block d_x is m1, and the sum may overflow
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
             float v[V];

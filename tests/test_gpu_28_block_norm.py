@@ -280,3 +280,20 @@ def test_backward_in_place_of_rows_with_a_shared_piece(B, d, dt):
             B.slicemoe_block_norm_backward(cfg, t["x"], t["post"], t["gate"], s, t["pre"], stats, g["dy"], o["d_x"], o["d_residual"], o.get("d_post"),
                                            o.get("d_gate"), o["d_pre"], ws, d_sum=g["dsum"])
             assert all(torch.equal(o[n], want[n]) for n in want), (gate, dx_at, dr_at)
+
+
+@pytest.mark.parametrize("dt", [B16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [100, 1000, 5000])
+def test_gradients_without_a_norm_behind_of_large_values(B, d, dt):
+    """d_x is then d_s times the gate, whatever the block's output: the sum of d_s x, which leaves fp32 here, has no part in it."""
+    T = 9
+    for gate in (None, "token"):
+        t = inputs(T, d, dt, gate, post=False)
+        t["x"][::2] = t["x"][::2] * 2.0 ** 100
+        cfg, s, y, stats, _ = forward(B, t, gate, 0.5, 1e-5)
+        dy, dsum = rows(T, d, dt, 8, 0.1), rows(T, d, dt, 9, 2.0 ** 40)
+        out = backward(B, cfg, t, s, stats, dy, dsum)
+        ref = N.backward(t["x"], None, t["gate"], s, t["pre"], stats, dy, dsum, 0.5, dt, gate == "token")
+        for name in ("d_x", "d_residual"):
+            assert bool(out[name].isfinite().all())
+            R.within(out[name], *ref[name], f"{name} {gate}")
