@@ -560,6 +560,7 @@ slicemoe_status slicemoe_gated_ffn_mx(const slicemoe_gated_config *cfg, int32_t 
  *               pre_weight y or y_mx has to be there.
  *   stats       [T, 2] out float, 8-byte aligned, for the backward pass: 1 / rms(x) (1 without post_weight) and 1 / rms(s); may be NULL.
  *               (Infinite for a row below 2^-126 with eps = 0; its gradients are then not finite.)
+ * An output in the place of an input or of another output that is not allowed here is an INVALID_ARG.
  */
 typedef enum { SLICEMOE_GATE_NONE = 0, SLICEMOE_GATE_CHANNEL = 1, SLICEMOE_GATE_TOKEN = 2 } slicemoe_gate;
 typedef struct {
@@ -584,6 +585,7 @@ slicemoe_status slicemoe_block_norm(const slicemoe_block_norm_config *cfg, const
  *   d_post_weight, d_pre_weight [d] out float, overwritten (zeros for T = 0); d_post_weight is not written without post_weight
  *   d_gate SLICEMOE_GATE_CHANNEL: [d] out float, overwritten; SLICEMOE_GATE_TOKEN: [T, d] out, storage dtype; else not written
  *   workspace >= slicemoe_block_norm_backward_workspace_bytes(cfg) (0 on an invalid config), 256-byte aligned; its size never falls as T grows
+ * An output or the workspace in the place of an input or an output that is not allowed here is an INVALID_ARG.
  */
 size_t slicemoe_block_norm_backward_workspace_bytes(const slicemoe_block_norm_config *cfg);
 slicemoe_status slicemoe_block_norm_backward(const slicemoe_block_norm_config *cfg, const void *x, const void *post_weight, const void *gate,

@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <memory>
 #include <new>
 
@@ -68,6 +69,11 @@ static slicemoe_status validate_mx(const slicemoe_gated_config *c, int bits)
     if (st != SLICEMOE_OK) return st;
     if (!bits_ok(bits)) return SLICEMOE_ERR_INVALID_ARG;
     return c->dtype != SLICEMOE_BF16 || c->T > 1 << 24 || (long long)c->T * std::max(c->d, c->H) > kMxMost ? SLICEMOE_ERR_UNSUPPORTED : SLICEMOE_OK;
+}
+// Whether p (may be null) is none of the others.
+static bool apart(const void *p, std::initializer_list<const void *> others)
+{
+    return !p || std::find(others.begin(), others.end(), p) == others.end();
 }
 // A workspace of at least `need` bytes on the alignment every workspace has.
 static slicemoe_status check_workspace(const void *ws, size_t bytes, size_t need)
@@ -277,6 +283,7 @@ slicemoe_status slicemoe_block_norm(const slicemoe_block_norm_config *cfg, const
         if (p && (p == sum || p == y)) return SLICEMOE_ERR_INVALID_ARG;
     for (const void *p : {x, post_weight, gate, residual, pre_weight})
         if (y_mx && p == y_mx) return SLICEMOE_ERR_INVALID_ARG;
+    if (!apart(stats, {x, post_weight, gate, residual, pre_weight, sum, y, y_mx})) return SLICEMOE_ERR_INVALID_ARG;
     return status_of(launch_block_norm(*cfg, x, post_weight, gate, residual, pre_weight, sum, y, (uint8_t *)y_mx, y_bits, stats, (hipStream_t)stream));
 }
 
@@ -311,6 +318,14 @@ slicemoe_status slicemoe_block_norm_backward(const slicemoe_block_norm_config *c
     }
     st = check_workspace(workspace, workspace_bytes, slicemoe_block_norm_backward_workspace_bytes(cfg));
     if (st != SLICEMOE_OK) return st;
+    // what every row reads, and the workspace, stay as they are until the end; sums over the rows are apart from everything
+    const void *row_gate = token ? d_gate : nullptr, *column_gate = cfg->gate == SLICEMOE_GATE_CHANNEL ? d_gate : nullptr, *column_post = post_weight ? d_post_weight : nullptr;
+    for (const void *p : {(const void *)d_x, (const void *)d_residual, row_gate})
+        if (some && !apart(p, {post_weight, gate, pre_weight, stats, workspace})) return SLICEMOE_ERR_INVALID_ARG;
+    for (const void *p : {column_post, column_gate, (const void *)d_pre_weight})
+        if (!apart(p, {post_weight, gate, pre_weight, workspace}) || (some && !apart(p, {x, sum, stats, d_y, d_sum, d_x, d_residual, row_gate}))) return SLICEMOE_ERR_INVALID_ARG;
+    if (!apart(column_post, {column_gate, d_pre_weight}) || !apart(column_gate, {d_pre_weight})) return SLICEMOE_ERR_INVALID_ARG;
+    if (!apart(workspace, {x, post_weight, gate, sum, pre_weight, stats, d_y, d_sum})) return SLICEMOE_ERR_INVALID_ARG;
     return status_of(launch_block_norm_backward(*cfg, x, post_weight, gate, sum, pre_weight, stats, d_y, d_sum, d_x, d_residual,
                                                 post_weight ? d_post_weight : nullptr, d_gate, d_pre_weight, (float *)workspace, (hipStream_t)stream));
 }

@@ -147,3 +147,37 @@ def test_binding_checks_its_arguments(B):
         B.slicemoe_forward_few(B.make_config(4, 1024, 16, 2, 32, 256), t, {"packed": t}, t)
     with pytest.raises(TypeError):
         B.slicemoe_block_norm(B.make_block_norm_config(4, 64), t, t, t, t, t, t, t)
+
+
+def test_block_norm_outputs_in_the_place_of_others(B):
+    """Only what the header allows; a refusal of the workspace shows that a call was accepted so far (nothing is launched)."""
+    f, g, inv, wsp = B.lib().slicemoe_block_norm, B.lib().slicemoe_block_norm_backward, B.SLICEMOE_ERR_INVALID_ARG, B.SLICEMOE_ERR_WORKSPACE
+    at = lambda i: ctypes.c_void_p((i + 1) << 20)  # noqa: E731
+    # x, post, gate, residual, pre, sum, y, y_mx, bits, stats
+    n = [at(i) for i in range(8)] + [4, at(8)]
+    for gate in ("channel", "token"):
+        c = B.make_block_norm_config(4, 64, gate=gate)
+        for other in range(8):
+            assert f(by(c), *[n[other] if i == 9 else v for i, v in enumerate(n)], NULL) == inv, other
+    # x, post, gate, sum, pre, stats, d_y, d_sum, d_x, d_residual, d_post, d_gate, d_pre
+    names = ["x", "post", "gate", "sum", "pre", "stats", "d_y", "d_sum", "d_x", "d_residual", "d_post", "d_gate", "d_pre", "workspace"]
+    good = {name: at(i) for i, name in enumerate(names)}
+    allowed = {frozenset(p) for p in (("d_x", "d_y"), ("d_x", "d_sum"), ("d_residual", "d_y"), ("d_residual", "d_sum"))}
+    outputs = names[8:]
+    for gate in ("channel", "token"):
+        c = B.make_block_norm_config(4, 64, gate=gate)
+
+        def call(p, size):
+            return g(by(c), *[p[name] for name in names], size, NULL)
+        assert call(good, 0) == wsp
+        for o in outputs:
+            for other in names:
+                if other != o and frozenset((o, other)) not in allowed:
+                    assert call({**good, o: good[other]}, BIG) == inv, (gate, o, other)
+                    assert call({**good, other: good[o]}, BIG) == inv, (gate, o, other)
+        for o, other in (("d_x", "d_y"), ("d_x", "d_sum"), ("d_residual", "d_y"), ("d_residual", "d_sum")):
+            assert call({**good, o: good[other]}, 0) == wsp
+    # what the configuration does not have is not written and may be anything
+    c = B.make_block_norm_config(4, 64, gate=None)
+    p = {**good, "gate": NULL, "post": NULL, "d_gate": good["x"], "d_post": good["x"]}
+    assert g(by(c), *[p[name] for name in names], 0, NULL) == wsp
