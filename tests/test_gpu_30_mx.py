@@ -214,3 +214,53 @@ def test_no_rows(B):
         ws = torch.empty(B.slicemoe_gated_ffn_mx_workspace_bytes(gc, bits), dtype=torch.uint8, device="cuda")
         B.slicemoe_gated_ffn_mx(gc, bits, mx, w, none, ws)
     torch.cuda.synchronize()
+
+
+# many tiles over a long contraction: by the measured costs of both tiles these take 256 x 256, whatever the bits; the last tile of either side is a ragged one
+LARGE = [(4090, 2900, 4000), (4000, 2900, 4090)]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dt", [B16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,K,N", LARGE)
+def test_large_product(B, T, K, N, dt, bits):
+    """Every result, with an addend (elsewhere and in place) and without, whole pieces of a row and not."""
+    x, w, add = rand((T, K), 1, dt), rand((N, K), 2, dt, 0.2), rand((T, N), 3, dt)
+    cfg = B.make_mx_product_config(T, K, N, bits, NAME[dt])
+    (_, xm), (_, wm) = pack(B, x, bits), pack(B, w, 4)
+    ws = torch.empty(max(256, B.slicemoe_mx_product_workspace_bytes(cfg)), dtype=torch.uint8, device="cuda")
+    vx, vw = M.to_mx(x, bits), M.to_mx(w, 4)
+    guard = torch.full((T + 2, N), 7.0, dtype=dt, device="cuda")      # whole rows on both sides that must stay
+    for addend in (None, add):
+        y = guard[1:-1] if N % 8 == 0 else torch.full((T, N), 7.0, dtype=dt, device="cuda")
+        B.slicemoe_mx_product(cfg, xm, wm, y, ws, addend=addend)
+        R.within(y, *M.product(vx, vw, addend, dt, bits), "y")
+    assert bool((guard[0] == 7).all()) and bool((guard[-1] == 7).all())
+    first = y.clone()
+    y = add.clone()
+    B.slicemoe_mx_product(cfg, xm, wm, y, ws, addend=y)
+    assert torch.equal(y, first)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("T,d,H", [(4000, 4000, 4090), (3990, 3990, 4060)])
+def test_large_network(B, T, d, H, bits):
+    """Every seventh row against 64 bits, and those of the last tile.  A row's bits are the same wherever in the batch it is: the batch moved on by one to
+    six rows shows every row's place."""
+    x, add = rand((T, d), 1, B16), rand((T, d), 2, B16)
+    w = {"Wg": rand((d, H), 3, B16, d ** -0.5), "Wu": rand((d, H), 4, B16, d ** -0.5), "Wd": rand((H, d), 5, B16, H ** -0.5)}
+    packed, cfg = B.quantize_gated_weights_mx(w), B.make_gated_config(T, d, H)
+    ws = torch.full((B.slicemoe_gated_ffn_mx_workspace_bytes(cfg, bits),), 0xFF, dtype=torch.uint8, device="cuda")
+    _, xm = pack(B, x, bits)
+    y = torch.full_like(x, 7.0)
+    B.slicemoe_gated_ffn_mx(cfg, bits, xm, packed, y, ws, addend=add)
+    pick = torch.cat([torch.arange(0, T - 160, 7), torch.arange(T - 160, T)])
+    Wg, Wu, Wd = (M.to_mx(w[n].t(), 4) for n in ("Wg", "Wu", "Wd"))
+    R.within(y[pick.cuda()], *M.gated(M.to_mx(x.cpu()[pick], bits), Wg, Wu, Wd, add.cpu()[pick], bits), "y")
+    in_place = add.clone()
+    B.slicemoe_gated_ffn_mx(cfg, bits, xm, packed, in_place, ws, addend=in_place)
+    assert torch.equal(in_place, y)
+    for by in range(1, 7):
+        moved = torch.empty_like(x)
+        B.slicemoe_gated_ffn_mx(cfg, bits, pack(B, x.roll(by, 0), bits)[1], packed, moved, ws, addend=add.roll(by, 0))
+        assert torch.equal(moved, y.roll(by, 0))
