@@ -262,8 +262,9 @@ slicemoe_status slicemoe_forward(const slicemoe_config *cfg, const void *h, cons
  * The whole layer for a few tokens (a decoding step) in one launch, without a workspace: h[T, d] -> h_out[T, d] as slicemoe_forward, which
  * takes four launches whatever the batch.  A block has a slice from its router to its sum: faster than slicemoe_forward up to one or two
  * slices (T*S) per compute unit, slower from 512 slices of 128 columns and more on.  On the matrix-core path (slicemoe_uses_mfma) it reads
- * w->packed, which has to be there (the logical tensors may be NULL), and gives the bits of slicemoe_forward; otherwise it reads the logical
- * tensors, in fp32.
+ * w->packed, which has to be there (the logical tensors may be NULL), and gives the bits of slicemoe_forward where logits are numbers or, of at most E - k
+ * masked experts, -infinity; otherwise it reads the logical tensors, in fp32.  (With fewer than k experts left the masked ones follow by their index, with
+ * probability 0, an expert never twice; logits that are NaN come behind all others.  slicemoe_forward may repeat an expert there.)
  *   topk_idx, topk_p [T*S, k] out, as slicemoe_route leaves them; may be NULL, each
  *   h_out     may be h
  * UNSUPPORTED for more than SLICEMOE_FEW_ASSIGNMENTS assignments (T*S*k), for a capacity limit, and on the matrix-core path where a slice's k He

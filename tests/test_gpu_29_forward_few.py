@@ -132,3 +132,24 @@ def test_no_tokens_and_refusals(B):
         B.slicemoe_forward_few(cfg, h.float(), w, h)
     with pytest.raises(ValueError):
         B.slicemoe_forward_few(cfg, h[:3], w, h)
+
+
+@pytest.mark.parametrize("E,k", [(16, 2), (33, 2), (16, 5), (64, 8)])
+def test_masked_experts(B, E, k):
+    """Experts whose bias is -infinity: the bits of the whole forward while k are left; with fewer the masked ones follow, each once and with probability 0."""
+    for left in (E - 1, k, k - 1, 1):
+        for dtype in ("bf16", "f32"):
+            shape = wl.SliceMoEShape("masked", T=7, d=128, S=2, E=E, k=k, He=64, dtype=dtype)
+            _, h, w = make_inputs(shape)
+            keep = np.sort(np.random.default_rng(left).permutation(E)[:left])
+            masked = np.setdiff1d(np.arange(E), keep)
+            w["br2"][masked] = -np.inf
+            cfg = B.config_of(shape, flags=0 if dtype == "bf16" else B.SLICEMOE_FLAG_FORCE_GENERIC)
+            wd, hd = B.pack(cfg, B.weights_to_device(w, dtype)), B.to_device(h, dtype)
+            out, idx, p = few(B, cfg, hd, wd)
+            if left >= k and B.slicemoe_uses_mfma(cfg):
+                assert all(torch.equal(a, b) for a, b in zip((out, idx, p), whole(B, cfg, hd, wd)))
+            got = idx.cpu().numpy()
+            assert all(len(set(r)) == k for r in got.tolist())
+            assert np.isin(got[:, :min(k, left)], keep).all() and bool(out.isfinite().all())
+            assert (got[:, left:] == masked[:max(0, k - left)]).all() and bool((p[:, left:] == 0).all()) and bool((p[:, :left] > 0).all())
