@@ -100,3 +100,24 @@ def gated(x, Wg, Wu, Wd, addend, bits):
     y = f + add
     bound = eq @ Wd.abs().t() + dropped(q, Wd, bits) + (q.abs() @ Wd.abs().t()) * adds(a.shape[1]) + R.HALF[torch.bfloat16] * y.abs() + R.U * add.abs()
     return y, bound
+
+
+def dropped_in_parts(x, w):
+    """What is dropped where 8-bit rows are multiplied in two parts, values of 4 and more (in units of their block's scale) and the others: of the
+    first nothing (products from 2^1 = 4 / 8 * 1/2 to 448 * 6 < 2^12: bits from 2^-2 on are kept), of the others (below 4 * 6 < 2^5) at most the bit
+    2^-10 that a value below 2^-5 and a weight of an odd number of halves have.  The largest of a block of rows is above 224, of weights above 3."""
+    def by_block(v):
+        b = blocks(v).abs()
+        return b, b.amax(2)
+    (bx, mx), (_, mw) = by_block(x), by_block(w)
+    few = ((bx > 0) & (bx < mx[..., None] * 2.0 ** -12)).sum(2).double()
+    return 2.0 ** -10 / (224 * 3) * (few * mx) @ mw.t()
+
+
+def product_in_parts(x, w, addend):
+    """The product in fp32 storage with 8-bit rows: twice as many instructions, nothing of their operands dropped but the above."""
+    x, w = x.double(), w.double()
+    f = x @ w.t()
+    add = addend.double().cpu() if addend is not None else torch.zeros_like(f)
+    y = f + add
+    return y, (x.abs() @ w.abs().t()) * (x.shape[1] / 4 + 48) * 2.0 ** -23 + dropped_in_parts(x, w) + R.HALF[torch.float32] * y.abs() + R.U * add.abs()

@@ -264,3 +264,48 @@ def test_large_network(B, T, d, H, bits):
         moved = torch.empty_like(x)
         B.slicemoe_gated_ffn_mx(cfg, bits, pack(B, x.roll(by, 0), bits)[1], packed, moved, ws, addend=add.roll(by, 0))
         assert torch.equal(moved, y.roll(by, 0))
+
+
+# every kernel: few rows with 16 and with 32 features a block, tiles, shares of the contraction, large tiles
+IN_PARTS = [(1, 64, 5), (16, 300, 129), (33, 513, 200), (64, 1000, 96), (16, 4500, 4200), (50, 257, 5003), (66, 2000, 300), (257, 511, 257), (2000, 700, 520), (1100, 256, 4100),
+            (4090, 2900, 4000)]
+
+
+@pytest.mark.parametrize("T,K,N", IN_PARTS)
+def test_eight_bit_rows_in_fp32_storage_are_exact(B, T, K, N):
+    """Products and sums of which each, in any order, is an fp32 number: large products that cancel beside small ones 2^-17 of their size.  Rows and
+    weights are microscaled values already; a row's result in fp32 storage is the exact one."""
+    gen = torch.Generator().manual_seed(T + K + N)
+    blocks = -(-K // 32)
+    x = torch.randint(-15, 16, (T, blocks, 32), generator=gen).double() / 64          # products with weights: multiples of 2^-7, below 2
+    w = torch.randint(-2, 3, (N, blocks, 32), generator=gen).double() / 2
+    place = torch.randint(0, 32, (blocks,), generator=gen)
+    at = torch.arange(blocks)
+    sign = torch.where(at % 2 == 0, 1.0, -1.0).double()
+    x[:, at, place], w[:, at, place] = 448.0, 6.0 * sign                              # +- 2688 by turns
+    x, w = x.flatten(1)[:, :K], w.flatten(1)[:, :K]
+    y = torch.empty((T, N), device="cuda")
+    (_, xm), (_, wm) = pack(B, x.float().cuda(), 8), pack(B, w.float().cuda(), 4)
+    assert torch.equal(M.to_mx(x, 8), x) and torch.equal(M.to_mx(w, 4), w)
+    cfg = B.make_mx_product_config(T, K, N, 8, "f32")
+    ws = torch.empty(max(256, B.slicemoe_mx_product_workspace_bytes(cfg)), dtype=torch.uint8, device="cuda")
+    B.slicemoe_mx_product(cfg, xm, wm, y, ws)
+    # a sum of any of the products is a multiple of 2^-7 and below half of the large ones and all of the small ones together: 24 bits
+    exact = 2688 * ((blocks + 1) // 2) + 0.25 * K < 2.0 ** 17
+    want = x @ w.t()
+    if exact:
+        assert torch.equal(y.double().cpu(), want)
+    R.within(y, *M.product_in_parts(x, w, None), "y")
+
+
+@pytest.mark.parametrize("T,K,N", IN_PARTS)
+def test_eight_bit_rows_in_fp32_storage(B, T, K, N):
+    x, w, add = rand((T, K), 1, F32), rand((N, K), 2, F32, 0.2), rand((T, N), 3, F32)
+    cfg = B.make_mx_product_config(T, K, N, 8, "f32")
+    (_, xm), (_, wm) = pack(B, x, 8), pack(B, w, 4)
+    ws = torch.empty(max(256, B.slicemoe_mx_product_workspace_bytes(cfg)), dtype=torch.uint8, device="cuda")
+    vx, vw = M.to_mx(x, 8), M.to_mx(w, 4)
+    for addend in (add, None):
+        y = torch.full((T, N), 7.0, device="cuda")
+        B.slicemoe_mx_product(cfg, xm, wm, y, ws, addend=addend)
+        R.within(y, *M.product_in_parts(vx, vw, addend), "y")
