@@ -774,10 +774,12 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
 {
     constexpr bool WHOLE = kMxWhole<BITS, T>;
     const int f_tiles = DUAL ? 8 * A.hKt : A.w.tiles;
-    // A pair of more than 32 rows has one block of few rows a CU: a second round of them loses to the tiles, but for long rows in 8 bits.  The network, us, few
-    // rows / tiles for the pair: H 8192, 48 rows: 4 bits d 4096 17.6 / 22.6, d 1024 12.1 / 12.0, 8 bits 21.5 / 32.4, 14.5 / 15.6; H 11008: 4 bits 26.1 / 25.2,
-    // 16.6 / 13.3, 8 bits 32.5 / 34.7, 20.6 / 16.8.  (32 rows, H 11008: 4 bits 20.5 / 22.8, 11.9 / 11.0, 8 bits 23.8 / 31.6, 13.8 / 13.9.)
-    const bool second_round = DUAL && A.T > 32 && f_tiles > num_compute_units() && (BITS == 4 || A.Kt <= 8);
+    // A pair of more than 32 rows has one block of few rows a CU: a second round of them loses to the tiles.  The network, us, few rows / tiles for the pair: 48
+    // rows, H 11008, 4 bits d 512 15.8 / 13.2, 1024 16.9 / 13.9, 2048 19.8 / 17.4, 4096 26.7 / 21.6, 8 bits 19.1 / 16.0, 21.4 / 17.9, 24.7 / 22.8, 33.5 / 28.5; H 8448,
+    // d 4096 23.8 / 19.8, 29.2 / 25.8; H 16384 32.3 / 28.5, 40.9 / 35.5; 33 rows, H 11008, d 4096 25.5 / 21.3, 32.1 / 27.6.  In one round few rows are the faster ones:
+    // H 8192 4 bits d 1024 12.7 / 13.3, 4096 18.0 / 19.7, 8 bits 14.8 / 16.1, 21.8 / 25.6; and up to 32 rows, of which a CU has two blocks, in two rounds near
+    // the tiles: 32 rows, H 11008, 4 bits d 1024 12.6 / 12.1, 4096 21.4 / 19.9, 8 bits 14.4 / 14.8, 24.3 / 25.3, 17 rows 11.7 / 11.8, 19.7 / 19.9, 13.7 / 14.3, 23.0 / 24.4.
+    const bool second_round = DUAL && A.T > 32 && f_tiles > num_compute_units();
     if (A.T <= kFewRows && !second_round) {
         if constexpr (!DUAL)
             if (2 * f_tiles <= num_compute_units()) {
@@ -793,8 +795,10 @@ template <int BITS, bool DUAL, typename T> static hipError_t run_product(const M
     // 1024 4096 11008 83 / 80, 16384 1024 2816 48.3 / 48.4).  4 bits: four images of half the step, two blocks a CU (with two whole ones / so: the network, 1024
     // rows, 4096 11008 91.3 / 85.4, 256 rows, 1024 2816 16.0 / 14.8, 16384 1024 2816 110.7 / 110.6), where no CU has a second block three whole ones (700
     // 11008 4096 29.9 / 25.7 / 21.6; with a second block 512 4096 11008 19.3 / 19.7 / 20.9).
-    // Short contractions in 8 bits, where results count, take three blocks a CU: 4096 1024 2816 with an addend 17.8 / 18.8, 16384 256 768 11.9 / 13.7; of at most
-    // two blocks a CU 4096 512 1408 9.5 / 9.0.
+    // Short contractions in 8 bits, where results count, take three blocks a CU; without an addend / with one, two blocks against three: 16384 256 768 11.3 : 10.1 /
+    // 14.2 : 12.1, 16384 512 1408 20.1 : 19.3 / 24.2 : 23.2, 16384 1024 2816 46.5 : 46.9 / 52.6 : 51.5, 4096 1024 2816 15.6 : 15.7 / 18.5 : 17.7; beyond, 16384 1280 3456
+    // 66.2 : 66.2 / 72.3 : 73.9, 4096 1536 2816 19.4 : 20.4 / 22.1 : 22.0, 4096 2560 2816 27.7 : 29.4 / 29.1 : 31.1; of at most two blocks a CU 4096 512 1408 with an
+    // addend 9.0 : 9.5.
     const int cus = num_compute_units();
     if constexpr (BITS == 8) {
         if (A.Kt <= 4 && c.blocks > 2 * cus) return run_tiles<MxTile<8, DUAL, 2, 2, 2, 2, WHOLE>, T>(A, f_tiles, c.splits, shares, s);
