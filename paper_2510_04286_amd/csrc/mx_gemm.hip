@@ -10,10 +10,10 @@
 // v_mfma_scale_f32_32x32x64 takes 32 cycles of a SIMD with both operands in 4 bits, 64 with either in 8; with random values in the operands the
 // chip's power limit allows 6.1 and 3.7 PFLOP/s from registers alone (zeros: 8.8).
 //
-// Up to 64 rows, bound by the weights, one pass over them straight to the registers (16 rows in 8 bits, the network with d 4096, H 11008: 12.4 + 7.5 us for 45
-// and 22.5 MB); else tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits: the pair 194 us = 3.8 PFLOP/s, the
-// second product 83 = 4.4).  Wide results and short contractions are bound by the results: 16384 x 1024 x 2816 with an addend takes 53 us, its
-// 184 MB of addend and y 36 at the rate of a copy.
+// Up to 64 rows, bound by the weights, one pass over them straight to the registers (16 rows in 8 bits, the network with d 4096, H 11008: 12.6 + 7.0 us for 45
+// and 22.5 MB); else tiles of 128 x 128 and 256 x 256 through the LDS (4096 rows, 4096 x 11008 in 4 bits, medians of 64 passes: the pair 201 us = 3.7
+// PFLOP/s, the second product 83 = 4.4).  Wide results and short contractions are bound by the results: 16384 x 1024 x 2816 with an addend takes 53 us in one
+// process and 65 in another (least 52 in both), its 184 MB of addend and y 36 at the rate of a copy.
 #include <type_traits>
 
 #include "gemm_tile.h"
@@ -715,8 +715,9 @@ template <int BITS, bool DUAL, int TR, typename T> static hipError_t run_few(con
 }
 
 // Which kernel a product takes: few rows, tiles of 128 x 128 (several blocks a CU), or of 256 x 256 (one).
-// us, few rows / tiles: 8 bits 64 rows 4096 11008 10.0 / 17.3, 11008 4096 12.5 / 15.6, 1024 2816 4.0 / 6.3; 32 rows 8.5 / 14.8, 9.7 / 14.2, 3.1 / 5.9.  4 bits
-// 64 rows 8.1 / 9.8, 9.0 / 13.6, 3.7 / 5.1; in the network with d 4096, H 11008 see `second_round`.
+// us, few rows / tiles: 8 bits 64 rows 4096 11008 11.6 / 13.0, 11008 4096 12.7 / 14.8, 1024 2816 4.6 / 6.5; 32 rows 9.1 / 12.8, 10.0 / 12.8, 3.8 / 6.1.  4 bits
+// 64 rows 8.6 / 9.8, 9.0 / 14.3, 4.3 / 5.7; fp32 storage, 8 bits, 64 rows 15.9 / 22.7, 18.4 / 19.6, 5.3 / 9.6; 64 rows 11008 11008, a second round of blocks, 22.5 / 22.2 in
+// 4 bits, 29.4 / 26.1 in 8, 34.0 / 38.8 with fp32 storage; in the network see `second_round`.
 // With few rows, 16 features a block while every block has a CU, 32 else; us, 16 / 32 of them: 16 rows in 8 bits 11008 4096 7.5 / 8.9, 4096 4096 4.2 / 5.0,
 // 2816 1024 2.8 / 3.5, 64 rows 12.5 / 15.0, 6.1 / 7.5, 4.7 / 5.2; beyond, 4096 5120 5.5 / 5.1, 11008 8192 13.4 / 11.2.
 constexpr int kFewRows = 64;
